@@ -301,6 +301,128 @@ int rotate_attn_fwd_fp16(const ra_params* p, const void* q, const void* k, const
 int rotate_attn_fwd(const ra_params* p, int fallback, const void* q, const void* k, const void* v,
                     void* o, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * 4-bit paged KV cache
+ *
+ * For models that generate causally (frame after frame, token after token):
+ * keys and values of past tokens are kept in pages, as 4-bit codes, and a step
+ * makes four calls -- cache_plan (block tables, slots and positions from
+ * lengths), cache_append (the new tokens into the pages), cache_attn (the new
+ * queries against everything cached), and cache_read where cached tokens are
+ * wanted as dense tensors.  Tokens of a step are packed: request r owns rows
+ * q_start[r] .. q_start[r+1] of [T][heads][D] tensors, rows behind the last
+ * request are padding.
+ *
+ * All lengths, tables and slots are device data, read by the kernels when they
+ * run: a captured HIP graph follows them from replay to replay.  Values there
+ * that do not fit (a page number outside [0, num_pages), a slot or position
+ * out of range, offsets past T) touch nothing outside the tensors: keys on
+ * such a page count as masked, such tokens are not written and read as 0.
+ *
+ * Codes.  A row of D channels y (K after RoPE; times the +-1 Sylvester-Hadamard
+ * matrix, without 1/sqrt(D), where rotated) with a = max |y| is kept as E2M1
+ * floats (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign), code = E2M1(6 y / a) rounded
+ * to nearest, ties to the even code, and scale = a / 6 (times 1/sqrt(D) where
+ * rotated) in binary32.  Codes are those of 64-bit arithmetic: binary32 sums
+ * within 2^-16 of a border are done again in binary64.  A row with a < 2^-100
+ * is kept as zeros; one that is not finite has NaN for its scale, and every
+ * query that sees it gives NaN (nothing else does: masked and padding rows may
+ * hold anything).
+ *
+ * Page: for each KV head, page_size * (D + 8) bytes: K codes, V codes, K
+ * scales, V scales (ra_cache_sizes has the offsets).  For token t of the page
+ * and channel d (low nibble where d is even):
+ *   K code: byte (t/16)*8D + (d/(D/4))*2D + (t%16)*(D/8) + (d%(D/4))/2
+ *   V code: byte (t/4)*2D + (d/(D/16))*(D/8) + (t%4)*(D/32) + (d%(D/16))/2
+ * The cache may be uninitialised memory; it must be 128-byte aligned.
+ * ---------------------------------------------------------------------- */
+typedef struct ra_cache_params {
+  int32_t Hq, Hkv, D;      /* query heads, KV heads (Hq a multiple of Hkv), head dim (64 or 128) */
+  int32_t page_size;       /* tokens per page: 16, 32, 64, 128 or 256 */
+  int32_t num_pages;       /* pages of the cache */
+  int32_t max_blocks;      /* width of the block table: pages that one request can hold */
+  int32_t rotation;        /* RA_ROT_NONE or RA_ROT_HADAMARD: of K in the cache, and of Q */
+  int32_t v_rotation;      /* RA_VROT_*: of V in the cache; outputs are turned back */
+  int32_t causal;          /* 1: a query sees keys up to its own position; 0: all of its request */
+  int32_t window;          /* causal only: the last `window` keys, its own included; 0 = all */
+  float sm_scale;          /* softmax scale; 0 = 1/sqrt(D) */
+  int32_t in_dtype;        /* of q, k, v: RA_BF16 | RA_FP16 */
+  int32_t out_dtype;       /* of o and of cache_read's k, v: RA_BF16 | RA_FP16 | RA_FP32 */
+} ra_cache_params;
+
+typedef struct ra_cache_sizes {
+  int64_t head_bytes;   /* of one KV head in a page */
+  int64_t page_bytes;   /* Hkv * head_bytes */
+  int64_t cache_bytes;  /* num_pages * page_bytes */
+  int64_t v_codes, k_scales, v_scales;  /* offsets inside a head's block; the K codes are at 0 */
+} ra_cache_sizes;
+
+int rotate_attn_cache_layout(const ra_cache_params* p, ra_cache_sizes* out);
+
+/* Tables of a step, from lengths.  R requests hold seq_lens[r] cached tokens
+ * and bring new_lens[r] new ones; block_table[r][j] is the page of tokens
+ * j * page_size ..; free_pages is a stack of free page numbers, free_count[0]
+ * of them (the top at free_count - 1).  Requests with release[r] != 0 (release
+ * may be NULL) first give their pages back, in order, and begin again with
+ * length 0.  Then every request takes the pages it lacks from the top, in order of
+ * request and block, and
+ *   seq_out[r] = cached tokens after the step, count_out[0] = free pages left,
+ *   q_start[0 .. R] = exclusive sums of new_lens,
+ *   positions[t], slots[t] of every packed token (slot = page * page_size +
+ *   place in the page), -1 from q_start[R] up to T.
+ * seq_out may be seq_lens and count_out may be free_count (updated in place).
+ * status[0] is 0, or tells why the step was refused as a whole -- bit 0: a
+ * length that is negative or past max_blocks * page_size, bit 1: more than T
+ * new tokens, bit 2: too few free pages, bit 3: free_count impossible.  Then
+ * nothing has changed, q_start is all 0 (cache_attn does nothing) and the
+ * slots are -1 (cache_append writes nothing).  status[1] = pages the step
+ * takes, status[2] = new tokens, status[3] = the longest request after it
+ * (over the lengths that are valid).
+ * At most 65536 requests, 2^24 tokens. */
+int rotate_attn_cache_plan(const ra_cache_params* p, int32_t R, int32_t T, const int32_t* seq_lens,
+                           const int32_t* new_lens, const int32_t* release, int32_t* block_table, int32_t* free_pages,
+                           const int32_t* free_count, int32_t* seq_out, int32_t* count_out, int32_t* q_start,
+                           int32_t* positions, int32_t* slots, int32_t* status, void* stream);
+
+/* Writes T tokens into their slots: RoPE of K (where rope is given), rotation,
+ * codes.  k and v are [T][Hkv][D] with token and head strides in elements
+ * (multiples of 8; channels adjacent), 16-byte aligned.  rope is
+ * [rope_rows][D/2][2] binary32 cosines and sines by position, turning the
+ * channel pair (2i, 2i+1); any RoPE that turns adjacent pairs, 3D RoPE of a
+ * token grid too, is such a table.  Tokens whose slot (or position, where rope
+ * is given) is out of range are left out.  Slots of one call must differ: the
+ * content of a slot given twice is unspecified. */
+int rotate_attn_cache_append(const ra_cache_params* p, int32_t T, const void* k, int64_t k_token_stride,
+                             int64_t k_head_stride, const void* v, int64_t v_token_stride, int64_t v_head_stride,
+                             const int32_t* slots, const int32_t* positions, const float* rope, int32_t rope_rows,
+                             void* cache, void* stream);
+
+/* The values that T cached tokens stand for, in the basis they were given in
+ * (K after RoPE), into contiguous [T][Hkv][D] tensors of out_dtype.  Slots out
+ * of range give zeros; the same slot may be read several times. */
+int rotate_attn_cache_read(const ra_cache_params* p, int32_t T, const void* cache, const int32_t* slots, void* k,
+                           void* v, void* stream);
+
+/* Attention of packed queries to the cache.  Request r's queries are the last
+ * ones of its seq_lens[r] cached tokens (their own keys appended before the
+ * call): query i has position seq_lens[r] - queries + i, which also picks its
+ * row of rope (NULL: q comes with its positions applied).  q is [T][Hq][D],
+ * strided like k above; query head n reads KV head n / (Hq / Hkv).  o is
+ * contiguous [T][Hq][D]; lse (may be NULL) is [T][Hq] binary32, the natural
+ * logarithm of the softmax's denominator.  A query that sees no key gives 0
+ * and lse -infinity.  Rows outside q_start[0] .. q_start[R] are left as they
+ * were.  max_q bounds the queries of a request (ones past it are not
+ * computed); R, T and max_q fix the grid, so a captured graph may hold them
+ * larger than a replay needs.
+ * Workspace: cache_workspace_size bytes, 256-byte aligned; its contents do not
+ * matter before or after. */
+int rotate_attn_cache_workspace_size(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, size_t* bytes);
+int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, const void* q,
+                           int64_t q_token_stride, int64_t q_head_stride, const void* cache,
+                           const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
+                           const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
 /* Status code -> static text; and the thread-local message of the last failure
  * on the calling thread (library utilities, no paper passage). */
 const char* rotate_attn_error_string(int status);

@@ -17,6 +17,7 @@
 #include <vector>
 
 #include "../../include/rotate_attn.h"
+#include "ra_cache.h"
 #include "ra_internal.h"
 
 namespace {
@@ -652,6 +653,19 @@ int noalloc_tables(const ra_params* p, NoAllocState* ns, float* dev, hipStream_t
 }
 
 }  // namespace
+
+namespace ra {
+
+// The error message of the other translation units.
+int set_error(int code, const char* msg) noexcept {
+  try {
+    g_err = msg;
+  } catch (...) {   // no memory for the text: the status code still tells
+  }
+  return code;
+}
+
+}  // namespace ra
 
 // Input tensors and code buffers are read and written in 16-byte pieces.
 bool al16(const void* ptr) { return ptr == nullptr || reinterpret_cast<uintptr_t>(ptr) % 16 == 0; }

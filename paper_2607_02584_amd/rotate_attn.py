@@ -49,6 +49,19 @@ class Layout(ctypes.Structure):
                 ("v_scale_count", ctypes.c_int64), ("mu_count", ctypes.c_int64), ("k_bias_count", ctypes.c_int64)]
 
 
+class CacheParams(ctypes.Structure):
+    _fields_ = [("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_blocks", ctypes.c_int32),
+                ("rotation", ctypes.c_int32), ("v_rotation", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sm_scale", ctypes.c_float), ("in_dtype", ctypes.c_int32),
+                ("out_dtype", ctypes.c_int32)]
+
+
+class CacheSizes(ctypes.Structure):
+    _fields_ = [("head_bytes", ctypes.c_int64), ("page_bytes", ctypes.c_int64), ("cache_bytes", ctypes.c_int64),
+                ("v_codes", ctypes.c_int64), ("k_scales", ctypes.c_int64), ("v_scales", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -65,6 +78,7 @@ def lib():
         L = ctypes.CDLL(LIB_PATH)
         P = ctypes.c_void_p
         PP = ctypes.POINTER(Params)
+        CP, I, S = ctypes.POINTER(CacheParams), ctypes.c_int32, ctypes.c_int64
         sig = {
             "rotate_attn_layout": [PP, ctypes.POINTER(Layout)],
             "rotate_attn_workspace_size": [PP, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)],
@@ -80,6 +94,12 @@ def lib():
             "rotate_attn_fwd_fp16": [PP, P, P, P, P, P, ctypes.c_size_t, P],
             "rotate_attn_fwd": [PP, ctypes.c_int, P, P, P, P, P, ctypes.c_size_t, P],
             "rotate_attn_fwd_int4_noalloc": [PP, P, P, P, P, P],
+            "rotate_attn_cache_layout": [CP, ctypes.POINTER(CacheSizes)],
+            "rotate_attn_cache_workspace_size": [CP, I, I, I, ctypes.POINTER(ctypes.c_size_t)],
+            "rotate_attn_cache_plan": [CP, I, I] + [P] * 13,
+            "rotate_attn_cache_append": [CP, I, P, S, S, P, S, S, P, P, P, I, P, P],
+            "rotate_attn_cache_read": [CP, I, P, P, P, P, P],
+            "rotate_attn_cache_attn": [CP, I, I, I, P, S, S, P, P, P, P, P, I, P, P, P, ctypes.c_size_t, P],
         }
         for name, args in sig.items():
             fn = getattr(L, name)
@@ -307,6 +327,205 @@ def fwd(p, fallback, q, k, v, o, ws, stream=None):
     _check_fwd(p, q, k, v, o, ws, PATH_FP16 if fallback else PATH_INT4)
     _check(lib().rotate_attn_fwd(ctypes.byref(p), int(bool(fallback)), _ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(ws),
                                  _nbytes(ws), _stream(stream)), "rotate_attn_fwd")
+
+
+# ------------------------------------------------------ 4-bit paged KV cache --
+
+def make_cache_params(Hq, Hkv, D=128, *, page_size=64, num_pages, max_blocks, rotation=ROT_HADAMARD,
+                      v_rotation=VROT_NONE, causal=True, window=0, sm_scale=0.0, in_dtype=BF16,
+                      out_dtype=BF16) -> CacheParams:
+    p = CacheParams()
+    p.Hq, p.Hkv, p.D = Hq, Hkv, D
+    p.page_size, p.num_pages, p.max_blocks = page_size, num_pages, max_blocks
+    p.rotation, p.v_rotation = rotation, v_rotation
+    p.causal, p.window = int(causal), window
+    p.sm_scale = float(sm_scale)
+    p.in_dtype, p.out_dtype = in_dtype, out_dtype
+    return p
+
+
+def cache_layout(p: CacheParams) -> dict:
+    out = CacheSizes()
+    _check(lib().rotate_attn_cache_layout(ctypes.byref(p), ctypes.byref(out)), "rotate_attn_cache_layout")
+    return {f: getattr(out, f) for f, _ in CacheSizes._fields_}
+
+
+def cache_workspace_size(p: CacheParams, R: int, T: int, max_q: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().rotate_attn_cache_workspace_size(ctypes.byref(p), R, T, max_q, ctypes.byref(n)),
+           "rotate_attn_cache_workspace_size")
+    return n.value
+
+
+_TORCH_DTYPES = {BF16: "bfloat16", FP16: "float16", FP32: "float32"}
+
+
+def _cache_tensor(t, name, dtype, shape, device, strided=False):
+    """A device tensor of this type and shape; `strided`: channels adjacent, the
+    other strides multiples of 8 elements."""
+    import torch
+    if not isinstance(t, torch.Tensor):
+        raise ValueError(f"{name} must be a tensor")
+    if t.dtype != getattr(torch, dtype):
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if strided:
+        # the stride of an axis of one element is never used, whatever it says
+        if t.numel() and (t.stride(-1) != 1 and t.shape[-1] > 1 or any(
+                t.stride(i) % 8 or t.stride(i) < 0 for i in range(t.dim() - 1) if t.shape[i] > 1)):
+            raise ValueError(f"{name} needs adjacent channels and other strides that are multiples of 8 elements")
+    elif not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the cache call runs on {device}")
+
+
+def _cache_rows(t):
+    """Token and head stride of [T, heads, D] (0 on an axis of one element)."""
+    return [t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1)]
+
+
+def _cache_rope(p, rope, device):
+    """rope [rows, D/2, 2]: every position the block table can hold has a row."""
+    import torch
+    if rope is None:
+        return 0
+    if not isinstance(rope, torch.Tensor) or rope.dim() != 3:
+        raise ValueError("rope must be a tensor of shape [positions, D/2, 2]")
+    _cache_tensor(rope, "rope", "float32", (rope.shape[0], int(p.D) // 2, 2), device)
+    if rope.shape[0] < int(p.max_blocks) * int(p.page_size):
+        raise ValueError(f"rope has {rope.shape[0]} positions, max_blocks * page_size is "
+                         f"{int(p.max_blocks) * int(p.page_size)}")
+    if rope.shape[0] > 0x7fffffff:
+        raise ValueError("rope has more than 2^31 - 1 positions")
+    return rope.shape[0]
+
+
+class _CacheCall:
+    """The device and stream of a call: the tensors' device, that device's
+    current stream unless one is given."""
+
+    def __init__(self, t, stream):
+        import torch
+        self.guard = torch.cuda.device(t.device)
+        self.device, self.stream = t.device, stream
+
+    def __enter__(self):
+        import torch
+        self.guard.__enter__()
+        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device).cuda_stream
+        return ctypes.c_void_p(s)
+
+    def __exit__(self, *exc):
+        return self.guard.__exit__(*exc)
+
+
+def _cache_pages(p, cache):
+    _cache_tensor(cache, "cache", "uint8", (int(p.num_pages), cache_layout(p)["page_bytes"]), None)
+
+
+def cache_plan(p, seq_lens, new_lens, block_table, free_pages, free_count, q_start, positions, slots, status,
+               release=None, seq_out=None, count_out=None, stream=None):
+    """Block tables, offsets, positions and slots of a step from its lengths
+    (all int32; rotate_attn.h has the rules).  seq_lens and free_count are
+    updated in place unless seq_out and count_out are given.  The call only
+    enqueues: status is read by whoever wants to know."""
+    R, T = seq_lens.numel(), slots.numel()
+    dev = getattr(block_table, "device", None)
+    seq_out = seq_lens if seq_out is None else seq_out
+    count_out = free_count if count_out is None else count_out
+    shapes = [(seq_lens, "seq_lens", (R,)), (new_lens, "new_lens", (R,)),
+              (block_table, "block_table", (R, int(p.max_blocks))), (free_pages, "free_pages", (int(p.num_pages),)),
+              (free_count, "free_count", (1,)), (q_start, "q_start", (R + 1,)), (positions, "positions", (T,)),
+              (slots, "slots", (T,)), (status, "status", (4,)), (seq_out, "seq_out", (R,)),
+              (count_out, "count_out", (1,))]
+    if release is not None:
+        shapes.append((release, "release", (R,)))
+    for t, name, shape in shapes:
+        _cache_tensor(t, name, "int32", shape, dev)
+    with _CacheCall(block_table, stream) as s:
+        _check(lib().rotate_attn_cache_plan(ctypes.byref(p), R, T, _ptr(seq_lens), _ptr(new_lens), _ptr(release),
+                                            _ptr(block_table), _ptr(free_pages), _ptr(free_count), _ptr(seq_out),
+                                            _ptr(count_out), _ptr(q_start), _ptr(positions), _ptr(slots),
+                                            _ptr(status), s), "rotate_attn_cache_plan")
+
+
+def cache_append(p, k, v, slots, cache, positions=None, rope=None, stream=None):
+    """Tokens k, v [T, Hkv, D] into their slots of the cache: RoPE by position
+    where rope is given, rotation, 4-bit codes."""
+    _cache_pages(p, cache)
+    T = slots.numel()
+    shape = (T, int(p.Hkv), int(p.D))
+    for t, name in ((k, "k"), (v, "v")):
+        _cache_tensor(t, name, _TORCH_DTYPES[int(p.in_dtype)], shape, cache.device, strided=True)
+    _cache_tensor(slots, "slots", "int32", (T,), cache.device)
+    rows = _cache_rope(p, rope, cache.device)
+    if rope is not None and positions is None:
+        raise ValueError("rope needs positions")
+    if positions is not None:
+        _cache_tensor(positions, "positions", "int32", (T,), cache.device)
+    with _CacheCall(cache, stream) as s:
+        _check(lib().rotate_attn_cache_append(ctypes.byref(p), T, _ptr(k), *_cache_rows(k), _ptr(v), *_cache_rows(v),
+                                              _ptr(slots), _ptr(positions), _ptr(rope), rows, _ptr(cache), s),
+               "rotate_attn_cache_append")
+
+
+def cache_read(p, cache, slots, k, v, stream=None):
+    """The values that cached tokens stand for, into k, v [T, Hkv, D] of out_dtype."""
+    _cache_pages(p, cache)
+    T = slots.numel()
+    for t, name in ((k, "k"), (v, "v")):
+        _cache_tensor(t, name, _TORCH_DTYPES[int(p.out_dtype)], (T, int(p.Hkv), int(p.D)), cache.device)
+    _cache_tensor(slots, "slots", "int32", (T,), cache.device)
+    with _CacheCall(cache, stream) as s:
+        _check(lib().rotate_attn_cache_read(ctypes.byref(p), T, _ptr(cache), _ptr(slots), _ptr(k), _ptr(v), s),
+               "rotate_attn_cache_read")
+
+
+def cache_attn(p, q, cache, block_table, q_start, seq_lens, max_q, o, ws, lse=None, rope=None, stream=None):
+    """Attention of packed queries q [T, Hq, D] to their requests' cached
+    tokens into o [T, Hq, D] (and lse [T, Hq])."""
+    _cache_pages(p, cache)
+    dev, R = cache.device, seq_lens.numel()
+    T = q.shape[0] if q.dim() else 0
+    shape = (T, int(p.Hq), int(p.D))
+    _cache_tensor(q, "q", _TORCH_DTYPES[int(p.in_dtype)], shape, dev, strided=True)
+    _cache_tensor(o, "o", _TORCH_DTYPES[int(p.out_dtype)], shape, dev)
+    _cache_tensor(block_table, "block_table", "int32", (R, int(p.max_blocks)), dev)
+    _cache_tensor(q_start, "q_start", "int32", (R + 1,), dev)
+    _cache_tensor(seq_lens, "seq_lens", "int32", (R,), dev)
+    if lse is not None:
+        _cache_tensor(lse, "lse", "float32", shape[:2], dev)
+    rows = _cache_rope(p, rope, dev)
+    _need(ws, cache_workspace_size(p, R, T, max_q), "workspace")
+    if ws.device != dev:
+        raise ValueError(f"workspace is on {ws.device}, the cache call runs on {dev}")
+    with _CacheCall(cache, stream) as s:
+        _check(lib().rotate_attn_cache_attn(ctypes.byref(p), R, T, max_q, _ptr(q), *_cache_rows(q), _ptr(cache),
+                                            _ptr(block_table), _ptr(q_start), _ptr(seq_lens), _ptr(rope), rows,
+                                            _ptr(o), _ptr(lse), _ptr(ws), _nbytes(ws), s), "rotate_attn_cache_attn")
+
+
+def alloc_cache(p: CacheParams, R: int, device="cuda"):
+    """The state of R requests: pages, block table, lengths and the stack of free
+    pages, all free."""
+    import torch
+    i32 = dict(dtype=torch.int32, device=device)
+    return dict(
+        cache=torch.empty((int(p.num_pages), cache_layout(p)["page_bytes"]), dtype=torch.uint8, device=device),
+        block_table=torch.full((R, int(p.max_blocks)), -1, **i32),
+        seq_lens=torch.zeros(R, **i32),
+        free_pages=torch.arange(int(p.num_pages) - 1, -1, -1, **i32),
+        free_count=torch.full((1,), int(p.num_pages), **i32),
+    )
+
+
+def cache_workspace(p: CacheParams, R: int, T: int, max_q: int, device="cuda"):
+    import torch
+    return torch.empty(max(cache_workspace_size(p, R, T, max_q), 256), dtype=torch.uint8, device=device)
 
 
 # ---------------------------------------------------------------- helpers --
