@@ -251,7 +251,7 @@ __device__ __forceinline__ void split_bf16(float x, __bf16& hi, __bf16& lo) {
 // The rows' Q as the second operand of K Q^T: lane = 16 * part + row, its
 // D / 4 channels from part * D / 4 on, after RoPE and rotation.
 template <int D>
-__device__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane, v8bf (&hi)[D / 32],
+__device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane, v8bf (&hi)[D / 32],
                        v8bf (&lo)[D / 32]) {
   constexpr int N = D / 4;
   const int part = lane >> 4;
@@ -292,7 +292,7 @@ __device__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, i
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       __bf16 x0, x1;
-      split_bf16(y[8 * c + e], x0, x1);
+      split_bf16(y[8 * c + e] * a.c, x0, x1);   // scores come out in base 2
       hi[c][e] = x0;
       lo[c][e] = x1;
     }
@@ -304,14 +304,140 @@ __device__ __forceinline__ uint32_t dword_of(const typename std::conditional<D =
   else return i == 0 ? v.x : v.y;
 }
 
+// The rows' state in a wave: Q, running maximum and sum, O^T.
 template <int D, int NT>
-__global__ __launch_bounds__(256) void k_few(CacheAttnArgs a) {
-  constexpr int M = 16 * NT, E = D / 16, KC = D / 32;
+struct Rows {
+  v8bf qh[NT][D / 32], ql[NT][D / 32];
+  v4f o[NT][D / 16];
+  float m[NT], l[NT];
+  int hi[NT], lo[NT];   // keys that the lane's row sees: [lo, hi)
+};
+
+// One step of 16 KT keys.  `there` bit i: the i-th 16 keys are on a page; whole:
+// every row sees every key.
+template <int D, int NT, int KT>
+__device__ __forceinline__ void few_step(Rows<D, NT>& x, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
+                                          int g) {
+  constexpr int KC = D / 32;
+  v4f s[NT][KT];
+#pragma unroll
+  for (int i = 0; i < KT; ++i) {
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) s[nt][i] = v4f{0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      const v8bf k = codes8(dword_of<D>(t[i].k, c));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, x.qh[nt][c], s[nt][i], 0, 0, 0);
+        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, x.ql[nt][c], s[nt][i], 0, 0, 0);
+      }
+    }
+    const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[nt][i][e] *= ks[e];
+  }
+  v8bf ph[NT][KT / 2], pl[NT][KT / 2];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    unsigned seen = 0xffff;   // bit 4 i + e: this lane's row sees key 16 i + 4 g + e of the step
+    if (!whole) {
+      seen = 0;
+#pragma unroll
+      for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int key = key0 + 16 * i + 4 * g + e;
+          const bool on = ((there >> i) & 1) && key < x.hi[nt] && key >= x.lo[nt];
+          seen |= static_cast<unsigned>(on) << (4 * i + e);
+          s[nt][i][e] = on ? s[nt][i][e] : kNegInf;
+        }
+    }
+    float mx = x.m[nt];
+#pragma unroll
+    for (int i = 0; i < KT; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[nt][i][e]);
+    mx = fmaxf(mx, lane_xor<16>(mx));
+    mx = fmaxf(mx, lane_xor<32>(mx));
+    const float ref = mx == kNegInf ? 0.0f : mx;   // nothing seen yet: any finite reference gives 0
+    if (__any(mx != x.m[nt])) {
+      const float alpha = __builtin_amdgcn_exp2f(x.m[nt] - ref);
+      x.m[nt] = mx;
+      x.l[nt] *= alpha;
+#pragma unroll
+      for (int e = 0; e < D / 16; ++e) x.o[nt][e] *= alpha;
+    }
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const float vs[4] = {t[i].vs.x, t[i].vs.y, t[i].vs.z, t[i].vs.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float pr = __builtin_amdgcn_exp2f(s[nt][i][e] - ref);
+        x.l[nt] += pr;
+        float w = pr * vs[e];
+        // a scale that is not finite must not reach rows that do not see its token
+        if (!whole) w = (seen >> (4 * i + e)) & 1 ? w : 0.0f;
+        __bf16 x0, x1;
+        split_bf16(w, x0, x1);
+        ph[nt][i / 2][4 * (i % 2) + e] = x0;
+        pl[nt][i / 2][4 * (i % 2) + e] = x1;
+      }
+    }
+  }
+  // V: eight keys of one channel, channel e of the lane's chunk
+#pragma unroll
+  for (int u = 0; u < KT / 2; ++u) {
+    uint32_t ev[D / 32], od[D / 32];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      if constexpr (D == 128) {
+        const uint4 v = t[2 * u + y].v;
+        ev[2 * y] = even_of(v.x, v.y);
+        od[2 * y] = odd_of(v.x, v.y);
+        ev[2 * y + 1] = even_of(v.z, v.w);
+        od[2 * y + 1] = odd_of(v.z, v.w);
+      } else {
+        const uint2 v = t[2 * u + y].v;
+        const uint32_t t02 = (v.x & 0xffffu) | (v.y << 16), t13 = (v.x >> 16) | (v.y & 0xffff0000u);
+        ev[y] = even_of(t02, t13);
+        od[y] = odd_of(t02, t13);
+      }
+    }
+    auto pv = [&](auto bb, const uint32_t (&n)[D / 32], int e) {
+      constexpr int B = decltype(bb)::value;
+      v8bf v;
+      if constexpr (D == 128) v = join(codes2<B>(n[0]), codes2<B>(n[1]), codes2<B>(n[2]), codes2<B>(n[3]));
+      else v = join(codes2<B>(n[0]), codes2<B + 2>(n[0]), codes2<B>(n[1]), codes2<B + 2>(n[1]));
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[nt][u], x.o[nt][e], 0, 0, 0);
+        x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
+      }
+    };
+    pv(std::integral_constant<int, 0>{}, ev, 0);
+    pv(std::integral_constant<int, 0>{}, od, 1);
+    pv(std::integral_constant<int, 1>{}, ev, 2);
+    pv(std::integral_constant<int, 1>{}, od, 3);
+    if constexpr (D == 128) {
+      pv(std::integral_constant<int, 2>{}, ev, 4);
+      pv(std::integral_constant<int, 2>{}, od, 5);
+      pv(std::integral_constant<int, 3>{}, ev, 6);
+      pv(std::integral_constant<int, 3>{}, od, 7);
+    }
+  }
+}
+
+template <int D, int NT, int KT>
+__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
+  constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
   __shared__ __align__(16) float so[4][16][kStride];
   __shared__ float sm[4][M], sl[4][M];
   __shared__ SchedShared sched;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, g = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
   const int h = blockIdx.y;
   Piece p;
   if (!find_piece<M>(a, sched, blockIdx.x, false, &p)) return;
@@ -330,164 +456,80 @@ __global__ __launch_bounds__(256) void k_few(CacheAttnArgs a) {
   const int bl = lo / kBlock, bh = hi > lo ? (hi + kBlock - 1) / kBlock : bl;
   const int per = (bh - bl + p.parts - 1) / p.parts;
   const int b0 = bl + p.part * per, b1 = b0 + per < bh ? b0 + per : bh;
-  const int wper = (b1 - b0 + 3) / 4;
-  const int w0 = b0 + w * wper, w1 = w0 + wper < b1 ? w0 + wper : b1;               // this wave's blocks
+  const int wper = (b1 - b0) > 0 ? ((b1 - b0) * S + 3) / 4 : 0;
+  const int w0 = b0 * S + w * wper, w1 = w0 + wper < b1 * S ? w0 + wper : b1 * S;   // this wave's steps
 
-  v8bf qh[NT][KC], ql[NT][KC];
-  int row_hi[NT], row_lo[NT];
-  float m[NT], l[NT];
-  v4f o[NT][E];
+  // Page numbers of 64 tiles of 16 keys at a time, one per lane, and of the 64 after them.
+  const int page_shift = a.g.page_log - 4;
+  const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
+  const int last16 = (p.q.n + 15) / 16;   // tiles that hold cached tokens
+  auto ids_from = [&](int t16) {
+    const int t = t16 + lane;
+    const int id = t < last16 ? row_table[t >> page_shift] : -1;
+    // an entry that is no page leaves its keys out
+    return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages) ? id : -1;
+  };
+  int ids = -1, ids_next = -1;
+  if (w0 < w1) {
+    ids = ids_from(w0 * KT);
+    if (w0 + 64 / KT < w1) ids_next = ids_from(w0 * KT + 64);
+  }
+  auto load = [&](int b, Tile16<D> (&t)[KT]) {   // steps in order; returns the bits of pages that are there
+    const int at = (b - w0) * KT;
+    unsigned there = 0;
+#pragma unroll
+    for (int i = 0; i < KT; ++i) {
+      const int id = __builtin_amdgcn_readlane(ids, (at + i) & 63);
+      there |= static_cast<unsigned>(id >= 0) << i;
+      load_tile<D>(a, t[i], id >= 0 ? id : 0, h, (b * KT + i) * 16, lane);
+    }
+    if (((at + KT) & 63) == 0) {   // the next step begins the next 64
+      ids = ids_next;
+      if (b + 1 + 64 / KT < w1) ids_next = ids_from((b + 1) * KT + 64);
+    }
+    return there;
+  };
+
+  Tile16<D> ta[KT], tb[KT];
+  unsigned ha = 0, hb = 0;
+  if (w0 < w1) ha = load(w0, ta);
+
+  Rows<D, NT> x;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
-    load_q<D>(a, p, h, row, lane, qh[nt], ql[nt]);
+    load_q<D>(a, p, h, row, lane, x.qh[nt], x.ql[nt]);
     const int pos = first + row / a.G;
-    row_hi[nt] = a.causal ? pos + 1 : p.q.n;
-    if (row_hi[nt] > p.q.n) row_hi[nt] = p.q.n;
-    row_lo[nt] = a.window ? pos - a.window + 1 : 0;
-    m[nt] = kNegInf;
-    l[nt] = 0.0f;
+    x.hi[nt] = a.causal ? pos + 1 : p.q.n;
+    if (x.hi[nt] > p.q.n) x.hi[nt] = p.q.n;
+    x.lo[nt] = a.window ? pos - a.window + 1 : 0;
+    x.m[nt] = kNegInf;
+    x.l[nt] = 0.0f;
 #pragma unroll
-    for (int e = 0; e < E; ++e) o[nt][e] = v4f{0, 0, 0, 0};
+    for (int e = 0; e < E; ++e) x.o[nt][e] = v4f{0, 0, 0, 0};
   }
-
-  const int per_page = a.g.page / 16;
-  const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
-  const int last16 = (p.q.n + 15) / 16;   // 16-key tiles that hold cached tokens
-
-  for (int b = w0; b < w1; ++b) {
-    Tile16<D> t[4];
-    bool there[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t16 = b * 4 + i;
-      int id = -1;
-      if (t16 < last16) id = row_table[t16 / per_page];
-      id = __builtin_amdgcn_readfirstlane(id);
-      // an entry that is no page leaves its keys out
-      there[i] = static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages);
-      load_tile<D>(a, t[i], there[i] ? id : 0, h, t16 * 16, lane);
-    }
-    const int key0 = b * kBlock;
-    const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi && key0 + kBlock <= p.q.n && there[0] && there[1] &&
-                       there[2] && there[3];
-    v8bf kc[4][KC];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int c = 0; c < KC; ++c) kc[i][c] = codes8(dword_of<D>(t[i].k, c));
-    v8bf ph[NT][2], pl[NT][2];
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      v4f s[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        s[i] = v4f{0, 0, 0, 0};
-#pragma unroll
-        for (int c = 0; c < KC; ++c) {
-          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[i][c], qh[nt][c], s[i], 0, 0, 0);
-          s[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kc[i][c], ql[nt][c], s[i], 0, 0, 0);
-        }
-        const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[i][e] *= ks[e] * a.c;
-      }
-      unsigned seen = 0xffff;   // bit 4 i + e: this lane's row sees key 16 i + 4 g + e of the block
-      if (!whole) {
-        seen = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int key = key0 + 16 * i + 4 * g + e;
-            const bool on = there[i] && key < row_hi[nt] && key >= row_lo[nt];
-            seen |= static_cast<unsigned>(on) << (4 * i + e);
-            s[i][e] = on ? s[i][e] : kNegInf;
-          }
-      }
-      float mx = m[nt];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[i][e]);
-      mx = fmaxf(mx, lane_xor<16>(mx));
-      mx = fmaxf(mx, lane_xor<32>(mx));
-      const float ref = mx == kNegInf ? 0.0f : mx;   // nothing seen yet: any finite reference gives 0
-      const float alpha = exp2f(m[nt] - ref);
-      m[nt] = mx;
-      l[nt] *= alpha;
-#pragma unroll
-      for (int e = 0; e < E; ++e) o[nt][e] *= alpha;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float vs[4] = {t[i].vs.x, t[i].vs.y, t[i].vs.z, t[i].vs.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float pr = exp2f(s[i][e] - ref);
-          l[nt] += pr;
-          // a scale that is not finite must not reach rows that do not see its token
-          const float x = (seen >> (4 * i + e)) & 1 ? pr * vs[e] : 0.0f;
-          __bf16 x0, x1;
-          split_bf16(x, x0, x1);
-          ph[nt][i / 2][4 * (i % 2) + e] = x0;
-          pl[nt][i / 2][4 * (i % 2) + e] = x1;
-        }
-      }
-    }
-    // V: eight keys of one channel, channel e of the lane's chunk
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      uint32_t ev[4], od[4];
-      if constexpr (D == 128) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint4 v = t[2 * u + x].v;
-          ev[2 * x] = even_of(v.x, v.y);
-          od[2 * x] = odd_of(v.x, v.y);
-          ev[2 * x + 1] = even_of(v.z, v.w);
-          od[2 * x + 1] = odd_of(v.z, v.w);
-        }
-      } else {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          const uint2 v = t[2 * u + x].v;
-          const uint32_t t02 = (v.x & 0xffffu) | (v.y << 16), t13 = (v.x >> 16) | (v.y & 0xffff0000u);
-          ev[x] = even_of(t02, t13);
-          od[x] = odd_of(t02, t13);
-        }
-      }
-      auto pv = [&](auto bb, const uint32_t (&n)[4], int e) {
-        constexpr int B = decltype(bb)::value;
-        v8bf x;
-        if constexpr (D == 128) x = join(codes2<B>(n[0]), codes2<B>(n[1]), codes2<B>(n[2]), codes2<B>(n[3]));
-        else x = join(codes2<B>(n[0]), codes2<B + 2>(n[0]), codes2<B>(n[1]), codes2<B + 2>(n[1]));
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, ph[nt][u], o[nt][e], 0, 0, 0);
-          o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, pl[nt][u], o[nt][e], 0, 0, 0);
-        }
-      };
-      pv(std::integral_constant<int, 0>{}, ev, 0);
-      pv(std::integral_constant<int, 0>{}, od, 1);
-      pv(std::integral_constant<int, 1>{}, ev, 2);
-      pv(std::integral_constant<int, 1>{}, od, 3);
-      if constexpr (D == 128) {
-        pv(std::integral_constant<int, 2>{}, ev, 4);
-        pv(std::integral_constant<int, 2>{}, od, 5);
-        pv(std::integral_constant<int, 3>{}, ev, 6);
-        pv(std::integral_constant<int, 3>{}, od, 7);
-      }
-    }
+  auto whole = [&](int b, unsigned there) {
+    return b * kStep >= all_lo && b * kStep + kStep <= all_hi && b * kStep + kStep <= p.q.n && there == (1u << KT) - 1;
+  };
+  // the next step's loads are in flight while a step is computed
+  for (int b = w0; b < w1; b += 2) {
+    if (b + 1 < w1) hb = load(b + 1, tb);
+    __builtin_amdgcn_sched_barrier(0);
+    few_step<D, NT, KT>(x, ta, ha, whole(b, ha), b * kStep, g);
+    if (b + 1 >= w1) break;
+    if (b + 2 < w1) ha = load(b + 2, ta);
+    __builtin_amdgcn_sched_barrier(0);
+    few_step<D, NT, KT>(x, tb, hb, whole(b + 1, hb), (b + 1) * kStep, g);
   }
 
   // join the four waves
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
-    l[nt] += lane_xor<16>(l[nt]);
-    l[nt] += lane_xor<32>(l[nt]);
+    x.l[nt] += lane_xor<16>(x.l[nt]);
+    x.l[nt] += lane_xor<32>(x.l[nt]);
     if (lane < 16) {
-      sm[w][nt * 16 + lane] = m[nt];
-      sl[w][nt * 16 + lane] = l[nt];
+      sm[w][nt * 16 + lane] = x.m[nt];
+      sl[w][nt * 16 + lane] = x.l[nt];
     }
   }
 #pragma unroll
@@ -498,7 +540,7 @@ __global__ __launch_bounds__(256) void k_few(CacheAttnArgs a) {
       float* dst = &so[w][lane & 15][(g * 4 + r) * E];
 #pragma unroll
       for (int e = 0; e < E; e += 4)
-        *reinterpret_cast<float4*>(dst + e) = make_float4(o[nt][e][r], o[nt][e + 1][r], o[nt][e + 2][r], o[nt][e + 3][r]);
+        *reinterpret_cast<float4*>(dst + e) = make_float4(x.o[nt][e][r], x.o[nt][e + 1][r], x.o[nt][e + 2][r], x.o[nt][e + 3][r]);
     }
     __syncthreads();
     for (int rr = w; rr < 16; rr += 4) {
@@ -513,7 +555,7 @@ __global__ __launch_bounds__(256) void k_few(CacheAttnArgs a) {
         const float f = rescale(sm[i][row], mm);
         ll += f * sl[i][row];
 #pragma unroll
-        for (int x = 0; x < D / 64; ++x) y[x] += f * so[i][rr][lane * (D / 64) + x];
+        for (int z = 0; z < D / 64; ++z) y[z] += f * so[i][rr][lane * (D / 64) + z];
       }
       if (p.parts == 1) {
         const int i = (p.tile * M + row) / a.G;
@@ -521,53 +563,93 @@ __global__ __launch_bounds__(256) void k_few(CacheAttnArgs a) {
       } else {
         const int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + row;
 #pragma unroll
-        for (int x = 0; x < D / 64; ++x) a.part_o[at * D + lane * (D / 64) + x] = y[x];
+        for (int z = 0; z < D / 64; ++z) a.part_o[at * D + lane * (D / 64) + z] = y[z];
         if (lane == 0) a.part_ml[at] = make_float2(mm, ll);
       }
     }
   }
 }
 
-// Joins the parts of split tiles, a wave per row.
+// Joins the parts of split tiles, a workgroup per row: the parts' weights
+// first, then the sum of their outputs, eight at a time (D / 4 threads each).
+constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
+
 template <int D, int M>
 __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a) {
+  constexpr int W = D / 4, NG = 256 / W;
   __shared__ SchedShared sched;
+  __shared__ float f[kMostParts];
+  __shared__ float red[8];
+  __shared__ __align__(16) float4 sum[NG][W];
   Piece p;
   if (!find_piece<M>(a, sched, blockIdx.x, true, &p)) return;
-  const int lane = threadIdx.x & 63, h = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y, row = blockIdx.z;
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
-  for (int row = threadIdx.x >> 6; row < rows; row += 4) {
-    float mm = kNegInf;
-    for (int i = 0; i < p.parts; ++i)
-      mm = fmaxf(mm, a.part_ml[(static_cast<int64_t>(p.slot + i) * a.g.Hkv + h) * M + row].x);
-    float l = 0.0f, y[D / 64] = {};
-    for (int i = 0; i < p.parts; ++i) {
-      const int64_t at = (static_cast<int64_t>(p.slot + i) * a.g.Hkv + h) * M + row;
-      const float2 ml = a.part_ml[at];
-      const float f = rescale(ml.x, mm);
-      l += f * ml.y;
-#pragma unroll
-      for (int x = 0; x < D / 64; ++x) y[x] += f * a.part_o[at * D + lane * (D / 64) + x];
-    }
-    const int i = (p.tile * M + row) / a.G;
-    finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, y, mm, l, lane);
+  if (row >= rows) return;
+  const int64_t first = (static_cast<int64_t>(p.slot) * a.g.Hkv + h) * M + row;   // of part 0
+  const int64_t step = static_cast<int64_t>(a.g.Hkv) * M;
+  float mm = kNegInf;
+  for (int i = tid; i < p.parts; i += 256) {
+    const float m = a.part_ml[first + i * step].x;
+    f[i] = m;
+    mm = fmaxf(mm, m);
   }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
+  if (lane == 0) red[w] = mm;
+  __syncthreads();
+  mm = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+  float l = 0.0f;
+  for (int i = tid; i < p.parts; i += 256) {
+    f[i] = rescale(f[i], mm);
+    l += f[i] * a.part_ml[first + i * step].y;
+  }
+#pragma unroll
+  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+  if (lane == 0) red[4 + w] = l;
+  __syncthreads();
+  l = red[4] + red[5] + red[6] + red[7];
+  const int g = tid / W, c = tid % W;
+  float4 y = make_float4(0, 0, 0, 0);
+#pragma unroll 4
+  for (int i = g; i < p.parts; i += NG) {
+    const float4 o = *reinterpret_cast<const float4*>(a.part_o + (first + i * step) * D + c * 4);
+    const float x = f[i];
+    y.x += x * o.x, y.y += x * o.y, y.z += x * o.z, y.w += x * o.w;
+  }
+  sum[g][c] = y;
+  __syncthreads();
+  if (w) return;
+  float out[D / 64] = {};
+  const float* s = reinterpret_cast<const float*>(&sum[0][0]);
+#pragma unroll
+  for (int i = 0; i < NG; ++i)
+#pragma unroll
+    for (int x = 0; x < D / 64; ++x) out[x] += s[i * D + lane * (D / 64) + x];
+  const int i = (p.tile * M + row) / a.G;
+  finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, out, mm, l, lane);
 }
 
 constexpr int kPieces = 1024;   // pieces of work over all KV heads aimed at
 
-template <int D>
-hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
-  constexpr int M = 32;
+template <int D, int NT>
+hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
+  constexpr int M = 16 * NT;
   const int64_t per = (static_cast<int64_t>(a.max_q) * a.G + M - 1) / M;
   int64_t tiles = a.R + static_cast<int64_t>(a.T) * a.G / M;
   if (tiles > a.R * per) tiles = a.R * per;
-  k_few<D, 2><<<dim3(static_cast<unsigned>(tiles + a.target), a.g.Hkv), dim3(256), 0, s>>>(a);
+  k_few<D, NT, 2><<<dim3(static_cast<unsigned>(tiles + a.target), a.g.Hkv), dim3(256), 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int64_t merges = tiles < a.target ? tiles : a.target;
-  k_merge<D, M><<<dim3(static_cast<unsigned>(merges), a.g.Hkv), dim3(256), 0, s>>>(a);
+  const int64_t rows = static_cast<int64_t>(a.max_q) * a.G;
+  k_merge<D, M><<<dim3(static_cast<unsigned>(merges), a.g.Hkv, static_cast<unsigned>(rows < M ? rows : M)), dim3(256), 0, s>>>(a);
   return hipGetLastError();
+}
+
+template <int D>
+hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
+  return static_cast<int64_t>(a.max_q) * a.G <= 16 ? few<D, 1>(a, s) : few<D, 2>(a, s);
 }
 
 }  // namespace

@@ -357,74 +357,85 @@ def cache_workspace_size(p: CacheParams, R: int, T: int, max_q: int) -> int:
     return n.value
 
 
-_TORCH_DTYPES = {BF16: "bfloat16", FP16: "float16", FP32: "float32"}
+# The cache calls are made once per layer and token: what is checked stays one
+# comparison per tensor while all is well (a call with its launch takes 6 to 11
+# us of host time), the reasons are worked out on the way to the error.
+
+_dtypes = None
 
 
-def _cache_tensor(t, name, dtype, shape, device, strided=False):
-    """A device tensor of this type and shape; `strided`: channels adjacent, the
-    other strides multiples of 8 elements."""
+def _cache_dtypes():
+    global _dtypes
+    if _dtypes is None:
+        import torch
+        _dtypes = {BF16: torch.bfloat16, FP16: torch.float16, FP32: torch.float32, "i32": torch.int32,
+                   "u8": torch.uint8}
+    return _dtypes
+
+
+def _cache_tensor(t, name, dtype, shape, device=None, strided=False):
+    """A device tensor of this type and shape, contiguous; `strided`: channels
+    adjacent, the other strides multiples of 8 elements."""
     import torch
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a tensor")
-    if t.dtype != getattr(torch, dtype):
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
-    if strided:
+    if not t.is_contiguous():
+        if not strided:
+            raise ValueError(f"{name} must be contiguous")
         # the stride of an axis of one element is never used, whatever it says
-        if t.numel() and (t.stride(-1) != 1 and t.shape[-1] > 1 or any(
-                t.stride(i) % 8 or t.stride(i) < 0 for i in range(t.dim() - 1) if t.shape[i] > 1)):
+        if t.stride(-1) != 1 or any(t.stride(i) % 8 or t.stride(i) < 0 for i in (0, 1) if shape[i] > 1):
             raise ValueError(f"{name} needs adjacent channels and other strides that are multiples of 8 elements")
-    elif not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a device tensor")
     if device is not None and t.device != device:
         raise ValueError(f"{name} is on {t.device}, the cache call runs on {device}")
+    return t.data_ptr()
 
 
 def _cache_rows(t):
     """Token and head stride of [T, heads, D] (0 on an axis of one element)."""
-    return [t.stride(i) if t.shape[i] > 1 else 0 for i in (0, 1)]
+    n, h, _ = t.shape
+    a, b, _ = t.stride()
+    return a if n > 1 else 0, b if h > 1 else 0
 
 
 def _cache_rope(p, rope, device):
     """rope [rows, D/2, 2]: every position the block table can hold has a row."""
     import torch
     if rope is None:
-        return 0
+        return None, 0
     if not isinstance(rope, torch.Tensor) or rope.dim() != 3:
         raise ValueError("rope must be a tensor of shape [positions, D/2, 2]")
-    _cache_tensor(rope, "rope", "float32", (rope.shape[0], int(p.D) // 2, 2), device)
-    if rope.shape[0] < int(p.max_blocks) * int(p.page_size):
-        raise ValueError(f"rope has {rope.shape[0]} positions, max_blocks * page_size is "
-                         f"{int(p.max_blocks) * int(p.page_size)}")
-    if rope.shape[0] > 0x7fffffff:
+    rows = rope.shape[0]
+    ptr = _cache_tensor(rope, "rope", _cache_dtypes()[FP32], (rows, p.D // 2, 2), device)
+    if rows < p.max_blocks * p.page_size:
+        raise ValueError(f"rope has {rows} positions, max_blocks * page_size is {p.max_blocks * p.page_size}")
+    if rows > 0x7fffffff:
         raise ValueError("rope has more than 2^31 - 1 positions")
-    return rope.shape[0]
+    return ptr, rows
 
 
-class _CacheCall:
-    """The device and stream of a call: the tensors' device, that device's
-    current stream unless one is given."""
-
-    def __init__(self, t, stream):
-        import torch
-        self.guard = torch.cuda.device(t.device)
-        self.device, self.stream = t.device, stream
-
-    def __enter__(self):
-        import torch
-        self.guard.__enter__()
-        s = self.stream if self.stream is not None else torch.cuda.current_stream(self.device).cuda_stream
-        return ctypes.c_void_p(s)
-
-    def __exit__(self, *exc):
-        return self.guard.__exit__(*exc)
+def _cache_call(fn, where, device, stream, *args):
+    """fn(*args, stream) with the tensors' device current, on `stream` or that
+    device's current stream."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        status = fn(*args, stream)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, stream)
+    if status != 0:
+        _check(status, where)
 
 
-def _cache_pages(p, cache):
-    _cache_tensor(cache, "cache", "uint8", (int(p.num_pages), cache_layout(p)["page_bytes"]), None)
+def _cache_pages(p, cache, u8):
+    return _cache_tensor(cache, "cache", u8, (p.num_pages, p.Hkv * p.page_size * (p.D + 8)))
 
 
 def cache_plan(p, seq_lens, new_lens, block_table, free_pages, free_count, q_start, positions, slots, status,
@@ -433,80 +444,67 @@ def cache_plan(p, seq_lens, new_lens, block_table, free_pages, free_count, q_sta
     (all int32; rotate_attn.h has the rules).  seq_lens and free_count are
     updated in place unless seq_out and count_out are given.  The call only
     enqueues: status is read by whoever wants to know."""
+    i32 = _cache_dtypes()["i32"]
     R, T = seq_lens.numel(), slots.numel()
-    dev = getattr(block_table, "device", None)
-    seq_out = seq_lens if seq_out is None else seq_out
-    count_out = free_count if count_out is None else count_out
-    shapes = [(seq_lens, "seq_lens", (R,)), (new_lens, "new_lens", (R,)),
-              (block_table, "block_table", (R, int(p.max_blocks))), (free_pages, "free_pages", (int(p.num_pages),)),
-              (free_count, "free_count", (1,)), (q_start, "q_start", (R + 1,)), (positions, "positions", (T,)),
-              (slots, "slots", (T,)), (status, "status", (4,)), (seq_out, "seq_out", (R,)),
-              (count_out, "count_out", (1,))]
-    if release is not None:
-        shapes.append((release, "release", (R,)))
-    for t, name, shape in shapes:
-        _cache_tensor(t, name, "int32", shape, dev)
-    with _CacheCall(block_table, stream) as s:
-        _check(lib().rotate_attn_cache_plan(ctypes.byref(p), R, T, _ptr(seq_lens), _ptr(new_lens), _ptr(release),
-                                            _ptr(block_table), _ptr(free_pages), _ptr(free_count), _ptr(seq_out),
-                                            _ptr(count_out), _ptr(q_start), _ptr(positions), _ptr(slots),
-                                            _ptr(status), s), "rotate_attn_cache_plan")
+    dev, per_request, per_token = seq_lens.device, (R,), (T,)
+    lens = _cache_tensor(seq_lens, "seq_lens", i32, per_request)
+    table = _cache_tensor(block_table, "block_table", i32, (R, p.max_blocks), dev)
+    count = _cache_tensor(free_count, "free_count", i32, (1,), dev)
+    _cache_call(
+        lib().rotate_attn_cache_plan, "rotate_attn_cache_plan", dev, stream, ctypes.byref(p), R, T, lens,
+        _cache_tensor(new_lens, "new_lens", i32, per_request, dev),
+        None if release is None else _cache_tensor(release, "release", i32, per_request, dev), table,
+        _cache_tensor(free_pages, "free_pages", i32, (p.num_pages,), dev), count,
+        lens if seq_out is None else _cache_tensor(seq_out, "seq_out", i32, per_request, dev),
+        count if count_out is None else _cache_tensor(count_out, "count_out", i32, (1,), dev),
+        _cache_tensor(q_start, "q_start", i32, (R + 1,), dev), _cache_tensor(positions, "positions", i32, per_token, dev),
+        _cache_tensor(slots, "slots", i32, per_token, dev), _cache_tensor(status, "status", i32, (4,), dev))
 
 
 def cache_append(p, k, v, slots, cache, positions=None, rope=None, stream=None):
     """Tokens k, v [T, Hkv, D] into their slots of the cache: RoPE by position
     where rope is given, rotation, 4-bit codes."""
-    _cache_pages(p, cache)
-    T = slots.numel()
-    shape = (T, int(p.Hkv), int(p.D))
-    for t, name in ((k, "k"), (v, "v")):
-        _cache_tensor(t, name, _TORCH_DTYPES[int(p.in_dtype)], shape, cache.device, strided=True)
-    _cache_tensor(slots, "slots", "int32", (T,), cache.device)
-    rows = _cache_rope(p, rope, cache.device)
+    dt = _cache_dtypes()
+    pages, dev, T = _cache_pages(p, cache, dt["u8"]), cache.device, slots.numel()
+    shape, kind = (T, p.Hkv, p.D), dt[p.in_dtype]
     if rope is not None and positions is None:
         raise ValueError("rope needs positions")
-    if positions is not None:
-        _cache_tensor(positions, "positions", "int32", (T,), cache.device)
-    with _CacheCall(cache, stream) as s:
-        _check(lib().rotate_attn_cache_append(ctypes.byref(p), T, _ptr(k), *_cache_rows(k), _ptr(v), *_cache_rows(v),
-                                              _ptr(slots), _ptr(positions), _ptr(rope), rows, _ptr(cache), s),
-               "rotate_attn_cache_append")
+    table, rows = _cache_rope(p, rope, dev)
+    _cache_call(
+        lib().rotate_attn_cache_append, "rotate_attn_cache_append", dev, stream, ctypes.byref(p), T,
+        _cache_tensor(k, "k", kind, shape, dev, True), *_cache_rows(k),
+        _cache_tensor(v, "v", kind, shape, dev, True), *_cache_rows(v),
+        _cache_tensor(slots, "slots", dt["i32"], (T,), dev),
+        None if positions is None else _cache_tensor(positions, "positions", dt["i32"], (T,), dev), table, rows, pages)
 
 
 def cache_read(p, cache, slots, k, v, stream=None):
     """The values that cached tokens stand for, into k, v [T, Hkv, D] of out_dtype."""
-    _cache_pages(p, cache)
-    T = slots.numel()
-    for t, name in ((k, "k"), (v, "v")):
-        _cache_tensor(t, name, _TORCH_DTYPES[int(p.out_dtype)], (T, int(p.Hkv), int(p.D)), cache.device)
-    _cache_tensor(slots, "slots", "int32", (T,), cache.device)
-    with _CacheCall(cache, stream) as s:
-        _check(lib().rotate_attn_cache_read(ctypes.byref(p), T, _ptr(cache), _ptr(slots), _ptr(k), _ptr(v), s),
-               "rotate_attn_cache_read")
+    dt = _cache_dtypes()
+    pages, dev, T = _cache_pages(p, cache, dt["u8"]), cache.device, slots.numel()
+    shape, kind = (T, p.Hkv, p.D), dt[p.out_dtype]
+    _cache_call(
+        lib().rotate_attn_cache_read, "rotate_attn_cache_read", dev, stream, ctypes.byref(p), T, pages,
+        _cache_tensor(slots, "slots", dt["i32"], (T,), dev), _cache_tensor(k, "k", kind, shape, dev),
+        _cache_tensor(v, "v", kind, shape, dev))
 
 
 def cache_attn(p, q, cache, block_table, q_start, seq_lens, max_q, o, ws, lse=None, rope=None, stream=None):
     """Attention of packed queries q [T, Hq, D] to their requests' cached
     tokens into o [T, Hq, D] (and lse [T, Hq])."""
-    _cache_pages(p, cache)
-    dev, R = cache.device, seq_lens.numel()
-    T = q.shape[0] if q.dim() else 0
-    shape = (T, int(p.Hq), int(p.D))
-    _cache_tensor(q, "q", _TORCH_DTYPES[int(p.in_dtype)], shape, dev, strided=True)
-    _cache_tensor(o, "o", _TORCH_DTYPES[int(p.out_dtype)], shape, dev)
-    _cache_tensor(block_table, "block_table", "int32", (R, int(p.max_blocks)), dev)
-    _cache_tensor(q_start, "q_start", "int32", (R + 1,), dev)
-    _cache_tensor(seq_lens, "seq_lens", "int32", (R,), dev)
-    if lse is not None:
-        _cache_tensor(lse, "lse", "float32", shape[:2], dev)
-    rows = _cache_rope(p, rope, dev)
-    _need(ws, cache_workspace_size(p, R, T, max_q), "workspace")
-    if ws.device != dev:
-        raise ValueError(f"workspace is on {ws.device}, the cache call runs on {dev}")
-    with _CacheCall(cache, stream) as s:
-        _check(lib().rotate_attn_cache_attn(ctypes.byref(p), R, T, max_q, _ptr(q), *_cache_rows(q), _ptr(cache),
-                                            _ptr(block_table), _ptr(q_start), _ptr(seq_lens), _ptr(rope), rows,
-                                            _ptr(o), _ptr(lse), _ptr(ws), _nbytes(ws), s), "rotate_attn_cache_attn")
+    dt = _cache_dtypes()
+    pages, dev, R, T = _cache_pages(p, cache, dt["u8"]), cache.device, seq_lens.numel(), q.shape[0]
+    shape, i32 = (T, p.Hq, p.D), dt["i32"]
+    table, rows = _cache_rope(p, rope, dev)
+    nws = _nbytes(ws)
+    _cache_call(
+        lib().rotate_attn_cache_attn, "rotate_attn_cache_attn", dev, stream, ctypes.byref(p), R, T, max_q,
+        _cache_tensor(q, "q", dt[p.in_dtype], shape, dev, True), *_cache_rows(q), pages,
+        _cache_tensor(block_table, "block_table", i32, (R, p.max_blocks), dev),
+        _cache_tensor(q_start, "q_start", i32, (R + 1,), dev), _cache_tensor(seq_lens, "seq_lens", i32, (R,), dev),
+        table, rows, _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
+        None if lse is None else _cache_tensor(lse, "lse", dt[FP32], shape[:2], dev),
+        _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
 
 
 def alloc_cache(p: CacheParams, R: int, device="cuda"):

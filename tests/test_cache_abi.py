@@ -142,13 +142,13 @@ def test_binding_checks_tensors(ra):
                       (torch.zeros(3, 2, 256, dtype=torch.bfloat16)[..., ::2], "adjacent"),
                       (torch.zeros(3, 2, 132, dtype=torch.bfloat16)[..., :128], "adjacent")):
         with pytest.raises(ValueError, match=word):
-            ra._cache_tensor(bad, "k", "bfloat16", (3, 2, 128), None, strided=True)
+            ra._cache_tensor(bad, "k", torch.bfloat16, (3, 2, 128), None, strided=True)
     with pytest.raises(ValueError, match="contiguous"):
-        ra._cache_tensor(torch.zeros(4, 4).t(), "x", "float32", (4, 4), None)
+        ra._cache_tensor(torch.arange(8.0).view(2, 4).t(), "x", torch.float32, (4, 2), None)
     # an axis of one element may have any stride
     one = torch.zeros(1, 4, 2, 128, dtype=torch.bfloat16)[:, 0].as_strided((1, 2, 128), (3, 128, 1))
     with pytest.raises(ValueError, match="device tensor"):
-        ra._cache_tensor(one, "k", "bfloat16", (1, 2, 128), None, strided=True)
-    assert ra._cache_rows(one) == [0, 128]
+        ra._cache_tensor(one, "k", torch.bfloat16, (1, 2, 128), None, strided=True)
+    assert ra._cache_rows(one) == (0, 128)
     with pytest.raises(ValueError, match="positions"):
         ra._cache_rope(p, torch.zeros(2, 2), None)
