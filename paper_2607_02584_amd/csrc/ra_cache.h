@@ -84,7 +84,7 @@ struct CacheAttnArgs {
   float c;                          // softmax scale * log2(e), and 1/sqrt(D) where Q is rotated
   int rope_rows, R, T, max_q, Hq, G, max_blocks;
   int causal, window, is_fp16, out_dtype, had, vhad;
-  int target;                       // pieces of work per KV head aimed at
+  int target, target_rows;          // pieces of work per KV head aimed at (set by the launch)
 };
 
 hipError_t launch_cache_plan(const PlanArgs& a, hipStream_t s);
@@ -93,7 +93,6 @@ hipError_t launch_cache_read(const ReadArgs& a, int D, bool hadk, bool hadv, hip
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int D, hipStream_t s);
 // bytes of workspace that launch_cache_attn's part_o and part_ml take
 size_t cache_attn_partial_bytes(int D, int Hkv, int G, int max_q, size_t* ml_offset);
-int cache_attn_target(int Hkv);
 
 // stores a library error message for rotate_attn_last_error() and returns code
 int set_error(int code, const char* msg) noexcept;

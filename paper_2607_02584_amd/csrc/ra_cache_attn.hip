@@ -30,12 +30,20 @@ constexpr float kLn2 = 0.693147180559945309417232121458f;
 // same for every KV head.  Lengths live on the device (a captured graph runs
 // with whatever they are then), so every workgroup cuts alone, in the same
 // way: with W the sum over tiles of their blocks of 64 keys, a part has
-// C = max(least, W / target) blocks, and a request's tiles n = ceil(blocks / C)
-// parts.  There are then at most (tiles + target) pieces, and at most
+// C = max(least, W / target) blocks, and a request's tiles have
+// n = ceil(blocks / C) parts.  There are then at most (tiles + target) pieces, and at most
 // 2 * target of tiles that have several parts, whatever the lengths: the grid
 // and the workspace follow from that.
-constexpr int kBlock = 64;        // keys per step
-constexpr int kLeastBlocks = 4;   // least part: one step for each of four waves
+constexpr int kBlock = 64;        // keys
+
+// The two kernels share a call's requests by their number of rows: up to
+// kFewRows a request is bound by its keys (k_few), above by the matrix cores
+// (k_rows).
+constexpr int kFewRows = 32;
+// blocks of the least part: a step of 32 keys for each of the four waves of
+// k_few, twice; for k_rows enough to pay for a partial output of M rows
+template <int M>
+constexpr int least_blocks() { return M <= kFewRows ? 4 : 16; }
 
 struct Request {
   int q0, ql, n;    // first query row, queries to compute (max_q at most), cached tokens
@@ -56,7 +64,8 @@ __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int r) {
   x.ql = q1 - q0 < a.max_q ? q1 - q0 : a.max_q;
   x.n = n < 0 ? 0 : n > most ? most : n;
   x.first = x.n - (q1 - q0);
-  x.tiles = (x.ql * a.G + M - 1) / M;
+  const int rows = x.ql * a.G;
+  x.tiles = (rows <= kFewRows) == (M <= kFewRows) ? (rows + M - 1) / M : 0;
   int keys = x.n;
   if (a.window) {
     const int first = x.first - a.window + 1;
@@ -74,18 +83,18 @@ struct Piece {
 };
 
 struct SchedShared {
-  long long w[4];
-  int s[4][2];
+  long long w[8];
+  int s[8][2];
   int hit[8];
 };
 
 // Piece number x (or, for the merge, tile number x of those with several
-// parts); false past the end.  All 256 threads call it.
-template <int M>
-__device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool merge, Piece* out) {
+// parts); false past the end.  All threads of the workgroup call it.
+template <int M, int THREADS>
+__device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool merge, int target, Piece* out) {
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   long long W = 0;
-  for (int r = tid; r < a.R; r += 256) {
+  for (int r = tid; r < a.R; r += THREADS) {
     const Request q = request_of<M>(a, r);
     W += static_cast<long long>(q.tiles) * q.blocks;
   }
@@ -94,11 +103,13 @@ __device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool 
   if (lane == 0) sh.w[w] = W;
   if (tid == 0) sh.hit[0] = -1;
   __syncthreads();
-  W = sh.w[0] + sh.w[1] + sh.w[2] + sh.w[3];
-  long long C = (W + a.target - 1) / a.target;
-  if (C < kLeastBlocks) C = kLeastBlocks;
+  W = 0;
+#pragma unroll
+  for (int i = 0; i < THREADS / 64; ++i) W += sh.w[i];
+  long long C = (W + target - 1) / target;
+  if (C < least_blocks<M>()) C = least_blocks<M>();
   int base = 0, slot = 0;
-  for (int r0 = 0; r0 < a.R; r0 += 256) {
+  for (int r0 = 0; r0 < a.R; r0 += THREADS) {
     const int r = r0 + tid;
     Request q = {};
     int n = 0;
@@ -124,7 +135,7 @@ __device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool 
     __syncthreads();
     int t0 = 0, t1 = 0, p0 = 0, p1 = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < THREADS / 64; ++i) {
       if (i < w) {
         p0 += sh.s[i][0];
         p1 += sh.s[i][1];
@@ -438,9 +449,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
   __shared__ float sm[4][M], sl[4][M];
   __shared__ SchedShared sched;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
-  const int h = blockIdx.y;
+  // heads fastest: the heads of a page, neighbours in memory, are read together
+  const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M>(a, sched, blockIdx.x, false, &p)) return;
+  if (!find_piece<M, 256>(a, sched, x0, false, a.target, &p)) return;
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;   // of this tile
   const int first = p.q.first;
@@ -570,19 +582,409 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
   }
 }
 
+// --------------------------------------------------------- many rows per request --
+//
+// Bound by the matrix cores and the softmax beside them.  NW waves of 32 rows
+// share tiles of 64 keys in LDS, as 16-bit values of the codes (exact), scales
+// apart: each wave loads its share of the next tile's codes while the present
+// one is computed, and converts them into the other LDS buffer at its end.
+// S^T = K Q^T and O^T += V^T P^T on the 32x32x16 product: a lane holds one
+// query's scores (key 32 c + 8 (r / 4) + 4 hh + r % 4 in register r of chunk
+// c), which rounded to 16 bits are the second operand of the next product, and
+// the same query's output, so that rescaling it is a factor per lane.
+//
+// Q (after RoPE, rotation and scale, in binary32) is rounded once to the input
+// type, P * (V's scale) once to it: 2^-8 and 2^-11 relative, the type's own
+// half step, as everything the model feeds in.  In binary16 the V scales are
+// taken relative to the power of two of the largest so far (`ref`; O is in
+// units of it), so that P * scale neither overflows nor loses small values.
+//
+// LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
+// bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
+// Channel d of V sits at position (d % E) * 16 + d / E, E = D / 16 (its page
+// order), an octet holds keys 16 s + 4 hh + {0..3, 8..11} of step s.
+
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+
+template <bool F16>
+struct Half16 {
+  typedef v8bf vec;
+  static __device__ __forceinline__ v16f mfma(vec a, vec b, v16f c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  template <int B>
+  static __device__ __forceinline__ uint32_t codes(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, B));
+  }
+};
+template <>
+struct Half16<true> {
+  typedef v8h vec;
+  static __device__ __forceinline__ v16f mfma(vec a, vec b, v16f c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+  template <int B>
+  static __device__ __forceinline__ uint32_t codes(uint32_t w) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, B));
+  }
+};
+
+template <int D, bool F16>
+__device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
+                                         typename Half16<F16>::vec (&out)[D / 16]) {
+  constexpr int N = D / 2;
+  const int hh = lane >> 5;
+  const bool ok = row < p.q.ql * a.G;
+  const int i = ok ? row / a.G : 0, head = h * a.G + (ok ? row - i * a.G : 0);
+  float y[N];
+  const uint16_t* src = a.q + static_cast<int64_t>(p.q.q0 + i) * a.q_ts + head * a.q_hs + hh * N;
+#pragma unroll
+  for (int c = 0; c < N / 8; ++c) {
+    uint4 w = {};
+    if (ok) w = *reinterpret_cast<const uint4*>(src + 8 * c);
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[8 * c + 2 * e] = cache_h2f(static_cast<uint16_t>(u[e] & 0xffff), F16);
+      y[8 * c + 2 * e + 1] = cache_h2f(static_cast<uint16_t>(u[e] >> 16), F16);
+    }
+  }
+  if (a.rope) {
+    int pos = p.q.first + i;
+    pos = pos < 0 ? 0 : pos >= a.rope_rows ? a.rope_rows - 1 : pos;
+    const float2* cs = reinterpret_cast<const float2*>(a.rope + static_cast<int64_t>(pos) * D) + hh * (N / 2);
+#pragma unroll
+    for (int e = 0; e < N / 2; ++e) {
+      const float2 t = cs[e];
+      const float u = y[2 * e], v = y[2 * e + 1];
+      y[2 * e] = u * t.x - v * t.y;
+      y[2 * e + 1] = u * t.y + v * t.x;
+    }
+  }
+  if (a.had) {
+    butterfly_regs(y);
+    butterfly_lanes<32>(y, lane);
+  }
+#pragma unroll
+  for (int c = 0; c < N / 8; ++c) {
+    uint4 w;
+    w.x = pack16(y[8 * c] * a.c, y[8 * c + 1] * a.c, F16);
+    w.y = pack16(y[8 * c + 2] * a.c, y[8 * c + 3] * a.c, F16);
+    w.z = pack16(y[8 * c + 4] * a.c, y[8 * c + 5] * a.c, F16);
+    w.w = pack16(y[8 * c + 6] * a.c, y[8 * c + 7] * a.c, F16);
+    out[c] = __builtin_bit_cast(typename Half16<F16>::vec, w);
+  }
+}
+
+template <int D, int NW, bool F16>
+__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs a) {
+  typedef Half16<F16> H;
+  typedef typename H::vec vec;
+  typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
+  constexpr int M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
+  struct Buf {
+    uint4 k[D / 8][64];
+    uint4 v[8][D];
+    float ks[64], vs[64];
+    unsigned long long there;   // keys that are on a page
+    float ref;
+  };
+  __shared__ __align__(16) Buf buf[2];
+  __shared__ SchedShared sched;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hh = lane >> 5, j = lane & 31;
+  // heads fastest: workgroups go round the 8 XCDs, so a head's keys stay in few L2s
+  const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
+  Piece p;
+  if (!find_piece<M, 64 * NW>(a, sched, x0, false, a.target_rows, &p)) return;
+  if (a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
+
+  const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
+  const int first = p.q.first;
+  const int i0 = p.tile * M / a.G, i1 = (p.tile * M + rows - 1) / a.G;
+  int hi = p.q.n, lo = 0;
+  if (a.causal) hi = first + i1 + 1;
+  if (hi < 0) hi = 0;
+  if (a.window) lo = first + i0 - a.window + 1 > 0 ? first + i0 - a.window + 1 : 0;
+  const int bl = lo / kBlock, bh = hi > lo ? (hi + kBlock - 1) / kBlock : bl;
+  const int per = (bh - bl + p.parts - 1) / p.parts;
+  const int b0 = bl + p.part * per, b1 = b0 + per < bh ? b0 + per : bh;
+  // bounds that every row of this wave sees, and its lane's row
+  const int wrow = p.tile * M + w * 32, row = wrow + j;
+  const int wi1 = wrow + 31 < p.tile * M + rows - 1 ? (wrow + 31) / a.G : i1;
+  const int all_hi = a.causal ? first + wrow / a.G + 1 : p.q.n;
+  const int all_lo = a.window ? first + wi1 - a.window + 1 : 0;
+  // keys that any row of this wave sees; a wave behind the tile's rows sees none
+  const int any_hi = w * 32 >= rows ? 0 : a.causal ? first + wi1 + 1 : p.q.n;
+  const int any_lo = a.window ? first + wrow / a.G - a.window + 1 : 0;
+  const int pos = first + row / a.G;
+  int row_hi = a.causal ? pos + 1 : p.q.n;
+  if (row_hi > p.q.n) row_hi = p.q.n;
+  const int row_lo = a.window ? pos - a.window + 1 : 0;
+
+  const int page = a.g.page, page_log = a.g.page_log;
+  const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
+  const uint8_t* head_base = a.g.cache + static_cast<int64_t>(h) * head_bytes<D>(page);
+  const int kb = page * D / 2;
+  // The page of token t of the request, -1 behind its end or where the entry is none.
+  auto page_of = [&](int t) {
+    const int id = t < p.q.n ? row_table[t >> page_log] : -1;
+    return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages) ? id : -1;
+  };
+  const bool do_k = NW == 4 || w < 4, do_v = NW == 4 || w >= 4, do_s = w == NW - 1;
+  const int mine = (w & 3) * 16;   // this wave's 16 tokens of a tile
+
+  // staged for the next tile: codes, and in the last wave a scale pair per lane
+  Codes sk = {}, sv = {};
+  float ks = 0.0f, vs = 0.0f;
+  bool here = false;
+  int id_c = -1, id_s = -1;   // pages of the tile after the staged one
+  auto ask_ids = [&](int b) {
+    if (b < b1) {
+      id_c = page_of(b * kBlock + mine);
+      if (do_s) id_s = page_of(b * kBlock + lane);
+    }
+  };
+  auto ask = [&](int b) {   // loads of tile b, whose page numbers are in hand; then the next tile's numbers
+    if (b >= b1) return;
+    const int tok = (b * kBlock + mine) & (page - 1);
+    const int id = __builtin_amdgcn_readfirstlane(id_c);
+    const uint8_t* base = head_base + static_cast<int64_t>(id < 0 ? 0 : id) * a.g.page_bytes + tok * (D / 2) + lane * (D / 8);
+    if (do_k) sk = *reinterpret_cast<const Codes*>(base);
+    if (do_v) {
+      // lane = chunk + 16 * (half of the octet) + 32 * hh
+      const int g = ((lane >> 4) & 1) * 2 + hh;   // tokens 4 g ..
+      sv = *reinterpret_cast<const Codes*>(base - lane * (D / 8) + kb + (g * 16 + (lane & 15)) * (D / 8));
+    }
+    if (do_s) {
+      const int t = b * kBlock + lane;
+      here = id_s >= 0 && t < p.q.n;
+      if (here) {
+        const float* sc = reinterpret_cast<const float*>(head_base + static_cast<int64_t>(id_s) * a.g.page_bytes + 2 * kb) +
+                          (t & (page - 1));
+        ks = sc[0];
+        vs = sc[page];
+      } else {
+        ks = vs = 0.0f;
+      }
+    }
+    ask_ids(b + 1);
+  };
+  float ref_s = 0.0f;   // last wave: power of two of the largest V scale so far
+  auto put = [&](Buf& t) {   // the staged tile into LDS
+    if (do_k) {
+      const int part = lane >> 4, key = mine + (lane & 15);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const uint32_t x = dword_of<D>(sk, c);
+        t.k[part * (D / 32) + c][key] = make_uint4(H::template codes<0>(x), H::template codes<1>(x),
+                                                   H::template codes<2>(x), H::template codes<3>(x));
+      }
+    }
+    if (do_v) {
+      const int half = (lane >> 4) & 1, i = lane & 15;
+      uint2* dst = reinterpret_cast<uint2*>(&t.v[(w & 3) * 2 + hh][i]) + half;   // position e * 16 + i
+      if constexpr (D == 128) {
+        const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
+                       o23 = odd_of(sv.z, sv.w);
+        dst[0 * 32] = make_uint2(H::template codes<0>(e01), H::template codes<0>(e23));
+        dst[1 * 32] = make_uint2(H::template codes<0>(o01), H::template codes<0>(o23));
+        dst[2 * 32] = make_uint2(H::template codes<1>(e01), H::template codes<1>(e23));
+        dst[3 * 32] = make_uint2(H::template codes<1>(o01), H::template codes<1>(o23));
+        dst[4 * 32] = make_uint2(H::template codes<2>(e01), H::template codes<2>(e23));
+        dst[5 * 32] = make_uint2(H::template codes<2>(o01), H::template codes<2>(o23));
+        dst[6 * 32] = make_uint2(H::template codes<3>(e01), H::template codes<3>(e23));
+        dst[7 * 32] = make_uint2(H::template codes<3>(o01), H::template codes<3>(o23));
+      } else {
+        const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
+        const uint32_t ev = even_of(t02, t13), od = odd_of(t02, t13);
+        dst[0 * 32] = make_uint2(H::template codes<0>(ev), H::template codes<2>(ev));
+        dst[1 * 32] = make_uint2(H::template codes<0>(od), H::template codes<2>(od));
+        dst[2 * 32] = make_uint2(H::template codes<1>(ev), H::template codes<3>(ev));
+        dst[3 * 32] = make_uint2(H::template codes<1>(od), H::template codes<3>(od));
+      }
+    }
+    if (do_s) {
+      if constexpr (F16) {
+        float m = vs;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+        m = __uint_as_float(__float_as_uint(m) & 0x7f800000u);
+        ref_s = fmaxf(fmaxf(ref_s, m), 0x1p-120f);   // (NaN scales are not the largest)
+        t.vs[lane] = vs * (1.0f / ref_s);
+        if (lane == 0) t.ref = ref_s;
+      } else {
+        t.vs[lane] = vs;
+      }
+      t.ks[lane] = ks;
+      const unsigned long long all = __ballot(here);
+      if (lane == 0) t.there = all;
+    }
+  };
+
+  ask_ids(b0);
+  ask(b0);
+  vec q[KC];
+  load_q32<D, F16>(a, p, h, row, lane, q);
+  v16f o[MT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
+  float m = kNegInf, l = 0.0f, ref = 0x1p-120f;
+  if (b0 < b1) put(buf[0]);
+  __syncthreads();
+
+  for (int b = b0; b < b1; ++b) {
+    const Buf& t = buf[(b - b0) & 1];
+    ask(b + 1);
+    const int key0 = b * kBlock;
+    if (key0 < any_hi && key0 + kBlock > any_lo) {
+      v16f s[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+          s[c] = H::mfma(__builtin_bit_cast(vec, t.k[hh * KC + kc][c * 32 + j]), q[kc], s[c]);
+      const unsigned long long there = t.there;
+      const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi && there == ~0ull;
+      float mx = m;
+      unsigned seen[2] = {0xffff, 0xffff};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
+          s[c][r] *= k4.x, s[c][r + 1] *= k4.y, s[c][r + 2] *= k4.z, s[c][r + 3] *= k4.w;
+        }
+        if (!whole) {
+          seen[c] = 0;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int at = c * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
+            const bool on = ((there >> at) & 1) && key0 + at < row_hi && key0 + at >= row_lo;
+            seen[c] |= static_cast<unsigned>(on) << r;
+            s[c][r] = on ? s[c][r] : kNegInf;
+          }
+        }
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[c][r]), s[c][r + 1]);
+      }
+      mx = fmaxf(mx, lane_xor<32>(mx));
+      const float to = mx == kNegInf ? 0.0f : mx;
+      float alpha = 1.0f;
+      if (__any(mx != m)) {
+        alpha = __builtin_amdgcn_exp2f(m - to);
+        m = mx;
+        l *= alpha;
+      }
+      if constexpr (F16) {
+        const float rn = t.ref;
+        alpha *= ref * (1.0f / rn);
+        ref = rn;
+      }
+      if (__any(alpha != 1.0f)) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t pw[8];
+#pragma unroll
+        for (int r = 0; r < 16; r += 4) {
+          const float4 v4 = *reinterpret_cast<const float4*>(&t.vs[c * 32 + 2 * r + 4 * hh]);
+          const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float pr = __builtin_amdgcn_exp2f(s[c][r + e] - to);
+            l += pr;
+            x[e] = pr * vv[e];
+            if (!whole) x[e] = (seen[c] >> (r + e)) & 1 ? x[e] : 0.0f;   // see few_step
+          }
+          pw[r / 2] = pack16(x[0], x[1], F16);
+          pw[r / 2 + 1] = pack16(x[2], x[3], F16);
+        }
+#pragma unroll
+        for (int st = 0; st < 2; ++st) {
+          const vec pb = __builtin_bit_cast(vec, make_uint4(pw[4 * st], pw[4 * st + 1], pw[4 * st + 2], pw[4 * st + 3]));
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+            o[i] = H::mfma(__builtin_bit_cast(vec, t.v[(c * 2 + st) * 2 + hh][i * 32 + j]), pb, o[i]);
+        }
+      }
+    }
+    if (b + 1 < b1) put(buf[(b - b0 + 1) & 1]);
+    __syncthreads();
+  }
+
+  // out through LDS, 8 rows of each wave at a time
+  l += lane_xor<32>(l);
+  if constexpr (F16) {
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[i][r] *= ref;
+  }
+  constexpr int kStride = D + 4;
+  static_assert(sizeof(buf) >= NW * 8 * kStride * sizeof(float), "the output rows pass through the tiles' LDS");
+  float* so = reinterpret_cast<float*>(&buf[0]) + w * 8 * kStride;
+#pragma unroll
+  for (int round = 0; round < 4; ++round) {
+    __syncthreads();
+    if ((j >> 3) == round) {
+      // register r of tile i: position 32 i + 8 (r / 4) + 4 hh + r % 4 = e * 16 + chunk
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int e = 2 * i + (r >> 3), chunk = 8 * ((r >> 2) & 1) + 4 * hh + (r & 3);
+          so[(j & 7) * kStride + chunk * E + e] = o[i][r];
+        }
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) {
+      const int rr = w * 32 + round * 8 + k;
+      if (rr >= rows) break;
+      const float mm = __shfl(m, round * 8 + k), ll = __shfl(l, round * 8 + k);
+      float y[D / 64];
+#pragma unroll
+      for (int z = 0; z < D / 64; ++z) y[z] = so[k * kStride + lane * (D / 64) + z];
+      if (p.parts == 1) {
+        const int i = (p.tile * M + rr) / a.G;
+        finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + rr - i * a.G, y, mm, ll, lane);
+      } else {
+        const int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + rr;
+#pragma unroll
+        for (int z = 0; z < D / 64; ++z) a.part_o[at * D + lane * (D / 64) + z] = y[z];
+        if (lane == 0) a.part_ml[at] = make_float2(mm, ll);
+      }
+    }
+  }
+}
+
 // Joins the parts of split tiles, a workgroup per row: the parts' weights
 // first, then the sum of their outputs, eight at a time (D / 4 threads each).
 constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 
 template <int D, int M>
-__global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a) {
+__global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target) {
   constexpr int W = D / 4, NG = 256 / W;
   __shared__ SchedShared sched;
   __shared__ float f[kMostParts];
   __shared__ float red[8];
   __shared__ __align__(16) float4 sum[NG][W];
   Piece p;
-  if (!find_piece<M>(a, sched, blockIdx.x, true, &p)) return;
+  if (!find_piece<M, 256>(a, sched, blockIdx.x, true, target, &p)) return;
+  if (M > kFewRows && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // as k_rows numbers them
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y, row = blockIdx.z;
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
   if (row >= rows) return;
@@ -630,42 +1032,77 @@ __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a) {
   finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, out, mm, l, lane);
 }
 
-constexpr int kPieces = 1024;   // pieces of work over all KV heads aimed at
+// Pieces of work over all KV heads aimed at, and rows of a tile of k_rows.
+constexpr int kPieces = 1024, kRowPieces = 512, kRowTile = 256;
+
+struct Grid {
+  int64_t tiles, merges;
+};
+// Bounds that hold for all lengths: tiles of the requests, tiles with several parts.
+Grid grid_of(const CacheAttnArgs& a, int M, int target) {
+  const int64_t per = (static_cast<int64_t>(a.max_q) * a.G + M - 1) / M;
+  Grid g;
+  g.tiles = a.R + static_cast<int64_t>(a.T) * a.G / M;
+  if (g.tiles > a.R * per) g.tiles = a.R * per;
+  g.merges = g.tiles < target ? g.tiles : target;
+  return g;
+}
+
+template <int D, int M>
+hipError_t merge(const CacheAttnArgs& a, const Grid& g, int target, int64_t rows, hipStream_t s) {
+  k_merge<D, M><<<dim3(static_cast<unsigned>(g.merges), a.g.Hkv, static_cast<unsigned>(rows < M ? rows : M)), dim3(256),
+                  0, s>>>(a, target);
+  return hipGetLastError();
+}
 
 template <int D, int NT>
 hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   constexpr int M = 16 * NT;
-  const int64_t per = (static_cast<int64_t>(a.max_q) * a.G + M - 1) / M;
-  int64_t tiles = a.R + static_cast<int64_t>(a.T) * a.G / M;
-  if (tiles > a.R * per) tiles = a.R * per;
-  k_few<D, NT, 2><<<dim3(static_cast<unsigned>(tiles + a.target), a.g.Hkv), dim3(256), 0, s>>>(a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t merges = tiles < a.target ? tiles : a.target;
-  const int64_t rows = static_cast<int64_t>(a.max_q) * a.G;
-  k_merge<D, M><<<dim3(static_cast<unsigned>(merges), a.g.Hkv, static_cast<unsigned>(rows < M ? rows : M)), dim3(256), 0, s>>>(a);
-  return hipGetLastError();
+  const Grid g = grid_of(a, M, a.target);
+  k_few<D, NT, 2><<<dim3(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv)), dim3(256), 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : merge<D, M>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
+}
+
+template <int D, bool F16>
+hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
+  const Grid g = grid_of(a, kRowTile, a.target_rows);
+  k_rows<D, kRowTile / 32, F16><<<dim3(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv)), dim3(2 * kRowTile), 0,
+                                  s>>>(a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : merge<D, kRowTile>(a, g, a.target_rows, static_cast<int64_t>(a.max_q) * a.G, s);
 }
 
 template <int D>
 hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
-  return static_cast<int64_t>(a.max_q) * a.G <= 16 ? few<D, 1>(a, s) : few<D, 2>(a, s);
+  const int64_t most = static_cast<int64_t>(a.max_q) * a.G;
+  if (most <= 16) return few<D, 1>(a, s);
+  hipError_t e = hipSuccess;
+  if (a.G <= kFewRows) e = few<D, 2>(a, s);   // requests of few rows; with more heads than that there are none
+  if (e != hipSuccess || most <= kFewRows) return e;
+  return a.is_fp16 ? rows<D, true>(a, s) : rows<D, false>(a, s);
 }
+
+int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }
 
 }  // namespace
 
-int cache_attn_target(int Hkv) { return (kPieces + Hkv - 1) / Hkv; }
-
+// Partial outputs: 2 * target tiles' worth, of either kernel (one after the other).
 size_t cache_attn_partial_bytes(int D, int Hkv, int G, int max_q, size_t* ml_offset) {
-  (void)G;
-  (void)max_q;
-  const size_t rows = static_cast<size_t>(2) * cache_attn_target(Hkv) * Hkv * 32;
+  size_t rows = static_cast<size_t>(2) * target_of(kPieces, Hkv) * Hkv * kFewRows;
+  if (static_cast<int64_t>(max_q) * G > kFewRows) {
+    const size_t many = static_cast<size_t>(2) * target_of(kRowPieces, Hkv) * Hkv * kRowTile;
+    rows = rows > many ? rows : many;
+  }
   *ml_offset = rows * D * sizeof(float);
   return rows * (D * sizeof(float) + sizeof(float2));
 }
 
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int D, hipStream_t s) {
-  return D == 128 ? attn_d<128>(a, s) : attn_d<64>(a, s);
+  CacheAttnArgs b = a;
+  b.target = target_of(kPieces, a.g.Hkv);
+  b.target_rows = target_of(kRowPieces, a.g.Hkv);
+  return D == 128 ? attn_d<128>(b, s) : attn_d<64>(b, s);
 }
 
 }  // namespace ra

@@ -273,7 +273,7 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
   a.out_dtype = p->out_dtype;
   a.had = p->rotation == RA_ROT_HADAMARD;
   a.vhad = p->v_rotation == RA_VROT_HADAMARD;
-  a.target = ra::cache_attn_target(p->Hkv);
+  a.target = a.target_rows = 0;
   return hip_status(ra::launch_cache_attn(a, p->D, static_cast<hipStream_t>(stream)), "cache_attn");
 }
 
