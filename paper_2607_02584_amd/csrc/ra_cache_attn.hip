@@ -155,14 +155,17 @@ __device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool 
     __syncthreads();
     if (x < base) break;   // found
   }
-  const int r = sh.hit[0];
+  // the same in every lane, and known to be: loops and addresses stay scalar
+  const int r = __builtin_amdgcn_readfirstlane(sh.hit[0]);
   if (r < 0) return false;
+  const int at = __builtin_amdgcn_readfirstlane(sh.hit[1]);
+  const Request q = request_of<M>(a, r);
   out->r = r;
-  out->q = request_of<M>(a, r);
-  out->parts = sh.hit[2];
-  out->tile = merge ? sh.hit[1] : sh.hit[1] / out->parts;
-  out->part = merge ? 0 : sh.hit[1] - out->tile * out->parts;
-  out->slot = sh.hit[3] + out->tile * out->parts;
+  out->q = q;
+  out->parts = __builtin_amdgcn_readfirstlane(sh.hit[2]);
+  out->tile = merge ? at : at / out->parts;
+  out->part = merge ? 0 : at - out->tile * out->parts;
+  out->slot = __builtin_amdgcn_readfirstlane(sh.hit[3]) + out->tile * out->parts;
   return true;
 }
 
@@ -240,6 +243,16 @@ __device__ __forceinline__ void load_tile(const CacheAttnArgs& a, Tile16<D>& t, 
   t.vs = *reinterpret_cast<const float4*>(sc + page);
 }
 
+// Lets the matrix products that write x finish: for uses behind control flow.
+template <typename V>
+__device__ __forceinline__ void settle(V& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 15\n\ts_nop 7" : "+v"(x));
+#else
+  (void)x;
+#endif
+}
+
 template <int B>
 __device__ __forceinline__ v2bf codes2(uint32_t w) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, B); }
 
@@ -315,44 +328,52 @@ __device__ __forceinline__ uint32_t dword_of(const typename std::conditional<D =
   else return i == 0 ? v.x : v.y;
 }
 
-// The rows' state in a wave: Q, running maximum and sum, O^T.
+// The rows' state in a wave: running maximum and sum, O^T, and Q -- in registers
+// for 16 rows, for 32 in LDS (two waves then fit a SIMD).
 template <int D, int NT>
 struct Rows {
-  v8bf qh[NT][D / 32], ql[NT][D / 32];
+  v8bf qh[NT == 1 ? D / 32 : 1], ql[NT == 1 ? D / 32 : 1];
   v4f o[NT][D / 16];
   float m[NT], l[NT];
   int hi[NT], lo[NT];   // keys that the lane's row sees: [lo, hi)
 };
 
-// One step of 16 KT keys.  `there` bit i: the i-th 16 keys are on a page; whole:
+// One step of 16 KT keys for the first 16 N rows.  `there` bit i: the i-th 16 keys are on a page; whole:
 // every row sees every key.
-template <int D, int NT, int KT>
-__device__ __forceinline__ void few_step(Rows<D, NT>& x, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
+//
+// Control flow here must not skip over a block between a matrix product and the
+// first use of its result: the compiler then leaves out the wait states that
+// the use needs on the skipping path (seen as wrong first registers when the
+// second 16 rows were skipped inside the step).  N is therefore a constant.
+template <int D, int NT, int N, int KT>
+__device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
                                           int g) {
   constexpr int KC = D / 32;
-  v4f s[NT][KT];
+  v4f s[N][KT];
 #pragma unroll
   for (int i = 0; i < KT; ++i) {
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) s[nt][i] = v4f{0, 0, 0, 0};
+    for (int nt = 0; nt < N; ++nt) s[nt][i] = v4f{0, 0, 0, 0};
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
       const v8bf k = codes8(dword_of<D>(t[i].k, c));
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, x.qh[nt][c], s[nt][i], 0, 0, 0);
-        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, x.ql[nt][c], s[nt][i], 0, 0, 0);
+      for (int nt = 0; nt < N; ++nt) {
+        const v8bf qh = NT == 1 ? x.qh[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128];
+        const v8bf ql = NT == 1 ? x.ql[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128 + 64];
+        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qh, s[nt][i], 0, 0, 0);
+        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[nt][i], 0, 0, 0);
       }
     }
     const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
+    for (int nt = 0; nt < N; ++nt)
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[nt][i][e] *= ks[e];
   }
-  v8bf ph[NT][KT / 2], pl[NT][KT / 2];
+  v8bf ph[N][KT / 2], pl[N][KT / 2];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
+  for (int nt = 0; nt < N; ++nt) {
     unsigned seen = 0xffff;   // bit 4 i + e: this lane's row sees key 16 i + 4 g + e of the step
     if (!whole) {
       seen = 0;
@@ -423,7 +444,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const Tile16<D> (&t)[KT
       if constexpr (D == 128) v = join(codes2<B>(n[0]), codes2<B>(n[1]), codes2<B>(n[2]), codes2<B>(n[3]));
       else v = join(codes2<B>(n[0]), codes2<B + 2>(n[0]), codes2<B>(n[1]), codes2<B + 2>(n[1]));
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
+      for (int nt = 0; nt < N; ++nt) {
         x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[nt][u], x.o[nt][e], 0, 0, 0);
         x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
       }
@@ -442,12 +463,13 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const Tile16<D> (&t)[KT
 }
 
 template <int D, int NT, int KT>
-__global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
+__global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
   __shared__ __align__(16) float so[4][16][kStride];
   __shared__ float sm[4][M], sl[4][M];
   __shared__ SchedShared sched;
+  __shared__ __align__(16) v8bf sq_all[NT == 1 ? 1 : NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
   // heads fastest: the heads of a page, neighbours in memory, are read together
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
@@ -495,7 +517,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
       there |= static_cast<unsigned>(id >= 0) << i;
       load_tile<D>(a, t[i], id >= 0 ? id : 0, h, (b * KT + i) * 16, lane);
     }
-    if (((at + KT) & 63) == 0) {   // the next step begins the next 64
+    if (((at + KT) & 63) == 0 && b + 1 < w1) {   // the next step begins the next 64
       ids = ids_next;
       if (b + 1 + 64 / KT < w1) ids_next = ids_from((b + 1) * KT + 64);
     }
@@ -510,7 +532,17 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
-    load_q<D>(a, p, h, row, lane, x.qh[nt], x.ql[nt]);
+    if constexpr (NT == 1) {
+      load_q<D>(a, p, h, row, lane, x.qh, x.ql);
+    } else if (w == nt) {   // one wave for all four
+      v8bf qh[D / 32], ql[D / 32];
+      load_q<D>(a, p, h, row, lane, qh, ql);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        sq_all[(nt * (D / 32) + c) * 128 + lane] = qh[c];
+        sq_all[(nt * (D / 32) + c) * 128 + 64 + lane] = ql[c];
+      }
+    }
     const int pos = first + row / a.G;
     x.hi[nt] = a.causal ? pos + 1 : p.q.n;
     if (x.hi[nt] > p.q.n) x.hi[nt] = p.q.n;
@@ -520,19 +552,31 @@ __global__ __launch_bounds__(256, NT == 1 ? 2 : 1) void k_few(CacheAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) x.o[nt][e] = v4f{0, 0, 0, 0};
   }
+  if constexpr (NT > 1) __syncthreads();
   auto whole = [&](int b, unsigned there) {
     return b * kStep >= all_lo && b * kStep + kStep <= all_hi && b * kStep + kStep <= p.q.n && there == (1u << KT) - 1;
   };
-  // the next step's loads are in flight while a step is computed
-  for (int b = w0; b < w1; b += 2) {
-    if (b + 1 < w1) hb = load(b + 1, tb);
-    __builtin_amdgcn_sched_barrier(0);
-    few_step<D, NT, KT>(x, ta, ha, whole(b, ha), b * kStep, g);
-    if (b + 1 >= w1) break;
-    if (b + 2 < w1) ha = load(b + 2, ta);
-    __builtin_amdgcn_sched_barrier(0);
-    few_step<D, NT, KT>(x, tb, hb, whole(b + 1, hb), (b + 1) * kStep, g);
-  }
+  // The next step's loads are in flight while a step is computed; behind the
+  // last step the last one is asked for again, so that every step waits for
+  // its own loads alone.
+  auto run = [&](auto nn) {
+    constexpr int N = decltype(nn)::value;
+    for (int b = w0; b < w1; b += 2) {
+      hb = load(b + 1 < w1 ? b + 1 : b, tb);
+      __builtin_amdgcn_sched_barrier(0);
+      few_step<D, NT, N, KT>(x, sq_all + lane, ta, ha, whole(b, ha), b * kStep, g);
+      if (b + 1 >= w1) break;
+      ha = load(b + 2 < w1 ? b + 2 : b + 1, ta);
+      __builtin_amdgcn_sched_barrier(0);
+      few_step<D, NT, N, KT>(x, sq_all + lane, tb, hb, whole(b + 1, hb), (b + 1) * kStep, g);
+    }
+  };
+  if (NT == 1 || rows <= 16) run(std::integral_constant<int, 1>{});
+  else run(std::integral_constant<int, NT>{});
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+    for (int e = 0; e < E; ++e) settle(x.o[nt][e]);
 
   // join the four waves
 #pragma unroll
@@ -925,6 +969,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     __syncthreads();
   }
 
+#pragma unroll
+  for (int i = 0; i < MT; ++i) settle(o[i]);
+
   // out through LDS, 8 rows of each wave at a time
   l += lane_xor<32>(l);
   if constexpr (F16) {
@@ -971,12 +1018,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   }
 }
 
-// Joins the parts of split tiles, a workgroup per row: the parts' weights
-// first, then the sum of their outputs, eight at a time (D / 4 threads each).
+// Joins the parts of split tiles, a workgroup for per_group rows one after
+// the other: the parts'
+// weights first, then the sum of their outputs, eight at a time (D / 4 threads
+// each).
 constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 
 template <int D, int M>
-__global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target) {
+__global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target, int per_group) {
   constexpr int W = D / 4, NG = 256 / W;
   __shared__ SchedShared sched;
   __shared__ float f[kMostParts];
@@ -985,51 +1034,56 @@ __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target) {
   Piece p;
   if (!find_piece<M, 256>(a, sched, blockIdx.x, true, target, &p)) return;
   if (M > kFewRows && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // as k_rows numbers them
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y, row = blockIdx.z;
-  const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
-  if (row >= rows) return;
-  const int64_t first = (static_cast<int64_t>(p.slot) * a.g.Hkv + h) * M + row;   // of part 0
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y;
+  int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
+  const int row0 = blockIdx.z * per_group;
+  if (row0 + per_group < rows) rows = row0 + per_group;
   const int64_t step = static_cast<int64_t>(a.g.Hkv) * M;
-  float mm = kNegInf;
-  for (int i = tid; i < p.parts; i += 256) {
-    const float m = a.part_ml[first + i * step].x;
-    f[i] = m;
-    mm = fmaxf(mm, m);
-  }
+  for (int row = row0; row < rows; ++row) {
+    const int64_t first = (static_cast<int64_t>(p.slot) * a.g.Hkv + h) * M + row;   // of part 0
+    float mm = kNegInf;
+    for (int i = tid; i < p.parts; i += 256) {
+      const float m = a.part_ml[first + i * step].x;
+      f[i] = m;
+      mm = fmaxf(mm, m);
+    }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
-  if (lane == 0) red[w] = mm;
-  __syncthreads();
-  mm = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  float l = 0.0f;
-  for (int i = tid; i < p.parts; i += 256) {
-    f[i] = rescale(f[i], mm);
-    l += f[i] * a.part_ml[first + i * step].y;
-  }
+    for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
+    if (lane == 0) red[w] = mm;
+    __syncthreads();
+    mm = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    float l = 0.0f;
+    for (int i = tid; i < p.parts; i += 256) {
+      f[i] = rescale(f[i], mm);
+      l += f[i] * a.part_ml[first + i * step].y;
+    }
 #pragma unroll
-  for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-  if (lane == 0) red[4 + w] = l;
-  __syncthreads();
-  l = red[4] + red[5] + red[6] + red[7];
-  const int g = tid / W, c = tid % W;
-  float4 y = make_float4(0, 0, 0, 0);
+    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
+    if (lane == 0) red[4 + w] = l;
+    __syncthreads();
+    l = red[4] + red[5] + red[6] + red[7];
+    const int g = tid / W, c = tid % W;
+    float4 y = make_float4(0, 0, 0, 0);
 #pragma unroll 4
-  for (int i = g; i < p.parts; i += NG) {
-    const float4 o = *reinterpret_cast<const float4*>(a.part_o + (first + i * step) * D + c * 4);
-    const float x = f[i];
-    y.x += x * o.x, y.y += x * o.y, y.z += x * o.z, y.w += x * o.w;
+    for (int i = g; i < p.parts; i += NG) {
+      const float4 o = *reinterpret_cast<const float4*>(a.part_o + (first + i * step) * D + c * 4);
+      const float x = f[i];
+      y.x += x * o.x, y.y += x * o.y, y.z += x * o.z, y.w += x * o.w;
+    }
+    sum[g][c] = y;
+    __syncthreads();
+    if (w == 0) {
+      float out[D / 64] = {};
+      const float* s = reinterpret_cast<const float*>(&sum[0][0]);
+#pragma unroll
+      for (int i = 0; i < NG; ++i)
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) out[x] += s[i * D + lane * (D / 64) + x];
+      const int i = (p.tile * M + row) / a.G;
+      finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, out, mm, l, lane);
+    }
+    __syncthreads();   // before the next row's parts
   }
-  sum[g][c] = y;
-  __syncthreads();
-  if (w) return;
-  float out[D / 64] = {};
-  const float* s = reinterpret_cast<const float*>(&sum[0][0]);
-#pragma unroll
-  for (int i = 0; i < NG; ++i)
-#pragma unroll
-    for (int x = 0; x < D / 64; ++x) out[x] += s[i * D + lane * (D / 64) + x];
-  const int i = (p.tile * M + row) / a.G;
-  finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, out, mm, l, lane);
 }
 
 // Pieces of work over all KV heads aimed at, and rows of a tile of k_rows.
@@ -1050,15 +1104,20 @@ Grid grid_of(const CacheAttnArgs& a, int M, int target) {
 
 template <int D, int M>
 hipError_t merge(const CacheAttnArgs& a, const Grid& g, int target, int64_t rows, hipStream_t s) {
-  k_merge<D, M><<<dim3(static_cast<unsigned>(g.merges), a.g.Hkv, static_cast<unsigned>(rows < M ? rows : M)), dim3(256),
-                  0, s>>>(a, target);
+  if (rows > M) rows = M;
+  // a workgroup per row while those are few enough to run at once
+  const int per_group = g.merges * a.g.Hkv * rows <= 4096 ? 1 : M > kFewRows ? 16 : 8;
+  k_merge<D, M><<<dim3(static_cast<unsigned>(g.merges), a.g.Hkv, static_cast<unsigned>((rows + per_group - 1) / per_group)),
+                  dim3(256), 0, s>>>(a, target, per_group);
   return hipGetLastError();
 }
 
 template <int D, int NT>
 hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   constexpr int M = 16 * NT;
-  const Grid g = grid_of(a, M, a.target);
+  Grid g;
+  g.tiles = a.R;   // a request of few rows is one tile
+  g.merges = g.tiles < a.target ? g.tiles : a.target;
   k_few<D, NT, 2><<<dim3(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv)), dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, M>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
