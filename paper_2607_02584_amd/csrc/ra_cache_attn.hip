@@ -10,6 +10,7 @@
 // list of rows (row = token * G + head in group), so that a tile of rows
 // shares the K and V it reads.
 #include <type_traits>
+#include <utility>
 
 #include "../../include/rotate_attn.h"
 #include "ra_cache.h"
@@ -640,8 +641,8 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // Q (after RoPE, rotation and scale, in binary32) is rounded once to the input
 // type, P * (V's scale) once to it: 2^-8 and 2^-11 relative, the type's own
 // half step, as everything the model feeds in.  In binary16 the V scales are
-// taken relative to the power of two of the largest so far (`ref`; O is in
-// units of it), so that P * scale neither overflows nor loses small values.
+// taken relative to the power of two of the largest so far (O is in units of
+// it), so that P * scale neither overflows nor loses small values.
 //
 // LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
 // bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
@@ -721,20 +722,44 @@ __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p,
   }
 }
 
+// Scores are taken relative to a reference per row that moves only when one
+// passes it by kSlack (weights up to 2^8 keep their precision in either type):
+// x = s * (K's scale) - ref is one operation, and most tiles rescale nothing.
+constexpr float kSlack = 8.0f;
+
+// f(0) .. f(N - 1), each index a compile-time constant
+template <typename F, int... I>
+__device__ __forceinline__ void each_(F&& f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>()), ...);
+}
+template <int N, typename F>
+__device__ __forceinline__ void each(F&& f) {
+  each_(f, std::make_integer_sequence<int, N>());
+}
+
+// Pipeline over tiles: a tile begins with its scores in registers.  Once a
+// chunk of 32 keys has its probabilities, its score registers take the next
+// tile's scores of that chunk; those products and the chunk's P V run on the
+// matrix cores beside the next chunk's probabilities, their LDS operands read
+// kAhead products ahead.  So K is staged two tiles ahead and V (with both
+// scales) one, and two LDS buffers of each suffice.
 template <int D, int NW, bool F16>
 __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs a) {
   typedef Half16<F16> H;
   typedef typename H::vec vec;
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
-  struct Buf {
-    uint4 k[D / 8][64];
-    uint4 v[8][D];
+  struct Scales {
     float ks[64], vs[64];
     unsigned long long there;   // keys that are on a page
     float ref;
   };
-  __shared__ __align__(16) Buf buf[2];
+  struct Buf {
+    uint4 k[2][D / 8][64];
+    uint4 v[2][8][D];
+    Scales sc[2];
+  };
+  __shared__ __align__(16) Buf buf;
   __shared__ SchedShared sched;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
@@ -756,12 +781,16 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   const int b0 = bl + p.part * per, b1 = b0 + per < bh ? b0 + per : bh;
   // bounds that every row of this wave sees, and its lane's row
   const int wrow = p.tile * M + w * 32, row = wrow + j;
-  const int wi1 = wrow + 31 < p.tile * M + rows - 1 ? (wrow + 31) / a.G : i1;
-  const int all_hi = a.causal ? first + wrow / a.G + 1 : p.q.n;
+  const int wi0 = wrow / a.G, wi1 = wrow + 31 < p.tile * M + rows - 1 ? (wrow + 31) / a.G : i1;
+  const int all_hi = a.causal ? first + wi0 + 1 : p.q.n;
   const int all_lo = a.window ? first + wi1 - a.window + 1 : 0;
-  // keys that any row of this wave sees; a wave behind the tile's rows sees none
-  const int any_hi = w * 32 >= rows ? 0 : a.causal ? first + wi1 + 1 : p.q.n;
-  const int any_lo = a.window ? first + wrow / a.G - a.window + 1 : 0;
+  // tiles in which any row of this wave sees a key: [t0, t1); a wave behind the tile's rows has none
+  int any_hi = a.causal ? first + wi1 + 1 : p.q.n, any_lo = a.window ? first + wi0 - a.window + 1 : 0;
+  if (any_hi < 0) any_hi = 0;
+  if (any_lo < 0) any_lo = 0;
+  int t0 = any_lo / kBlock > b0 ? any_lo / kBlock : b0;
+  int t1 = (any_hi + kBlock - 1) / kBlock < b1 ? (any_hi + kBlock - 1) / kBlock : b1;
+  if (w * 32 >= rows || t1 <= t0) t0 = t1 = b1;
   const int pos = first + row / a.G;
   int row_hi = a.causal ? pos + 1 : p.q.n;
   if (row_hi > p.q.n) row_hi = p.q.n;
@@ -776,59 +805,71 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     const int id = t < p.q.n ? row_table[t >> page_log] : -1;
     return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages) ? id : -1;
   };
+  auto page_at = [&](int id) { return head_base + static_cast<int64_t>(id < 0 ? 0 : id) * a.g.page_bytes; };
+  // Of 8 waves four stage K, four V; the last one the scales too.
   const bool do_k = NW == 4 || w < 4, do_v = NW == 4 || w >= 4, do_s = w == NW - 1;
   const int mine = (w & 3) * 16;   // this wave's 16 tokens of a tile
 
-  // staged for the next tile: codes, and in the last wave a scale pair per lane
   Codes sk = {}, sv = {};
   float ks = 0.0f, vs = 0.0f;
   bool here = false;
-  int id_c = -1, id_s = -1;   // pages of the tile after the staged one
-  auto ask_ids = [&](int b) {
-    if (b < b1) {
-      id_c = page_of(b * kBlock + mine);
-      if (do_s) id_s = page_of(b * kBlock + lane);
-    }
+  int id_k = -1, id_v = -1, id_s = -1;   // pages of the tiles asked for next
+  auto ids_k = [&](int b) {
+    if (do_k && b < b1) id_k = page_of(b * kBlock + mine);
   };
-  auto ask = [&](int b) {   // loads of tile b, whose page numbers are in hand; then the next tile's numbers
+  auto ids_v = [&](int b) {
     if (b >= b1) return;
+    if (do_v) id_v = page_of(b * kBlock + mine);
+    if (do_s) id_s = page_of(b * kBlock + lane);
+  };
+  auto ask_k = [&](int b) {   // K of tile b, whose page numbers are in hand; then the next tile's numbers
+    if (!do_k || b >= b1) return;
     const int tok = (b * kBlock + mine) & (page - 1);
-    const int id = __builtin_amdgcn_readfirstlane(id_c);
-    const uint8_t* base = head_base + static_cast<int64_t>(id < 0 ? 0 : id) * a.g.page_bytes + tok * (D / 2) + lane * (D / 8);
-    if (do_k) sk = *reinterpret_cast<const Codes*>(base);
+    sk = *reinterpret_cast<const Codes*>(page_at(__builtin_amdgcn_readfirstlane(id_k)) + tok * (D / 2) + lane * (D / 8));
+    ids_k(b + 1);
+  };
+  auto ask_v = [&](int b) {
+    if (b >= b1) return;
     if (do_v) {
       // lane = chunk + 16 * (half of the octet) + 32 * hh
-      const int g = ((lane >> 4) & 1) * 2 + hh;   // tokens 4 g ..
-      sv = *reinterpret_cast<const Codes*>(base - lane * (D / 8) + kb + (g * 16 + (lane & 15)) * (D / 8));
+      const int tok = (b * kBlock + mine) & (page - 1), g = ((lane >> 4) & 1) * 2 + hh;   // tokens 4 g ..
+      sv = *reinterpret_cast<const Codes*>(page_at(__builtin_amdgcn_readfirstlane(id_v)) + kb + tok * (D / 2) +
+                                           (g * 16 + (lane & 15)) * (D / 8));
     }
     if (do_s) {
       const int t = b * kBlock + lane;
-      here = id_s >= 0 && t < p.q.n;
+      here = id_s >= 0;   // (then t < n)
+      ks = vs = 0.0f;
       if (here) {
-        const float* sc = reinterpret_cast<const float*>(head_base + static_cast<int64_t>(id_s) * a.g.page_bytes + 2 * kb) +
-                          (t & (page - 1));
+        const float* sc = reinterpret_cast<const float*>(page_at(id_s) + 2 * kb) + (t & (page - 1));
         ks = sc[0];
         vs = sc[page];
-      } else {
-        ks = vs = 0.0f;
+        // a token whose scale is not finite acts through its score alone, so
+        // that it reaches the rows that see it and no others
+        if (!(vs < __builtin_inff())) {
+          ks = vs;
+          vs = 0.0f;
+        }
       }
     }
-    ask_ids(b + 1);
+    ids_v(b + 1);
   };
   float ref_s = 0.0f;   // last wave: power of two of the largest V scale so far
-  auto put = [&](Buf& t) {   // the staged tile into LDS
-    if (do_k) {
-      const int part = lane >> 4, key = mine + (lane & 15);
+  auto put_k = [&](int b) {   // the staged K into LDS
+    if (!do_k || b >= b1) return;
+    const int part = lane >> 4, key = mine + (lane & 15);
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        const uint32_t x = dword_of<D>(sk, c);
-        t.k[part * (D / 32) + c][key] = make_uint4(H::template codes<0>(x), H::template codes<1>(x),
-                                                   H::template codes<2>(x), H::template codes<3>(x));
-      }
+    for (int c = 0; c < D / 32; ++c) {
+      const uint32_t x = dword_of<D>(sk, c);
+      buf.k[b & 1][part * (D / 32) + c][key] = make_uint4(H::template codes<0>(x), H::template codes<1>(x),
+                                                          H::template codes<2>(x), H::template codes<3>(x));
     }
+  };
+  auto put_v = [&](int b) {
+    if (b >= b1) return;
     if (do_v) {
       const int half = (lane >> 4) & 1, i = lane & 15;
-      uint2* dst = reinterpret_cast<uint2*>(&t.v[(w & 3) * 2 + hh][i]) + half;   // position e * 16 + i
+      uint2* dst = reinterpret_cast<uint2*>(&buf.v[b & 1][(w & 3) * 2 + hh][i]) + half;   // position e * 16 + i
       if constexpr (D == 128) {
         const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
                        o23 = odd_of(sv.z, sv.w);
@@ -850,12 +891,13 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
       }
     }
     if (do_s) {
+      Scales& t = buf.sc[b & 1];
       if constexpr (F16) {
-        float m = vs;
+        float mx = vs;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        m = __uint_as_float(__float_as_uint(m) & 0x7f800000u);
-        ref_s = fmaxf(fmaxf(ref_s, m), 0x1p-120f);   // (NaN scales are not the largest)
+        for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+        mx = __uint_as_float(__float_as_uint(mx) & 0x7f800000u);
+        ref_s = fmaxf(fmaxf(ref_s, mx), 0x1p-120f);   // (NaN scales are not the largest)
         t.vs[lane] = vs * (1.0f / ref_s);
         if (lane == 0) t.ref = ref_s;
       } else {
@@ -867,108 +909,167 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     }
   };
 
-  ask_ids(b0);
-  ask(b0);
+  ids_k(b0);
+  ids_v(b0);
+  ask_k(b0);
+  ask_v(b0);
   vec q[KC];
   load_q32<D, F16>(a, p, h, row, lane, q);
-  v16f o[MT];
+  v16f o[MT], s[2];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
-  float m = kNegInf, l = 0.0f, ref = 0x1p-120f;
-  if (b0 < b1) put(buf[0]);
+  float m = kNegInf, l = 0.0f, unit = 0x1p-120f;
+  put_k(b0);
+  put_v(b0);
+  ask_k(b0 + 1);
+  put_k(b0 + 1);
   __syncthreads();
 
-  for (int b = b0; b < b1; ++b) {
-    const Buf& t = buf[(b - b0) & 1];
-    ask(b + 1);
+  auto k_op = [&](int b, int c, int kc) { return __builtin_bit_cast(vec, buf.k[b & 1][hh * KC + kc][c * 32 + j]); };
+  auto scores = [&](int b) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
+#pragma unroll
+    for (int kc = 0; kc < KC; ++kc)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) s[c] = H::mfma(k_op(b, c, kc), q[kc], s[c]);
+#pragma unroll
+    for (int c = 0; c < 2; ++c) settle(s[c]);
+  };
+  if (t0 == b0 && t0 < t1) scores(b0);
+  __syncthreads();   // tile b0's K is read before tile b0 + 2's takes its place
+
+  auto step = [&](int b) {
+    // the waves of a SIMD alternate: the dependent chain of vector work at the
+    // higher priority, the products behind it at the lower one
+    __builtin_amdgcn_s_setprio(1);
+    const Scales& t = buf.sc[b & 1];
     const int key0 = b * kBlock;
-    if (key0 < any_hi && key0 + kBlock > any_lo) {
-      v16f s[2];
+    const float base = m == kNegInf ? 0.0f : m;
+    float mx = kNegInf;
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+      for (int r = 0; r < 16; r += 4) {
+        const float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
+        s[c][r] = __fmaf_rn(s[c][r], k4.x, -base);
+        s[c][r + 1] = __fmaf_rn(s[c][r + 1], k4.y, -base);
+        s[c][r + 2] = __fmaf_rn(s[c][r + 2], k4.z, -base);
+        s[c][r + 3] = __fmaf_rn(s[c][r + 3], k4.w, -base);
+      }
+    }
+    const unsigned long long there = t.there;
+    if (key0 < all_lo || key0 + kBlock > all_hi || there != ~0ull) {
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-#pragma unroll
-      for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-        for (int c = 0; c < 2; ++c)
-          s[c] = H::mfma(__builtin_bit_cast(vec, t.k[hh * KC + kc][c * 32 + j]), q[kc], s[c]);
-      const unsigned long long there = t.there;
-      const bool whole = key0 >= all_lo && key0 + kBlock <= all_hi && there == ~0ull;
-      float mx = m;
-      unsigned seen[2] = {0xffff, 0xffff};
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
-          s[c][r] *= k4.x, s[c][r + 1] *= k4.y, s[c][r + 2] *= k4.z, s[c][r + 3] *= k4.w;
+        for (int r = 0; r < 16; ++r) {
+          const int at = c * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
+          const bool on = ((there >> at) & 1) && key0 + at < row_hi && key0 + at >= row_lo;
+          s[c][r] = on ? s[c][r] : kNegInf;
         }
-        if (!whole) {
-          seen[c] = 0;
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int at = c * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
-            const bool on = ((there >> at) & 1) && key0 + at < row_hi && key0 + at >= row_lo;
-            seen[c] |= static_cast<unsigned>(on) << r;
-            s[c][r] = on ? s[c][r] : kNegInf;
-          }
-        }
-#pragma unroll
-        for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[c][r]), s[c][r + 1]);
-      }
-      mx = fmaxf(mx, lane_xor<32>(mx));
-      const float to = mx == kNegInf ? 0.0f : mx;
-      float alpha = 1.0f;
-      if (__any(mx != m)) {
-        alpha = __builtin_amdgcn_exp2f(m - to);
-        m = mx;
-        l *= alpha;
-      }
-      if constexpr (F16) {
-        const float rn = t.ref;
-        alpha *= ref * (1.0f / rn);
-        ref = rn;
-      }
-      if (__any(alpha != 1.0f)) {
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        uint32_t pw[8];
-#pragma unroll
-        for (int r = 0; r < 16; r += 4) {
-          const float4 v4 = *reinterpret_cast<const float4*>(&t.vs[c * 32 + 2 * r + 4 * hh]);
-          const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
-          float x[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float pr = __builtin_amdgcn_exp2f(s[c][r + e] - to);
-            l += pr;
-            x[e] = pr * vv[e];
-            if (!whole) x[e] = (seen[c] >> (r + e)) & 1 ? x[e] : 0.0f;   // see few_step
-          }
-          pw[r / 2] = pack16(x[0], x[1], F16);
-          pw[r / 2 + 1] = pack16(x[2], x[3], F16);
-        }
-#pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          const vec pb = __builtin_bit_cast(vec, make_uint4(pw[4 * st], pw[4 * st + 1], pw[4 * st + 2], pw[4 * st + 3]));
-#pragma unroll
-          for (int i = 0; i < MT; ++i)
-            o[i] = H::mfma(__builtin_bit_cast(vec, t.v[(c * 2 + st) * 2 + hh][i * 32 + j]), pb, o[i]);
-        }
-      }
     }
-    if (b + 1 < b1) put(buf[(b - b0 + 1) & 1]);
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[c][r]), s[c][r + 1]);
+    mx = fmaxf(mx, lane_xor<32>(mx));
+    const bool move = m == kNegInf ? mx > kNegInf : mx > kSlack;
+    float alpha = 1.0f;
+    if (__any(move)) {
+      const float by = move ? mx : 0.0f;
+      alpha = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(-by);
+      m = move ? base + by : m;
+      l *= alpha;
+#pragma unroll
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[c][r] -= by;
+    }
+    if constexpr (F16) {
+      const float next = t.ref;
+      alpha *= unit * (1.0f / next);
+      unit = next;
+    }
+    if (__any(alpha != 1.0f)) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
+    }
+
+    uint32_t pw[2][8];
+    float ls[4] = {0, 0, 0, 0};
+    auto probs = [&](int c, int r4) {   // registers 4 r4 .. 4 r4 + 3 of chunk c
+      const float4 v4 = *reinterpret_cast<const float4*>(&t.vs[c * 32 + 8 * r4 + 4 * hh]);
+      const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float pr = __builtin_amdgcn_exp2f(s[c][4 * r4 + e]);
+        ls[e] += pr;
+        x[e] = pr * vv[e];
+      }
+      pw[c][2 * r4] = pack16(x[0], x[1], F16);
+      pw[c][2 * r4 + 1] = pack16(x[2], x[3], F16);
+    };
+    // products of chunk c: 2 MT of P V (step i / MT, tile i % MT), then the KC
+    // score products of chunk c of the next tile (behind the last tile they
+    // take what lies there and nothing reads them: a second form of this code
+    // costs more than they do)
+    constexpr int NP = 2 * MT + KC, kAhead = 4;
+    auto operand = [&](int c, int i) {
+      if (i < 2 * MT) return __builtin_bit_cast(vec, buf.v[b & 1][(c * 2 + i / MT) * 2 + hh][(i % MT) * 32 + j]);
+      return k_op(b + 1, c, i - 2 * MT);
+    };
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4) probs(0, r4);
+    vec ops[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ops[i] = operand(0, i);
+    __builtin_amdgcn_sched_barrier(0);
+    each<2>([&](auto cc) {
+      constexpr int c = decltype(cc)::value;
+      each<NP>([&](auto ii) {
+        constexpr int i = decltype(ii)::value;
+        vec& op = ops[(c * NP + i) % kAhead];
+        if constexpr (i < 2 * MT) {
+          constexpr int st = i / MT;
+          o[i % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pw[c][4 * st], pw[c][4 * st + 1], pw[c][4 * st + 2],
+                                                                     pw[c][4 * st + 3])), o[i % MT]);
+        } else {
+          if constexpr (i == 2 * MT)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
+          s[c] = H::mfma(op, q[i - 2 * MT], s[c]);
+        }
+        constexpr int n = c * NP + i + kAhead;
+        if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
+        // chunk 1's probabilities beside chunk 0's products
+        if constexpr (c == 0 && i % (NP / 4) == NP / 4 - 1) probs(1, i / (NP / 4));
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (c == 0) __builtin_amdgcn_s_setprio(0);
+    });
+    l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+  };
+
+  for (int b = b0; b < b1; ++b) {
+    ask_k(b + 2);
+    ask_v(b + 1);
+    if (b >= t0 && b < t1) {
+      step(b);
+    } else if (b + 1 == t0 && t0 < t1) {
+      scores(b + 1);
+    }
+    put_v(b + 1);
+    put_k(b + 2);
     __syncthreads();
   }
-
 #pragma unroll
   for (int i = 0; i < MT; ++i) settle(o[i]);
 
@@ -978,11 +1079,11 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[i][r] *= ref;
+      for (int r = 0; r < 16; ++r) o[i][r] *= unit;
   }
   constexpr int kStride = D + 4;
   static_assert(sizeof(buf) >= NW * 8 * kStride * sizeof(float), "the output rows pass through the tiles' LDS");
-  float* so = reinterpret_cast<float*>(&buf[0]) + w * 8 * kStride;
+  float* so = reinterpret_cast<float*>(&buf) + w * 8 * kStride;
 #pragma unroll
   for (int round = 0; round < 4; ++round) {
     __syncthreads();
