@@ -498,11 +498,9 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   const int page_shift = a.g.page_log - 4;
   const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
   const int last16 = (p.q.n + 15) / 16;   // tiles that hold cached tokens
-  auto ids_from = [&](int t16) {
+  auto ids_from = [&](int t16) {   // (looked at when used, so that nothing waits here)
     const int t = t16 + lane;
-    const int id = t < last16 ? row_table[t >> page_shift] : -1;
-    // an entry that is no page leaves its keys out
-    return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages) ? id : -1;
+    return row_table[(t < last16 ? t : last16 - 1) >> page_shift];
   };
   int ids = -1, ids_next = -1;
   if (w0 < w1) {
@@ -515,8 +513,10 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
       const int id = __builtin_amdgcn_readlane(ids, (at + i) & 63);
-      there |= static_cast<unsigned>(id >= 0) << i;
-      load_tile<D>(a, t[i], id >= 0 ? id : 0, h, (b * KT + i) * 16, lane);
+      // an entry that is no page leaves its keys out (those behind the end are masked)
+      const bool page = static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages);
+      there |= static_cast<unsigned>(page) << i;
+      load_tile<D>(a, t[i], page ? id : 0, h, (b * KT + i) * 16, lane);
     }
     if (((at + KT) & 63) == 0 && b + 1 < w1) {   // the next step begins the next 64
       ids = ids_next;
@@ -784,13 +784,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   const int wi0 = wrow / a.G, wi1 = wrow + 31 < p.tile * M + rows - 1 ? (wrow + 31) / a.G : i1;
   const int all_hi = a.causal ? first + wi0 + 1 : p.q.n;
   const int all_lo = a.window ? first + wi1 - a.window + 1 : 0;
-  // tiles in which any row of this wave sees a key: [t0, t1); a wave behind the tile's rows has none
-  int any_hi = a.causal ? first + wi1 + 1 : p.q.n, any_lo = a.window ? first + wi0 - a.window + 1 : 0;
-  if (any_hi < 0) any_hi = 0;
-  if (any_lo < 0) any_lo = 0;
-  int t0 = any_lo / kBlock > b0 ? any_lo / kBlock : b0;
-  int t1 = (any_hi + kBlock - 1) / kBlock < b1 ? (any_hi + kBlock - 1) / kBlock : b1;
-  if (w * 32 >= rows || t1 <= t0) t0 = t1 = b1;
+  // tiles from t1 on hold no key that a row of this wave sees; a wave behind the rows of the tile has none at all
+  int t1 = a.causal ? (first + wi1 + kBlock) / kBlock : b1;
+  if (t1 > b1) t1 = b1;
+  if (w * 32 >= rows || t1 < b0) t1 = b0;
   const int pos = first + row / a.G;
   int row_hi = a.causal ? pos + 1 : p.q.n;
   if (row_hi > p.q.n) row_hi = p.q.n;
@@ -800,12 +797,13 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
   const uint8_t* head_base = a.g.cache + static_cast<int64_t>(h) * head_bytes<D>(page);
   const int kb = page * D / 2;
-  // The page of token t of the request, -1 behind its end or where the entry is none.
-  auto page_of = [&](int t) {
-    const int id = t < p.q.n ? row_table[t >> page_log] : -1;
-    return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages) ? id : -1;
-  };
-  auto page_at = [&](int id) { return head_base + static_cast<int64_t>(id < 0 ? 0 : id) * a.g.page_bytes; };
+  // Loads run ahead of their use: what is read here (page numbers one tile
+  // before the codes, codes and scales one before the tile) is looked at when
+  // it is used, not where it is asked for, which would wait for it there.
+  const int last = p.q.n > 0 ? p.q.n - 1 : 0;
+  auto entry_of = [&](int t) { return row_table[(t < last ? t : last) >> page_log]; };
+  auto is_page = [&](int id) { return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages); };
+  auto page_at = [&](int id) { return head_base + static_cast<int64_t>(is_page(id) ? id : 0) * a.g.page_bytes; };
   // Of 8 waves four stage K, four V; the last one the scales too.
   const bool do_k = NW == 4 || w < 4, do_v = NW == 4 || w >= 4, do_s = w == NW - 1;
   const int mine = (w & 3) * 16;   // this wave's 16 tokens of a tile
@@ -813,16 +811,16 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   Codes sk = {}, sv = {};
   float ks = 0.0f, vs = 0.0f;
   bool here = false;
-  int id_k = -1, id_v = -1, id_s = -1;   // pages of the tiles asked for next
+  int id_k = -1, id_v = -1, id_s = -1;   // table entries of the tiles asked for next
   auto ids_k = [&](int b) {
-    if (do_k && b < b1) id_k = page_of(b * kBlock + mine);
+    if (do_k && b < b1) id_k = entry_of(b * kBlock + mine);
   };
   auto ids_v = [&](int b) {
     if (b >= b1) return;
-    if (do_v) id_v = page_of(b * kBlock + mine);
-    if (do_s) id_s = page_of(b * kBlock + lane);
+    if (do_v) id_v = entry_of(b * kBlock + mine);
+    if (do_s) id_s = entry_of(b * kBlock + lane);
   };
-  auto ask_k = [&](int b) {   // K of tile b, whose page numbers are in hand; then the next tile's numbers
+  auto ask_k = [&](int b) {   // K of tile b, whose table entry is in hand; then the next tile's entry
     if (!do_k || b >= b1) return;
     const int tok = (b * kBlock + mine) & (page - 1);
     sk = *reinterpret_cast<const Codes*>(page_at(__builtin_amdgcn_readfirstlane(id_k)) + tok * (D / 2) + lane * (D / 8));
@@ -838,19 +836,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     }
     if (do_s) {
       const int t = b * kBlock + lane;
-      here = id_s >= 0;   // (then t < n)
-      ks = vs = 0.0f;
-      if (here) {
-        const float* sc = reinterpret_cast<const float*>(page_at(id_s) + 2 * kb) + (t & (page - 1));
-        ks = sc[0];
-        vs = sc[page];
-        // a token whose scale is not finite acts through its score alone, so
-        // that it reaches the rows that see it and no others
-        if (!(vs < __builtin_inff())) {
-          ks = vs;
-          vs = 0.0f;
-        }
-      }
+      here = is_page(id_s) && t < p.q.n;
+      const float* sc = reinterpret_cast<const float*>(page_at(id_s) + 2 * kb) + (t & (page - 1));
+      ks = sc[0];
+      vs = sc[page];
     }
     ids_v(b + 1);
   };
@@ -892,18 +881,23 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     }
     if (do_s) {
       Scales& t = buf.sc[b & 1];
+      // a token whose scale is not finite acts through its score alone, so that
+      // it reaches the rows that see it and no others
+      const bool odd = here && !(vs < __builtin_inff());
+      const float k0 = here ? (odd ? vs : ks) : 0.0f;
+      const float v0 = here && !odd ? vs : 0.0f;
       if constexpr (F16) {
-        float mx = vs;
+        float mx = v0;
 #pragma unroll
         for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
         mx = __uint_as_float(__float_as_uint(mx) & 0x7f800000u);
-        ref_s = fmaxf(fmaxf(ref_s, mx), 0x1p-120f);   // (NaN scales are not the largest)
-        t.vs[lane] = vs * (1.0f / ref_s);
+        ref_s = fmaxf(fmaxf(ref_s, mx), 0x1p-120f);
+        t.vs[lane] = v0 * (1.0f / ref_s);
         if (lane == 0) t.ref = ref_s;
       } else {
-        t.vs[lane] = vs;
+        t.vs[lane] = v0;
       }
-      t.ks[lane] = ks;
+      t.ks[lane] = k0;
       const unsigned long long all = __ballot(here);
       if (lane == 0) t.there = all;
     }
@@ -928,19 +922,14 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   __syncthreads();
 
   auto k_op = [&](int b, int c, int kc) { return __builtin_bit_cast(vec, buf.k[b & 1][hh * KC + kc][c * 32 + j]); };
-  auto scores = [&](int b) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c)
+  for (int c = 0; c < 2; ++c) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
+    for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) s[c] = H::mfma(k_op(b, c, kc), q[kc], s[c]);
-#pragma unroll
-    for (int c = 0; c < 2; ++c) settle(s[c]);
-  };
-  if (t0 == b0 && t0 < t1) scores(b0);
+    for (int kc = 0; kc < KC; ++kc) s[c] = H::mfma(k_op(b0, c, kc), q[kc], s[c]);
+    settle(s[c]);
+  }
   __syncthreads();   // tile b0's K is read before tile b0 + 2's takes its place
 
   auto step = [&](int b) {
@@ -950,16 +939,16 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     const Scales& t = buf.sc[b & 1];
     const int key0 = b * kBlock;
     const float base = m == kNegInf ? 0.0f : m;
-    float mx = kNegInf;
+    float x[2][16], mx = kNegInf;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         const float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
-        s[c][r] = __fmaf_rn(s[c][r], k4.x, -base);
-        s[c][r + 1] = __fmaf_rn(s[c][r + 1], k4.y, -base);
-        s[c][r + 2] = __fmaf_rn(s[c][r + 2], k4.z, -base);
-        s[c][r + 3] = __fmaf_rn(s[c][r + 3], k4.w, -base);
+        x[c][r] = __fmaf_rn(s[c][r], k4.x, -base);
+        x[c][r + 1] = __fmaf_rn(s[c][r + 1], k4.y, -base);
+        x[c][r + 2] = __fmaf_rn(s[c][r + 2], k4.z, -base);
+        x[c][r + 3] = __fmaf_rn(s[c][r + 3], k4.w, -base);
       }
     }
     const unsigned long long there = t.there;
@@ -970,13 +959,13 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
         for (int r = 0; r < 16; ++r) {
           const int at = c * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
           const bool on = ((there >> at) & 1) && key0 + at < row_hi && key0 + at >= row_lo;
-          s[c][r] = on ? s[c][r] : kNegInf;
+          x[c][r] = on ? x[c][r] : kNegInf;
         }
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, s[c][r]), s[c][r + 1]);
+      for (int r = 0; r < 16; r += 2) mx = fmaxf(fmaxf(mx, x[c][r]), x[c][r + 1]);
     mx = fmaxf(mx, lane_xor<32>(mx));
     const bool move = m == kNegInf ? mx > kNegInf : mx > kSlack;
     float alpha = 1.0f;
@@ -988,7 +977,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[c][r] -= by;
+        for (int r = 0; r < 16; ++r) x[c][r] -= by;
     }
     if constexpr (F16) {
       const float next = t.ref;
@@ -1004,18 +993,20 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
 
     uint32_t pw[2][8];
     float ls[4] = {0, 0, 0, 0};
+    auto v_scales = [&](int n) { return *reinterpret_cast<const float4*>(&t.vs[8 * n + 4 * hh]); };
+    float4 v4 = v_scales(0);   // read a group ahead
     auto probs = [&](int c, int r4) {   // registers 4 r4 .. 4 r4 + 3 of chunk c
-      const float4 v4 = *reinterpret_cast<const float4*>(&t.vs[c * 32 + 8 * r4 + 4 * hh]);
       const float vv[4] = {v4.x, v4.y, v4.z, v4.w};
-      float x[4];
+      if (4 * c + r4 < 7) v4 = v_scales(4 * c + r4 + 1);
+      float y[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float pr = __builtin_amdgcn_exp2f(s[c][4 * r4 + e]);
+        const float pr = __builtin_amdgcn_exp2f(x[c][4 * r4 + e]);
         ls[e] += pr;
-        x[e] = pr * vv[e];
+        y[e] = pr * vv[e];
       }
-      pw[c][2 * r4] = pack16(x[0], x[1], F16);
-      pw[c][2 * r4 + 1] = pack16(x[2], x[3], F16);
+      pw[c][2 * r4] = pack16(y[0], y[1], F16);
+      pw[c][2 * r4 + 1] = pack16(y[2], y[3], F16);
     };
     // products of chunk c: 2 MT of P V (step i / MT, tile i % MT), then the KC
     // score products of chunk c of the next tile (behind the last tile they
@@ -1061,11 +1052,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   for (int b = b0; b < b1; ++b) {
     ask_k(b + 2);
     ask_v(b + 1);
-    if (b >= t0 && b < t1) {
-      step(b);
-    } else if (b + 1 == t0 && t0 < t1) {
-      scores(b + 1);
-    }
+    if (b < t1) step(b);
     put_v(b + 1);
     put_k(b + 2);
     __syncthreads();
@@ -1188,7 +1175,7 @@ __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target, int 
 }
 
 // Pieces of work over all KV heads aimed at, and rows of a tile of k_rows.
-constexpr int kPieces = 1024, kRowPieces = 512, kRowTile = 256;
+constexpr int kPieces = 1024, kRowPieces = 512, kRowTile = 128;
 
 struct Grid {
   int64_t tiles, merges;
