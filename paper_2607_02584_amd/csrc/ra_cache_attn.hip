@@ -743,12 +743,12 @@ __device__ __forceinline__ void each(F&& f) {
 // matrix cores beside the next chunk's probabilities, their LDS operands read
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
-template <int D, int NW, bool F16>
-__global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs a) {
+template <int D, bool F16>
+__global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   typedef Half16<F16> H;
   typedef typename H::vec vec;
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
-  constexpr int M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
+  constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
   struct Scales {
     float ks[64], vs[64];
     unsigned long long there;   // keys that are on a page
@@ -804,48 +804,45 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   auto entry_of = [&](int t) { return row_table[(t < last ? t : last) >> page_log]; };
   auto is_page = [&](int id) { return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages); };
   auto page_at = [&](int id) { return head_base + static_cast<int64_t>(is_page(id) ? id : 0) * a.g.page_bytes; };
-  // Of 8 waves four stage K, four V; the last one the scales too.
-  const bool do_k = NW == 4 || w < 4, do_v = NW == 4 || w >= 4, do_s = w == NW - 1;
-  const int mine = (w & 3) * 16;   // this wave's 16 tokens of a tile
+  const int mine = w * 16;           // each of the four waves stages 16 tokens of a tile,
+  const bool do_s = w == NW - 1;     // the last one the scales too
 
   Codes sk = {}, sv = {};
   float ks = 0.0f, vs = 0.0f;
   bool here = false;
-  int id_k = -1, id_v = -1, id_s = -1;   // table entries of the tiles asked for next
-  auto ids_k = [&](int b) {
-    if (do_k && b < b1) id_k = entry_of(b * kBlock + mine);
+  int id_k = 0, id_v = 0, id_s = 0;   // table entries of the tiles asked for next
+  auto within = [&](int b) { return b < b1 ? b : b1 - 1; };
+  auto entries = [&](int bk, int bv) {
+    id_k = entry_of(within(bk) * kBlock + mine);
+    id_v = entry_of(within(bv) * kBlock + mine);
+    if (do_s) id_s = entry_of(within(bv) * kBlock + lane);
   };
-  auto ids_v = [&](int b) {
-    if (b >= b1) return;
-    if (do_v) id_v = entry_of(b * kBlock + mine);
-    if (do_s) id_s = entry_of(b * kBlock + lane);
-  };
-  auto ask_k = [&](int b) {   // K of tile b, whose table entry is in hand; then the next tile's entry
-    if (!do_k || b >= b1) return;
-    const int tok = (b * kBlock + mine) & (page - 1);
-    sk = *reinterpret_cast<const Codes*>(page_at(__builtin_amdgcn_readfirstlane(id_k)) + tok * (D / 2) + lane * (D / 8));
-    ids_k(b + 1);
-  };
-  auto ask_v = [&](int b) {
-    if (b >= b1) return;
-    if (do_v) {
-      // lane = chunk + 16 * (half of the octet) + 32 * hh
-      const int tok = (b * kBlock + mine) & (page - 1), g = ((lane >> 4) & 1) * 2 + hh;   // tokens 4 g ..
-      sv = *reinterpret_cast<const Codes*>(page_at(__builtin_amdgcn_readfirstlane(id_v)) + kb + tok * (D / 2) +
-                                           (g * 16 + (lane & 15)) * (D / 8));
-    }
+  // K of tile bk and V of tile bv, whose table entries are in hand, then the
+  // entries of the tiles after them.  All addresses come first: a use of an
+  // entry behind a load would wait for that load.  Past the last tile it is
+  // asked for again, so that there are no branches to wait at.
+  auto ask = [&](int bk, int bv) {
+    bk = within(bk);
+    const int cv = within(bv);
+    const int tk = (bk * kBlock + mine) & (page - 1), tv = (cv * kBlock + mine) & (page - 1);
+    const int g = ((lane >> 4) & 1) * 2 + hh;   // V: lane = chunk + 16 * (half of the octet) + 32 * hh, tokens 4 g ..
+    const uint8_t* pk = page_at(__builtin_amdgcn_readfirstlane(id_k)) + tk * (D / 2) + lane * (D / 8);
+    const uint8_t* pv =
+        page_at(__builtin_amdgcn_readfirstlane(id_v)) + kb + tv * (D / 2) + (g * 16 + (lane & 15)) * (D / 8);
     if (do_s) {
-      const int t = b * kBlock + lane;
+      const int t = cv * kBlock + lane;
       here = is_page(id_s) && t < p.q.n;
       const float* sc = reinterpret_cast<const float*>(page_at(id_s) + 2 * kb) + (t & (page - 1));
       ks = sc[0];
       vs = sc[page];
     }
-    ids_v(b + 1);
+    sk = *reinterpret_cast<const Codes*>(pk);
+    sv = *reinterpret_cast<const Codes*>(pv);
+    entries(bk + 1, cv + 1);
   };
   float ref_s = 0.0f;   // last wave: power of two of the largest V scale so far
   auto put_k = [&](int b) {   // the staged K into LDS
-    if (!do_k || b >= b1) return;
+    if (b >= b1) return;
     const int part = lane >> 4, key = mine + (lane & 15);
 #pragma unroll
     for (int c = 0; c < D / 32; ++c) {
@@ -856,28 +853,26 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   };
   auto put_v = [&](int b) {
     if (b >= b1) return;
-    if (do_v) {
-      const int half = (lane >> 4) & 1, i = lane & 15;
-      uint2* dst = reinterpret_cast<uint2*>(&buf.v[b & 1][(w & 3) * 2 + hh][i]) + half;   // position e * 16 + i
-      if constexpr (D == 128) {
-        const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
-                       o23 = odd_of(sv.z, sv.w);
-        dst[0 * 32] = make_uint2(H::template codes<0>(e01), H::template codes<0>(e23));
-        dst[1 * 32] = make_uint2(H::template codes<0>(o01), H::template codes<0>(o23));
-        dst[2 * 32] = make_uint2(H::template codes<1>(e01), H::template codes<1>(e23));
-        dst[3 * 32] = make_uint2(H::template codes<1>(o01), H::template codes<1>(o23));
-        dst[4 * 32] = make_uint2(H::template codes<2>(e01), H::template codes<2>(e23));
-        dst[5 * 32] = make_uint2(H::template codes<2>(o01), H::template codes<2>(o23));
-        dst[6 * 32] = make_uint2(H::template codes<3>(e01), H::template codes<3>(e23));
-        dst[7 * 32] = make_uint2(H::template codes<3>(o01), H::template codes<3>(o23));
-      } else {
-        const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
-        const uint32_t ev = even_of(t02, t13), od = odd_of(t02, t13);
-        dst[0 * 32] = make_uint2(H::template codes<0>(ev), H::template codes<2>(ev));
-        dst[1 * 32] = make_uint2(H::template codes<0>(od), H::template codes<2>(od));
-        dst[2 * 32] = make_uint2(H::template codes<1>(ev), H::template codes<3>(ev));
-        dst[3 * 32] = make_uint2(H::template codes<1>(od), H::template codes<3>(od));
-      }
+    const int half = (lane >> 4) & 1, i = lane & 15;
+    uint2* dst = reinterpret_cast<uint2*>(&buf.v[b & 1][w * 2 + hh][i]) + half;   // position e * 16 + i
+    if constexpr (D == 128) {
+      const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
+                     o23 = odd_of(sv.z, sv.w);
+      dst[0 * 32] = make_uint2(H::template codes<0>(e01), H::template codes<0>(e23));
+      dst[1 * 32] = make_uint2(H::template codes<0>(o01), H::template codes<0>(o23));
+      dst[2 * 32] = make_uint2(H::template codes<1>(e01), H::template codes<1>(e23));
+      dst[3 * 32] = make_uint2(H::template codes<1>(o01), H::template codes<1>(o23));
+      dst[4 * 32] = make_uint2(H::template codes<2>(e01), H::template codes<2>(e23));
+      dst[5 * 32] = make_uint2(H::template codes<2>(o01), H::template codes<2>(o23));
+      dst[6 * 32] = make_uint2(H::template codes<3>(e01), H::template codes<3>(e23));
+      dst[7 * 32] = make_uint2(H::template codes<3>(o01), H::template codes<3>(o23));
+    } else {
+      const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
+      const uint32_t ev = even_of(t02, t13), od = odd_of(t02, t13);
+      dst[0 * 32] = make_uint2(H::template codes<0>(ev), H::template codes<2>(ev));
+      dst[1 * 32] = make_uint2(H::template codes<0>(od), H::template codes<2>(od));
+      dst[2 * 32] = make_uint2(H::template codes<1>(ev), H::template codes<3>(ev));
+      dst[3 * 32] = make_uint2(H::template codes<1>(od), H::template codes<3>(od));
     }
     if (do_s) {
       Scales& t = buf.sc[b & 1];
@@ -903,10 +898,10 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
     }
   };
 
-  ids_k(b0);
-  ids_v(b0);
-  ask_k(b0);
-  ask_v(b0);
+  if (b0 < b1) {
+    entries(b0, b0);
+    ask(b0, b0);
+  }
   vec q[KC];
   load_q32<D, F16>(a, p, h, row, lane, q);
   v16f o[MT], s[2];
@@ -917,8 +912,9 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   float m = kNegInf, l = 0.0f, unit = 0x1p-120f;
   put_k(b0);
   put_v(b0);
-  ask_k(b0 + 1);
+  if (b0 < b1) ask(b0 + 1, b0 + 1);   // (this V is asked for again with the first tile)
   put_k(b0 + 1);
+  if (b0 < b1) entries(b0 + 2, b0 + 1);
   __syncthreads();
 
   auto k_op = [&](int b, int c, int kc) { return __builtin_bit_cast(vec, buf.k[b & 1][hh * KC + kc][c * 32 + j]); };
@@ -1050,8 +1046,7 @@ __global__ __launch_bounds__(64 * NW, NW == 8 ? 1 : 2) void k_rows(CacheAttnArgs
   };
 
   for (int b = b0; b < b1; ++b) {
-    ask_k(b + 2);
-    ask_v(b + 1);
+    ask(b + 2, b + 1);
     if (b < t1) step(b);
     put_v(b + 1);
     put_k(b + 2);
@@ -1214,8 +1209,7 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
 template <int D, bool F16>
 hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
   const Grid g = grid_of(a, kRowTile, a.target_rows);
-  k_rows<D, kRowTile / 32, F16><<<dim3(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv)), dim3(2 * kRowTile), 0,
-                                  s>>>(a);
+  k_rows<D, F16><<<dim3(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv)), dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, kRowTile>(a, g, a.target_rows, static_cast<int64_t>(a.max_q) * a.G, s);
 }
