@@ -235,7 +235,8 @@ template <int D>
 __device__ __forceinline__ void load_tile(const CacheAttnArgs& a, Tile16<D>& t, int id, int h, int key, int lane) {
   typedef typename std::conditional<D == 128, uint4, uint2>::type V;
   const int page = a.g.page, tok = key & (page - 1);
-  const uint8_t* b = a.g.cache + static_cast<int64_t>(id) * a.g.page_bytes + static_cast<int64_t>(h) * head_bytes<D>(page);
+  const uint8_t* b = a.g.cache + static_cast<uint64_t>(static_cast<unsigned>(id)) * static_cast<uint32_t>(a.g.page_bytes) +
+                     static_cast<unsigned>(h * head_bytes<D>(page));
   const int kb = page * D / 2;
   t.k = *reinterpret_cast<const V*>(b + tok * (D / 2) + lane * (D / 8));
   t.v = *reinterpret_cast<const V*>(b + kb + tok * (D / 2) + lane * (D / 8));
@@ -329,7 +330,12 @@ __device__ __forceinline__ uint32_t dword_of(const typename std::conditional<D =
   else return i == 0 ? v.x : v.y;
 }
 
-// The rows' state in a wave: running maximum and sum, O^T, and Q -- in registers
+// Scores are taken relative to a reference per row that moves only when one
+// passes it by kSlack (weights up to 2^8 keep their precision in either type):
+// x = s * (K's scale) - ref is one operation, and most tiles rescale nothing.
+constexpr float kSlack = 8.0f;
+
+// The rows' state in a wave: reference and sum, O^T, and Q -- in registers
 // for 16 rows, for 32 in LDS (two waves then fit a SIMD).
 template <int D, int NT>
 struct Rows {
@@ -368,9 +374,11 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
     }
     const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
 #pragma unroll
-    for (int nt = 0; nt < N; ++nt)
+    for (int nt = 0; nt < N; ++nt) {
+      const float base = x.m[nt] == kNegInf ? 0.0f : x.m[nt];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[nt][i][e] *= ks[e];
+      for (int e = 0; e < 4; ++e) s[nt][i][e] = __fmaf_rn(s[nt][i][e], ks[e], -base);
+    }
   }
   v8bf ph[N][KT / 2], pl[N][KT / 2];
 #pragma unroll
@@ -388,27 +396,32 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
           s[nt][i][e] = on ? s[nt][i][e] : kNegInf;
         }
     }
-    float mx = x.m[nt];
+    float mx = kNegInf;
 #pragma unroll
     for (int i = 0; i < KT; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[nt][i][e]);
     mx = fmaxf(mx, lane_xor<16>(mx));
     mx = fmaxf(mx, lane_xor<32>(mx));
-    const float ref = mx == kNegInf ? 0.0f : mx;   // nothing seen yet: any finite reference gives 0
-    if (__any(mx != x.m[nt])) {
-      const float alpha = __builtin_amdgcn_exp2f(x.m[nt] - ref);
-      x.m[nt] = mx;
+    const bool move = x.m[nt] == kNegInf ? mx > kNegInf : mx > kSlack;
+    if (__any(move)) {
+      const float by = move ? mx : 0.0f;
+      const float alpha = x.m[nt] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(-by);
+      x.m[nt] = move ? (x.m[nt] == kNegInf ? 0.0f : x.m[nt]) + by : x.m[nt];
       x.l[nt] *= alpha;
 #pragma unroll
       for (int e = 0; e < D / 16; ++e) x.o[nt][e] *= alpha;
+#pragma unroll
+      for (int i = 0; i < KT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[nt][i][e] -= by;
     }
 #pragma unroll
     for (int i = 0; i < KT; ++i) {
       const float vs[4] = {t[i].vs.x, t[i].vs.y, t[i].vs.z, t[i].vs.w};
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float pr = __builtin_amdgcn_exp2f(s[nt][i][e] - ref);
+        const float pr = __builtin_amdgcn_exp2f(s[nt][i][e]);
         x.l[nt] += pr;
         float w = pr * vs[e];
         // a scale that is not finite must not reach rows that do not see its token
@@ -507,7 +520,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
     ids = ids_from(w0 * KT);
     if (w0 + 64 / KT < w1) ids_next = ids_from(w0 * KT + 64);
   }
-  auto load = [&](int b, Tile16<D> (&t)[KT]) {   // steps in order; returns the bits of pages that are there
+  auto load = [&](int b, Tile16<D> (&t)[KT]) {   // steps in order (the last one again); the bits of pages that are there
     const int at = (b - w0) * KT;
     unsigned there = 0;
 #pragma unroll
@@ -525,9 +538,15 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
     return there;
   };
 
-  Tile16<D> ta[KT], tb[KT];
-  unsigned ha = 0, hb = 0;
-  if (w0 < w1) ha = load(w0, ta);
+  // Steps in flight: two more than the one computed for 16 rows, one for 32
+  // (registers).
+  constexpr int RING = NT == 1 ? 3 : 2;
+  Tile16<D> ring[RING][KT];
+  unsigned there[RING];
+  if (w0 < w1) {
+#pragma unroll
+    for (int i = 0; i + 1 < RING; ++i) there[i] = load(w0 + i < w1 ? w0 + i : w1 - 1, ring[i]);
+  }
 
   Rows<D, NT> x;
 #pragma unroll
@@ -557,19 +576,19 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   auto whole = [&](int b, unsigned there) {
     return b * kStep >= all_lo && b * kStep + kStep <= all_hi && b * kStep + kStep <= p.q.n && there == (1u << KT) - 1;
   };
-  // The next step's loads are in flight while a step is computed; behind the
-  // last step the last one is asked for again, so that every step waits for
-  // its own loads alone.
+  // Behind the last step the last one is asked for again, so that every step
+  // waits for its own loads alone.
   auto run = [&](auto nn) {
     constexpr int N = decltype(nn)::value;
-    for (int b = w0; b < w1; b += 2) {
-      hb = load(b + 1 < w1 ? b + 1 : b, tb);
-      __builtin_amdgcn_sched_barrier(0);
-      few_step<D, NT, N, KT>(x, sq_all + lane, ta, ha, whole(b, ha), b * kStep, g);
-      if (b + 1 >= w1) break;
-      ha = load(b + 2 < w1 ? b + 2 : b + 1, ta);
-      __builtin_amdgcn_sched_barrier(0);
-      few_step<D, NT, N, KT>(x, sq_all + lane, tb, hb, whole(b + 1, hb), (b + 1) * kStep, g);
+    for (int b = w0; b < w1; b += RING) {
+#pragma unroll
+      for (int i = 0; i < RING; ++i) {
+        if (b + i >= w1) break;
+        constexpr int ahead = RING - 1;
+        there[(i + ahead) % RING] = load(b + i + ahead < w1 ? b + i + ahead : w1 - 1, ring[(i + ahead) % RING]);
+        __builtin_amdgcn_sched_barrier(0);
+        few_step<D, NT, N, KT>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
+      }
     }
   };
   if (NT == 1 || rows <= 16) run(std::integral_constant<int, 1>{});
@@ -722,11 +741,6 @@ __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p,
   }
 }
 
-// Scores are taken relative to a reference per row that moves only when one
-// passes it by kSlack (weights up to 2^8 keep their precision in either type):
-// x = s * (K's scale) - ref is one operation, and most tiles rescale nothing.
-constexpr float kSlack = 8.0f;
-
 // f(0) .. f(N - 1), each index a compile-time constant
 template <typename F, int... I>
 __device__ __forceinline__ void each_(F&& f, std::integer_sequence<int, I...>) {
@@ -801,9 +815,10 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   // before the codes, codes and scales one before the tile) is looked at when
   // it is used, not where it is asked for, which would wait for it there.
   const int last = p.q.n > 0 ? p.q.n - 1 : 0;
-  auto entry_of = [&](int t) { return row_table[(t < last ? t : last) >> page_log]; };
+  auto entry_of = [&](int t) { return row_table[static_cast<unsigned>(t < last ? t : last) >> page_log]; };
   auto is_page = [&](int id) { return static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages); };
-  auto page_at = [&](int id) { return head_base + static_cast<int64_t>(is_page(id) ? id : 0) * a.g.page_bytes; };
+  const uint32_t stride = static_cast<uint32_t>(a.g.page_bytes);   // at most 2^26
+  auto page_at = [&](int id) { return head_base + static_cast<uint64_t>(is_page(id) ? id : 0u) * stride; };
   const int mine = w * 16;           // each of the four waves stages 16 tokens of a tile,
   const bool do_s = w == NW - 1;     // the last one the scales too
 
