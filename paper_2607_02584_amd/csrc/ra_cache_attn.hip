@@ -84,51 +84,99 @@ struct Piece {
 };
 
 struct SchedShared {
-  long long w[8];
-  int s[8][2];
-  int hit[8];
+  float w[4];
+  int s[4][2];
+  int hit[10];
 };
 
-// Piece number x (or, for the merge, tile number x of those with several
-// parts); false past the end.  All threads of the workgroup call it.
-template <int M, int THREADS>
-__device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool merge, int target, Piece* out) {
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  long long W = 0;
-  for (int r = tid; r < a.R; r += THREADS) {
-    const Request q = request_of<M>(a, r);
-    W += static_cast<long long>(q.tiles) * q.blocks;
-  }
+// Inclusive sum over a wave by register moves (row shifts, then the rows' last
+// lanes broadcast on).
+__device__ __forceinline__ int wave_sums(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);   // row_shr:1
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);   // row_bcast:15
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast:31
+  return v;
+}
+__device__ __forceinline__ float wave_total(float v) {
 #pragma unroll
-  for (int d = 32; d; d >>= 1) W += __shfl_xor(W, d);
+  for (int i = 0; i < 6; ++i) {
+    const int u = __float_as_int(v);
+    const int o = i == 0   ? __builtin_amdgcn_update_dpp(0, u, 0x111, 0xF, 0xF, false)
+                  : i == 1 ? __builtin_amdgcn_update_dpp(0, u, 0x112, 0xF, 0xF, false)
+                  : i == 2 ? __builtin_amdgcn_update_dpp(0, u, 0x114, 0xF, 0xF, false)
+                  : i == 3 ? __builtin_amdgcn_update_dpp(0, u, 0x118, 0xF, 0xF, false)
+                  : i == 4 ? __builtin_amdgcn_update_dpp(0, u, 0x142, 0xA, 0xF, false)
+                           : __builtin_amdgcn_update_dpp(0, u, 0x143, 0xC, 0xF, false);
+    v += __int_as_float(o);
+  }
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Blocks of a part, W blocks in all: at least W / target, the sum's roundings
+// (the same in every workgroup) included.
+template <int M>
+__device__ __forceinline__ unsigned part_blocks(float W, int target) {
+  const float c = W * (1.0f + 0x1p-10f) / static_cast<float>(target) + 1.0f;
+  const unsigned C = c < 0x1p26f ? static_cast<unsigned>(c) : 1u << 26;   // a request has 2^24 at most
+  return C < static_cast<unsigned>(least_blocks<M>()) ? least_blocks<M>() : C;
+}
+
+// Piece number x (or, for the merge, tile number x of those with several
+// parts); false past the end.  All 256 threads of the workgroup call it.  Up to
+// 64 requests every wave finds it alone, from one load of the lengths; above,
+// 256 requests at a time through LDS.
+template <int M>
+__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool merge, int target,
+                                           Piece* out) {
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  auto parts_of = [&](const Request& q, unsigned C) {
+    return q.tiles ? (q.blocks ? static_cast<int>((q.blocks + C - 1) / C) : 1) : 0;
+  };
+  auto finish = [&](int r, int at, int n, int slot, const Request& q) {
+    out->r = r;
+    out->q = q;
+    out->parts = n;
+    out->tile = merge ? at : at / n;
+    out->part = merge ? 0 : at - out->tile * n;
+    out->slot = slot + out->tile * n;
+  };
+  if (a.R <= 64) {
+    Request q = {};
+    if (lane < a.R) q = request_of<M>(a, lane);
+    const float W = wave_total(static_cast<float>(q.tiles) * static_cast<float>(q.blocks));
+    const int n = parts_of(q, part_blocks<M>(W, target));
+    const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
+    const int from = wave_sums(mine) - mine, slot = wave_sums(split) - split;
+    const unsigned long long hit = __ballot(x >= from && x < from + mine);
+    if (!hit) return false;
+    const int r = __builtin_ctzll(hit);
+    auto take = [&](int v) { return __builtin_amdgcn_readlane(v, r); };
+    finish(r, x - take(from), take(n), take(slot), {take(q.q0), take(q.ql), take(q.n), take(q.first), take(q.tiles), take(q.blocks)});
+    return true;
+  }
+  float W = 0.0f;
+  Request q0 = {};
+  for (int r = tid; r < a.R; r += 256) {
+    const Request q = request_of<M>(a, r);
+    if (r == tid) q0 = q;
+    W += static_cast<float>(q.tiles) * static_cast<float>(q.blocks);
+  }
+  W = wave_total(W);
   if (lane == 0) sh.w[w] = W;
   if (tid == 0) sh.hit[0] = -1;
   __syncthreads();
-  W = 0;
-#pragma unroll
-  for (int i = 0; i < THREADS / 64; ++i) W += sh.w[i];
-  long long C = (W + target - 1) / target;
-  if (C < least_blocks<M>()) C = least_blocks<M>();
+  const unsigned C = part_blocks<M>((sh.w[0] + sh.w[1]) + (sh.w[2] + sh.w[3]), target);
   int base = 0, slot = 0;
-  for (int r0 = 0; r0 < a.R; r0 += THREADS) {
+  for (int r0 = 0; r0 < a.R; r0 += 256) {
     const int r = r0 + tid;
     Request q = {};
-    int n = 0;
-    if (r < a.R) {
-      q = request_of<M>(a, r);
-      n = q.blocks ? static_cast<int>((q.blocks + C - 1) / C) : 1;
-    }
-    const int split = n > 1 ? q.tiles * n : 0;
-    const int mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
-    int s0 = mine, s1 = split;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const int b0 = __shfl_up(s0, d), b1 = __shfl_up(s1, d);
-      if (lane >= d) {
-        s0 += b0;
-        s1 += b1;
-      }
-    }
+    if (r < a.R) q = r0 == 0 ? q0 : request_of<M>(a, r);
+    const int n = parts_of(q, C);
+    const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
+    const int s0 = wave_sums(mine), s1 = wave_sums(split);
     if (lane == 63) {
       sh.s[w][0] = s0;
       sh.s[w][1] = s1;
@@ -136,7 +184,7 @@ __device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool 
     __syncthreads();
     int t0 = 0, t1 = 0, p0 = 0, p1 = 0;
 #pragma unroll
-    for (int i = 0; i < THREADS / 64; ++i) {
+    for (int i = 0; i < 4; ++i) {
       if (i < w) {
         p0 += sh.s[i][0];
         p1 += sh.s[i][1];
@@ -146,10 +194,9 @@ __device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool 
     }
     const int from = base + p0 + s0 - mine;
     if (x >= from && x < from + mine) {
-      sh.hit[0] = r;
-      sh.hit[1] = x - from;
-      sh.hit[2] = n;
-      sh.hit[3] = slot + p1 + s1 - split;
+      const int found[10] = {r, x - from, n, slot + p1 + s1 - split, q.q0, q.ql, q.n, q.first, q.tiles, q.blocks};
+#pragma unroll
+      for (int i = 0; i < 10; ++i) sh.hit[i] = found[i];
     }
     base += t0;
     slot += t1;
@@ -157,16 +204,9 @@ __device__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool 
     if (x < base) break;   // found
   }
   // the same in every lane, and known to be: loops and addresses stay scalar
-  const int r = __builtin_amdgcn_readfirstlane(sh.hit[0]);
-  if (r < 0) return false;
-  const int at = __builtin_amdgcn_readfirstlane(sh.hit[1]);
-  const Request q = request_of<M>(a, r);
-  out->r = r;
-  out->q = q;
-  out->parts = __builtin_amdgcn_readfirstlane(sh.hit[2]);
-  out->tile = merge ? at : at / out->parts;
-  out->part = merge ? 0 : at - out->tile * out->parts;
-  out->slot = __builtin_amdgcn_readfirstlane(sh.hit[3]) + out->tile * out->parts;
+  auto take = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.hit[i]); };
+  if (take(0) < 0) return false;
+  finish(take(0), take(1), take(2), take(3), {take(4), take(5), take(6), take(7), take(8), take(9)});
   return true;
 }
 
@@ -488,7 +528,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   // heads fastest: the heads of a page, neighbours in memory, are read together
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M, 256>(a, sched, x0, false, a.target, &p)) return;
+  if (!find_piece<M>(a, sched, x0, false, a.target, &p)) return;
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;   // of this tile
   const int first = p.q.first;
@@ -780,7 +820,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   // heads fastest: workgroups go round the 8 XCDs, so a head's keys stay in few L2s
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M, 64 * NW>(a, sched, x0, false, a.target_rows, &p)) return;
+  if (!find_piece<M>(a, sched, x0, false, a.target_rows, &p)) return;
   if (a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
@@ -1130,7 +1170,7 @@ __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target, int 
   __shared__ float red[8];
   __shared__ __align__(16) float4 sum[NG][W];
   Piece p;
-  if (!find_piece<M, 256>(a, sched, blockIdx.x, true, target, &p)) return;
+  if (!find_piece<M>(a, sched, blockIdx.x, true, target, &p)) return;
   if (M > kFewRows && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // as k_rows numbers them
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y;
   int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
