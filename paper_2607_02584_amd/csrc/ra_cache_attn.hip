@@ -252,18 +252,23 @@ __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf
 
 // ------------------------------------------------------ few rows per request --
 //
-// A wave takes 16 NT rows and its own part of the keys, 64 per step, all in
+// A wave takes 16 NT rows and its own part of the keys, 32 per step, all in
 // registers: per 16 keys one load each of K codes, V codes and their scales,
 // S^T = K Q^T (keys as rows, so that a lane holds one query's scores), and
 // O^T += V^T P^T, for which the lane's four keys of two 16-key tiles are
 // already the eight that the product's second operand wants from it.  V's
 // first operand, eight keys of one channel, comes from the four tokens per
 // load by exchanging nibbles of neighbouring tokens (two operations for eight
-// codes) before the conversion.  Q and P * (V's scale) are each the sum of two
-// bf16 values (16 bits: q is exact then when it is a bf16 or binary16 input,
-// P off by 2^-17), since the matrix cores have time: the kernel is bound by
-// HBM, (D + 8) bytes per token and KV head.  The four waves of a workgroup are
-// joined through LDS, the parts of a split tile by k_merge.
+// codes) before the conversion.
+//
+// Q (scaled) and P * (V's scale) are rounded once to bf16, the input type's
+// half step; for binary16 inputs (LO) each is the sum of two bf16 values, 16
+// bits over the whole range of the scales.
+//
+// Bound by HBM, (D + 8) bytes per token and KV head, with the vector units
+// close behind: 212 operations per step, 80 of them conversions of codes.  The
+// four waves of a workgroup are joined through LDS, the parts of a split tile
+// by k_merge.
 
 template <int D>
 struct Tile16 {   // a lane's share of 16 tokens
@@ -316,9 +321,9 @@ __device__ __forceinline__ void split_bf16(float x, __bf16& hi, __bf16& lo) {
 
 // The rows' Q as the second operand of K Q^T: lane = 16 * part + row, its
 // D / 4 channels from part * D / 4 on, after RoPE and rotation.
-template <int D>
-__device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane, v8bf (&hi)[D / 32],
-                       v8bf (&lo)[D / 32]) {
+template <int D, bool LO>
+__device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
+                                       v8bf (&hi)[D / 32], v8bf (&lo)[LO ? D / 32 : 1]) {
   constexpr int N = D / 4;
   const int part = lane >> 4;
   const bool ok = row < p.q.ql * a.G;
@@ -360,7 +365,7 @@ __device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, i
       __bf16 x0, x1;
       split_bf16(y[8 * c + e] * a.c, x0, x1);   // scores come out in base 2
       hi[c][e] = x0;
-      lo[c][e] = x1;
+      if constexpr (LO) lo[c][e] = x1;
     }
 }
 
@@ -377,9 +382,9 @@ constexpr float kSlack = 8.0f;
 
 // The rows' state in a wave: reference and sum, O^T, and Q -- in registers
 // for 16 rows, for 32 in LDS (two waves then fit a SIMD).
-template <int D, int NT>
+template <int D, int NT, bool LO>
 struct Rows {
-  v8bf qh[NT == 1 ? D / 32 : 1], ql[NT == 1 ? D / 32 : 1];
+  v8bf qh[NT == 1 ? D / 32 : 1], ql[NT == 1 && LO ? D / 32 : 1];
   v4f o[NT][D / 16];
   float m[NT], l[NT];
   int hi[NT], lo[NT];   // keys that the lane's row sees: [lo, hi)
@@ -392,8 +397,8 @@ struct Rows {
 // first use of its result: the compiler then leaves out the wait states that
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
-template <int D, int NT, int N, int KT>
-__device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
+template <int D, int NT, int N, int KT, bool LO>
+__device__ __forceinline__ void few_step(Rows<D, NT, LO>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
                                           int g) {
   constexpr int KC = D / 32;
   v4f s[N][KT];
@@ -407,9 +412,11 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
 #pragma unroll
       for (int nt = 0; nt < N; ++nt) {
         const v8bf qh = NT == 1 ? x.qh[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128];
-        const v8bf ql = NT == 1 ? x.ql[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128 + 64];
         s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qh, s[nt][i], 0, 0, 0);
-        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[nt][i], 0, 0, 0);
+        if constexpr (LO) {
+          const v8bf ql = NT == 1 ? x.ql[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128 + 64];
+          s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[nt][i], 0, 0, 0);
+        }
       }
     }
     const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
@@ -466,10 +473,14 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
         float w = pr * vs[e];
         // a scale that is not finite must not reach rows that do not see its token
         if (!whole) w = (seen >> (4 * i + e)) & 1 ? w : 0.0f;
-        __bf16 x0, x1;
-        split_bf16(w, x0, x1);
-        ph[nt][i / 2][4 * (i % 2) + e] = x0;
-        pl[nt][i / 2][4 * (i % 2) + e] = x1;
+        if constexpr (LO) {
+          __bf16 x0, x1;
+          split_bf16(w, x0, x1);
+          ph[nt][i / 2][4 * (i % 2) + e] = x0;
+          pl[nt][i / 2][4 * (i % 2) + e] = x1;
+        } else {
+          ph[nt][i / 2][4 * (i % 2) + e] = static_cast<__bf16>(w);
+        }
       }
     }
   }
@@ -500,7 +511,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
 #pragma unroll
       for (int nt = 0; nt < N; ++nt) {
         x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[nt][u], x.o[nt][e], 0, 0, 0);
-        x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
+        if constexpr (LO) x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
       }
     };
     pv(std::integral_constant<int, 0>{}, ev, 0);
@@ -516,7 +527,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
   }
 }
 
-template <int D, int NT, int KT>
+template <int D, int NT, int KT, bool LO>
 __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
@@ -578,29 +589,25 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
     return there;
   };
 
-  // Steps in flight: two more than the one computed for 16 rows, one for 32
-  // (registers).
-  constexpr int RING = NT == 1 ? 3 : 2;
-  Tile16<D> ring[RING][KT];
-  unsigned there[RING];
-  if (w0 < w1) {
-#pragma unroll
-    for (int i = 0; i + 1 < RING; ++i) there[i] = load(w0 + i < w1 ? w0 + i : w1 - 1, ring[i]);
-  }
+  // One step's loads are in flight while another is computed (two in flight
+  // cost a wave per SIMD for registers: 564k tokens, 131 against 133 us).
+  Tile16<D> ring[2][KT];
+  unsigned there[2];
+  if (w0 < w1) there[0] = load(w0, ring[0]);
 
-  Rows<D, NT> x;
+  Rows<D, NT, LO> x;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
     if constexpr (NT == 1) {
-      load_q<D>(a, p, h, row, lane, x.qh, x.ql);
+      load_q<D, LO>(a, p, h, row, lane, x.qh, x.ql);
     } else if (w == nt) {   // one wave for all four
-      v8bf qh[D / 32], ql[D / 32];
-      load_q<D>(a, p, h, row, lane, qh, ql);
+      v8bf qh[D / 32], ql[LO ? D / 32 : 1];
+      load_q<D, LO>(a, p, h, row, lane, qh, ql);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         sq_all[(nt * (D / 32) + c) * 128 + lane] = qh[c];
-        sq_all[(nt * (D / 32) + c) * 128 + 64 + lane] = ql[c];
+        if constexpr (LO) sq_all[(nt * (D / 32) + c) * 128 + 64 + lane] = ql[c];
       }
     }
     const int pos = first + row / a.G;
@@ -620,14 +627,13 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   // waits for its own loads alone.
   auto run = [&](auto nn) {
     constexpr int N = decltype(nn)::value;
-    for (int b = w0; b < w1; b += RING) {
+    for (int b = w0; b < w1; b += 2) {
 #pragma unroll
-      for (int i = 0; i < RING; ++i) {
+      for (int i = 0; i < 2; ++i) {
         if (b + i >= w1) break;
-        constexpr int ahead = RING - 1;
-        there[(i + ahead) % RING] = load(b + i + ahead < w1 ? b + i + ahead : w1 - 1, ring[(i + ahead) % RING]);
+        there[i ^ 1] = load(b + i + 1 < w1 ? b + i + 1 : w1 - 1, ring[i ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
-        few_step<D, NT, N, KT>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
+        few_step<D, NT, N, KT, LO>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
       }
     }
   };
@@ -1256,7 +1262,9 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   Grid g;
   g.tiles = a.R;   // a request of few rows is one tile
   g.merges = g.tiles < a.target ? g.tiles : a.target;
-  k_few<D, NT, 2><<<dim3(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv)), dim3(256), 0, s>>>(a);
+  const dim3 grid(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv));
+  if (a.is_fp16) k_few<D, NT, 2, true><<<grid, dim3(256), 0, s>>>(a);
+  else k_few<D, NT, 2, false><<<grid, dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, M>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
 }

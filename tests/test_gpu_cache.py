@@ -358,8 +358,9 @@ def _attn_case(ra, Hq, Hkv, D, page, lens, qs, dt="bf16", out=None, rope=False, 
 
 
 def _operand(dt, rows):
-    """Half a step of the matrix products' operands Q and P."""
-    return 2.0 ** -16 if rows <= 32 else HALF[dt]
+    """Half a step of the matrix products' operands Q and P: rounded once to the input type; requests of few rows in
+    binary16 take two bf16 values for each (8 bits and the 8 below them)."""
+    return 2.0 ** -16 if rows <= 32 and dt == "fp16" else HALF[dt]
 
 
 def _check_attn(o, lse, want, want_lse, size_v, size_s, dt, out, n, rows):
