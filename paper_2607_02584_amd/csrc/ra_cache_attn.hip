@@ -300,6 +300,17 @@ __device__ __forceinline__ void settle(V& x) {
 #endif
 }
 
+// Keeps what is computed from x behind this place (the compiler otherwise moves
+// it up to where x is loaded, and waits there).
+template <typename V>
+__device__ __forceinline__ void pin(V& x) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+v"(x));
+#else
+  (void)x;
+#endif
+}
+
 template <int B>
 __device__ __forceinline__ v2bf codes2(uint32_t w) { return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, B); }
 
@@ -787,6 +798,11 @@ __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p,
   }
 }
 
+// The lowest n bits (n below 0: none, above 64: all).
+__device__ __forceinline__ unsigned long long bits_below(int n) {
+  return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1;
+}
+
 // f(0) .. f(N - 1), each index a compile-time constant
 template <typename F, int... I>
 __device__ __forceinline__ void each_(F&& f, std::integer_sequence<int, I...>) {
@@ -902,61 +918,69 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     entries(bk + 1, cv + 1);
   };
   float ref_s = 0.0f;   // last wave: power of two of the largest V scale so far
-  auto put_k = [&](int b) {   // the staged K into LDS
-    if (b >= b1) return;
-    const int part = lane >> 4, key = mine + (lane & 15);
-#pragma unroll
-    for (int c = 0; c < D / 32; ++c) {
+  // The staged codes into LDS, in four parts each.  What is written past the
+  // last tile replaces tiles that are done with.
+  auto put_k = [&](int b, auto part) {
+    constexpr int c = decltype(part)::value;
+    if constexpr (c < D / 32) {
       const uint32_t x = dword_of<D>(sk, c);
-      buf.k[b & 1][part * (D / 32) + c][key] = make_uint4(H::template codes<0>(x), H::template codes<1>(x),
-                                                          H::template codes<2>(x), H::template codes<3>(x));
+      buf.k[b & 1][(lane >> 4) * (D / 32) + c][mine + (lane & 15)] =
+          make_uint4(H::template codes<0>(x), H::template codes<1>(x), H::template codes<2>(x), H::template codes<3>(x));
     }
   };
-  auto put_v = [&](int b) {
-    if (b >= b1) return;
-    const int half = (lane >> 4) & 1, i = lane & 15;
-    uint2* dst = reinterpret_cast<uint2*>(&buf.v[b & 1][w * 2 + hh][i]) + half;   // position e * 16 + i
+  auto put_v = [&](int b, auto part) {   // channels E / 4 * part .. of the lane's chunk
+    constexpr int c = decltype(part)::value;
+    // position e * 16 + chunk, half of an octet
+    uint2* dst = reinterpret_cast<uint2*>(&buf.v[b & 1][w * 2 + hh][lane & 15]) + ((lane >> 4) & 1);
     if constexpr (D == 128) {
       const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
                      o23 = odd_of(sv.z, sv.w);
-      dst[0 * 32] = make_uint2(H::template codes<0>(e01), H::template codes<0>(e23));
-      dst[1 * 32] = make_uint2(H::template codes<0>(o01), H::template codes<0>(o23));
-      dst[2 * 32] = make_uint2(H::template codes<1>(e01), H::template codes<1>(e23));
-      dst[3 * 32] = make_uint2(H::template codes<1>(o01), H::template codes<1>(o23));
-      dst[4 * 32] = make_uint2(H::template codes<2>(e01), H::template codes<2>(e23));
-      dst[5 * 32] = make_uint2(H::template codes<2>(o01), H::template codes<2>(o23));
-      dst[6 * 32] = make_uint2(H::template codes<3>(e01), H::template codes<3>(e23));
-      dst[7 * 32] = make_uint2(H::template codes<3>(o01), H::template codes<3>(o23));
+      dst[2 * c * 32] = make_uint2(H::template codes<c>(e01), H::template codes<c>(e23));
+      dst[(2 * c + 1) * 32] = make_uint2(H::template codes<c>(o01), H::template codes<c>(o23));
     } else {
       const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
-      const uint32_t ev = even_of(t02, t13), od = odd_of(t02, t13);
-      dst[0 * 32] = make_uint2(H::template codes<0>(ev), H::template codes<2>(ev));
-      dst[1 * 32] = make_uint2(H::template codes<0>(od), H::template codes<2>(od));
-      dst[2 * 32] = make_uint2(H::template codes<1>(ev), H::template codes<3>(ev));
-      dst[3 * 32] = make_uint2(H::template codes<1>(od), H::template codes<3>(od));
+      const uint32_t n = c % 2 ? odd_of(t02, t13) : even_of(t02, t13);
+      dst[c * 32] = make_uint2(H::template codes<c / 2>(n), H::template codes<c / 2 + 2>(n));
     }
-    if (do_s) {
-      Scales& t = buf.sc[b & 1];
-      // a token whose scale is not finite acts through its score alone, so that
-      // it reaches the rows that see it and no others
-      const bool odd = here && !(vs < __builtin_inff());
-      const float k0 = here ? (odd ? vs : ks) : 0.0f;
-      const float v0 = here && !odd ? vs : 0.0f;
-      if constexpr (F16) {
-        float mx = v0;
+  };
+  auto put_scales = [&](int b) {
+    if (!do_s) return;
+    Scales& t = buf.sc[b & 1];
+    // a token whose scale is not finite acts through its score alone, so that
+    // it reaches the rows that see it and no others
+    const bool odd = here && !(vs < __builtin_inff());
+    const float k0 = here ? (odd ? vs : ks) : 0.0f;
+    const float v0 = here && !odd ? vs : 0.0f;
+    if constexpr (F16) {
+      float mx = v0;
 #pragma unroll
-        for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-        mx = __uint_as_float(__float_as_uint(mx) & 0x7f800000u);
-        ref_s = fmaxf(fmaxf(ref_s, mx), 0x1p-120f);
-        t.vs[lane] = v0 * (1.0f / ref_s);
-        if (lane == 0) t.ref = ref_s;
-      } else {
-        t.vs[lane] = v0;
-      }
-      t.ks[lane] = k0;
-      const unsigned long long all = __ballot(here);
-      if (lane == 0) t.there = all;
+      for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
+      mx = __uint_as_float(__float_as_uint(mx) & 0x7f800000u);
+      ref_s = fmaxf(fmaxf(ref_s, mx), 0x1p-120f);
+      t.vs[lane] = v0 * (1.0f / ref_s);
+      if (lane == 0) t.ref = ref_s;
+    } else {
+      t.vs[lane] = v0;
     }
+    t.ks[lane] = k0;
+    const unsigned long long all = __ballot(here);
+    if (lane == 0) t.there = all;
+  };
+  auto pin_staged = [&] {
+    if constexpr (D == 128) {
+      pin(sk.x), pin(sk.y), pin(sk.z), pin(sk.w);
+      pin(sv.x), pin(sv.y), pin(sv.z), pin(sv.w);
+    } else {
+      pin(sk.x), pin(sk.y);
+      pin(sv.x), pin(sv.y);
+    }
+  };
+  auto put = [&](int bk, int bv) {
+    pin_staged();
+    each<4>([&](auto part) {
+      put_k(bk, part);
+      put_v(bv, part);
+    });
   };
 
   if (b0 < b1) {
@@ -971,11 +995,13 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
   float m = kNegInf, l = 0.0f, unit = 0x1p-120f;
-  put_k(b0);
-  put_v(b0);
-  if (b0 < b1) ask(b0 + 1, b0 + 1);   // (this V is asked for again with the first tile)
-  put_k(b0 + 1);
-  if (b0 < b1) entries(b0 + 2, b0 + 1);
+  put(b0, b0);
+  put_scales(b0);
+  if (b0 < b1) {
+    ask(b0 + 1, b0 + 1);   // (this V is asked for again with the first tile)
+    each<4>([&](auto part) { put_k(b0 + 1, part); });
+    entries(b0 + 2, b0 + 1);
+  }
   __syncthreads();
 
   auto k_op = [&](int b, int c, int kc) { return __builtin_bit_cast(vec, buf.k[b & 1][hh * KC + kc][c * 32 + j]); };
@@ -1010,14 +1036,14 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     }
     const unsigned long long there = t.there;
     if (key0 < all_lo || key0 + kBlock > all_hi || there != ~0ull) {
+      // the lane's keys of the tile, its own first: bit 32 c + 8 (r / 4) + r % 4
+      const unsigned long long on = (there & bits_below(row_hi - key0) & ~bits_below(row_lo - key0)) >> (4 * hh);
+      const unsigned half[2] = {static_cast<unsigned>(on), static_cast<unsigned>(on >> 32)};
 #pragma unroll
       for (int c = 0; c < 2; ++c)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int at = c * 32 + 8 * (r >> 2) + 4 * hh + (r & 3);
-          const bool on = ((there >> at) & 1) && key0 + at < row_hi && key0 + at >= row_lo;
-          x[c][r] = on ? x[c][r] : kNegInf;
-        }
+        for (int r = 0; r < 16; ++r)
+          x[c][r] = half[c] & (1u << (8 * (r >> 2) + (r & 3))) ? x[c][r] : kNegInf;
     }
 #pragma unroll
     for (int c = 0; c < 2; ++c)
@@ -1097,11 +1123,22 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
-        // chunk 1's probabilities beside chunk 0's products
-        if constexpr (c == 0 && i % (NP / 4) == NP / 4 - 1) probs(1, i / (NP / 4));
+        // beside chunk 0's products chunk 1's probabilities, beside chunk 1's
+        // the next tiles' codes
+        if constexpr (i % (NP / 4) == NP / 4 - 1) {
+          if constexpr (c == 0) {
+            probs(1, i / (NP / 4));
+          } else {
+            put_k(b + 2, std::integral_constant<int, i / (NP / 4)>{});
+            put_v(b + 1, std::integral_constant<int, i / (NP / 4)>{});
+          }
+        }
         __builtin_amdgcn_sched_barrier(0);
       });
-      if constexpr (c == 0) __builtin_amdgcn_s_setprio(0);
+      if constexpr (c == 0) {
+        __builtin_amdgcn_s_setprio(0);
+        pin_staged();
+      }
     });
     l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
   };
@@ -1109,8 +1146,8 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   for (int b = b0; b < b1; ++b) {
     ask(b + 2, b + 1);
     if (b < t1) step(b);
-    put_v(b + 1);
-    put_k(b + 2);
+    else put(b + 2, b + 1);
+    put_scales(b + 1);
     __syncthreads();
   }
 #pragma unroll
