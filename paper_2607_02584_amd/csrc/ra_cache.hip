@@ -265,9 +265,11 @@ __global__ __launch_bounds__(kPlanThreads) void k_place(PlanArgs a) {
 // rounded in binary32 can fall on either side: such a quotient is off by less
 // than 2^-21 and another one is at least 2^-13 away from the border, so it is
 // first rounded to multiples of 2^-16, which puts it back on it.  Turned
-// values meet borders only by chance: where |y| +- 2^-16 rounds to two codes
-// (the binary32 sums are off by less than 2^-18 in practice) the wave does the
-// row again in binary64.
+// values meet borders only by chance: where 6y / a +- 2^-18 rounds to two codes
+// the wave does the row again in binary64 (1 in 100 waves).  The roundings of
+// the seven stages leave 6y / a off by about 2^-22 (rms; they are of random
+// sign, each at most 2^-24 of a partial sum), a sixteenth of that margin.
+constexpr float kNear = 0x1p-18f;
 
 template <typename F, int D, bool ROPE, bool HAD>
 __device__ __forceinline__ void turn(const float (&x)[8], const float (&cs)[8], F (&y)[8], int lane) {
@@ -319,10 +321,18 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
   float y[8];
   turn<float, D, ROPE, HAD>(x, cs, y, lane);
   uint32_t m = 0;
+  if constexpr (HAD) {
+    // (one element that is not finite leaves none that is)
+    float f = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const uint32_t b = __float_as_uint(y[i]) & 0x7fffffffu;   // as integers NaN and infinity are the largest
-    m = b > m ? b : m;
+    for (int i = 0; i < 8; i += 2) f = fmaxf(fmaxf(f, fabsf(y[i])), fabsf(y[i + 1]));
+    m = y[0] == y[0] ? __float_as_uint(f) : 0x7fc00000u;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t b = __float_as_uint(y[i]) & 0x7fffffffu;   // as integers NaN and infinity are the largest
+      m = b > m ? b : m;
+    }
   }
   m = row_max_bits<D>(m);
   // a row of zeros (or below 2^-100) keeps scale 0; one that is not finite
@@ -336,17 +346,18 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
   float lo[8], hi[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float t = dead ? 0.0f : y[i] * inv, u = fabsf(t);
+    const float t = y[i] * inv;
     if constexpr (ROPE || HAD) {
-      hi[i] = copysignf(u + 0x1p-16f, t);
-      lo[i] = copysignf(fmaxf(u - 0x1p-16f, 0.0f), t);
+      const float by = copysignf(kNear, t);
+      hi[i] = t + by;
+      lo[i] = t - by;
     } else {
-      lo[i] = copysignf((u + 192.0f) - 192.0f, t);   // multiples of 2^-16
+      lo[i] = copysignf((fabsf(t) + 192.0f) - 192.0f, t);   // multiples of 2^-16
     }
   }
-  uint32_t code = pack_fp4(lo);
+  uint32_t code = dead ? 0u : pack_fp4(lo);
   if constexpr (ROPE || HAD) {
-    if (__any(code != pack_fp4(hi))) {
+    if (__any(!dead && code != pack_fp4(hi))) {
       double z[8];
       turn<double, D, ROPE, HAD>(x, cs, z, lane);
       double zm = 0.0;
@@ -366,7 +377,7 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
                         (u > 5.0 ? 2.0f : 0.0f);
         fix[i] = t < 0.0 ? -q : q;
       }
-      code = pack_fp4(fix);
+      code = dead ? 0u : pack_fp4(fix);
     }
   }
   return code;
