@@ -22,6 +22,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace ra {
 
 struct CacheGeom {
@@ -98,13 +100,14 @@ size_t cache_attn_partial_bytes(int D, int Hkv, int G, int max_q, size_t* ml_off
 int set_error(int code, const char* msg) noexcept;
 
 // ---- lanes ----
-// The value of lane ^ M, M = 1, 2, 4 or 8 (register moves inside a row of 16).
+// The value of lane ^ M (M = 1, 2, 7, 8: one register move inside a row of 16, 4: two).
 template <int M>
 __device__ __forceinline__ int lane_xor(int v) {
   if constexpr (M == 1) return __builtin_amdgcn_mov_dpp(v, 0xB1, 0xF, 0xF, true);    // quad_perm 1,0,3,2
   if constexpr (M == 2) return __builtin_amdgcn_mov_dpp(v, 0x4E, 0xF, 0xF, true);    // quad_perm 2,3,0,1
   if constexpr (M == 4)                                                              // half mirror (^7), then ^3
     return __builtin_amdgcn_mov_dpp(__builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true), 0x1B, 0xF, 0xF, true);
+  if constexpr (M == 7) return __builtin_amdgcn_mov_dpp(v, 0x141, 0xF, 0xF, true);   // half mirror
   if constexpr (M == 8) return __builtin_amdgcn_mov_dpp(v, 0x128, 0xF, 0xF, true);   // row_ror:8
   if constexpr (M == 16) {
     const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
@@ -146,6 +149,68 @@ __device__ __forceinline__ void butterfly_regs(F (&y)[N]) {
         y[i] = a + b;
         y[i + h] = a - b;
       }
+}
+
+// ---- rows of D channels, 8 per lane ----
+//
+// D / 8 lanes hold a row.  Lane l holds channels 8 b .., b = row_block(l): with
+// this order the three low lane stages of the Hadamard transform exchange with
+// lanes ^ 1, ^ 2 and ^ 7, each one register move (^ 4 would take two).
+__device__ __forceinline__ int row_block(int lane) { return lane ^ ((lane & 4) ? 3 : 0); }
+
+// y + s * (y of the partner lane), a stage of eight values: one multiply-add
+// each that takes its factor through the move (the compiler makes two
+// operations of it).  Values written just before need two wait states ahead of
+// such a move.
+#if defined(__HIP_DEVICE_COMPILE__)
+#define RA_STAGE8(move)                                                                                            \
+  asm volatile("s_nop 1\n\t"                                                                                       \
+               "v_fmac_f32_dpp %0, %0, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %1, %1, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %2, %2, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %3, %3, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %4, %4, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %5, %5, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %6, %6, %8 " move " row_mask:0xf bank_mask:0xf\n\t"                                 \
+               "v_fmac_f32_dpp %7, %7, %8 " move " row_mask:0xf bank_mask:0xf"                                      \
+               : "+v"(y[0]), "+v"(y[1]), "+v"(y[2]), "+v"(y[3]), "+v"(y[4]), "+v"(y[5]), "+v"(y[6]), "+v"(y[7])     \
+               : "v"(s))
+#else
+#define RA_STAGE8(move) (void)s
+#endif
+template <int M>
+__device__ __forceinline__ void stage8(float (&y)[8], bool up) {
+  const float s = up ? -1.0f : 1.0f;
+  if constexpr (M == 1) RA_STAGE8("quad_perm:[1,0,3,2]");
+  if constexpr (M == 2) RA_STAGE8("quad_perm:[2,3,0,1]");
+  if constexpr (M == 7) RA_STAGE8("row_half_mirror");
+  if constexpr (M == 8) RA_STAGE8("row_ror:8");
+}
+
+// Times the Sylvester-Hadamard matrix of +-1, and times row_sign(b): a stage is
+// y + s o with s = -1 in lanes whose bit is set, where o - y is meant, a sign
+// that all later partners share.
+template <int D>
+__device__ __forceinline__ void hadamard_row(float (&y)[8], int b) {
+  butterfly_regs(y);
+  stage8<1>(y, b & 1);
+  stage8<2>(y, b & 2);
+  stage8<7>(y, b & 4);
+  if constexpr (D == 128) stage8<8>(y, b & 8);
+}
+__device__ __forceinline__ float row_sign(int b) { return __builtin_popcount(b) & 1 ? -1.0f : 1.0f; }
+// The same in binary64, without the sign.
+template <int D>
+__device__ __forceinline__ void hadamard_row(double (&y)[8], int b) {
+  butterfly_regs(y);
+  auto stage = [&](auto mm, bool up) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = lane_xor<decltype(mm)::value>(y[i]) + (up ? -y[i] : y[i]);
+  };
+  stage(std::integral_constant<int, 1>{}, b & 1);
+  stage(std::integral_constant<int, 2>{}, b & 2);
+  stage(std::integral_constant<int, 7>{}, b & 4);
+  if constexpr (D == 128) stage(std::integral_constant<int, 8>{}, b & 8);
 }
 
 // ---- 16-bit values ----

@@ -271,6 +271,7 @@ __global__ __launch_bounds__(kPlanThreads) void k_place(PlanArgs a) {
 // sign, each at most 2^-24 of a partial sum), a sixteenth of that margin.
 constexpr float kNear = 0x1p-18f;
 
+// (lane: the lane's block of channels; a rotated row in binary32 comes times row_sign(lane))
 template <typename F, int D, bool ROPE, bool HAD>
 __device__ __forceinline__ void turn(const float (&x)[8], const float (&cs)[8], F (&y)[8], int lane) {
 #pragma unroll
@@ -285,13 +286,7 @@ __device__ __forceinline__ void turn(const float (&x)[8], const float (&cs)[8], 
       y[2 * i + 1] = b;
     }
   }
-  if constexpr (HAD) {
-    butterfly_regs(y);
-    butterfly_lanes<1>(y, lane);
-    butterfly_lanes<2>(y, lane);
-    butterfly_lanes<4>(y, lane);
-    if constexpr (D == 128) butterfly_lanes<8>(y, lane);
-  }
+  if constexpr (HAD) hadamard_row<D>(y, lane);
 }
 
 template <int B>
@@ -310,7 +305,7 @@ __device__ __forceinline__ uint32_t row_max_bits(uint32_t m) {
   auto take = [&](int o) { m = static_cast<uint32_t>(o) > m ? static_cast<uint32_t>(o) : m; };
   take(lane_xor<1>(static_cast<int>(m)));
   take(lane_xor<2>(static_cast<int>(m)));
-  take(lane_xor<4>(static_cast<int>(m)));
+  take(lane_xor<7>(static_cast<int>(m)));
   if constexpr (D == 128) take(lane_xor<8>(static_cast<int>(m)));
   return m;
 }
@@ -342,7 +337,7 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
   constexpr float norm = HAD ? (D == 128 ? 0.0883883476483184405501055452631f : 0.125f) : 1.0f;
   *scale = !finite ? __uint_as_float(0x7fc00000u) : tiny ? 0.0f : a / 6.0f * norm;
   const bool dead = !finite || tiny;
-  const float inv = dead ? 0.0f : 6.0f / a;
+  const float inv = dead ? 0.0f : HAD ? 6.0f * row_sign(lane) / a : 6.0f / a;
   float lo[8], hi[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
@@ -365,7 +360,7 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
       for (int i = 0; i < 8; ++i) zm = fmax(zm, fabs(z[i]));
       zm = fmax(zm, lane_xor<1>(zm));
       zm = fmax(zm, lane_xor<2>(zm));
-      zm = fmax(zm, lane_xor<4>(zm));
+      zm = fmax(zm, lane_xor<7>(zm));
       if constexpr (D == 128) zm = fmax(zm, lane_xor<8>(zm));
       // the code is 2 |t| rounded by its own step; borders and ties as above
       float fix[8];
@@ -398,7 +393,7 @@ __device__ __forceinline__ void unpack16(const uint4& w, int is_fp16, float (&x)
 template <int D, bool ROPE, bool HADK, bool HADV>
 __global__ __launch_bounds__(256) void k_append(AppendArgs a) {
   constexpr int L = D / 8;
-  const int lane = threadIdx.x & (L - 1);
+  const int lane = row_block(threadIdx.x & (L - 1));   // block of channels
   const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
   const int slot = t < a.T ? a.slots[t] : -1;
   float cs[8] = {};
@@ -469,12 +464,8 @@ __device__ __forceinline__ void values(uint32_t code, float scale, int lane, flo
   y[4] = p2[0], y[5] = p2[1], y[6] = p3[0], y[7] = p3[1];
   if constexpr (HAD) {
     // sums of multiples of 1/2 up to 6 D: exact
-    butterfly_regs(y);
-    butterfly_lanes<1>(y, lane);
-    butterfly_lanes<2>(y, lane);
-    butterfly_lanes<4>(y, lane);
-    if constexpr (D == 128) butterfly_lanes<8>(y, lane);
-    scale *= D == 128 ? 0.0883883476483184405501055452631f : 0.125f;
+    hadamard_row<D>(y, lane);
+    scale *= row_sign(lane) * (D == 128 ? 0.0883883476483184405501055452631f : 0.125f);
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) y[i] *= scale;
@@ -495,7 +486,7 @@ __device__ __forceinline__ void store8(void* base, int64_t at, const float (&y)[
 template <int D, bool HADK, bool HADV>
 __global__ __launch_bounds__(256) void k_read(ReadArgs a) {
   constexpr int L = D / 8;
-  const int lane = threadIdx.x & (L - 1);
+  const int lane = row_block(threadIdx.x & (L - 1));   // block of channels
   const int t = blockIdx.x * (256 / L) + threadIdx.x / L;
   const int slot = t < a.T ? a.slots[t] : -1;
   const bool ok = slot >= 0 && (slot >> a.g.page_log) < a.g.num_pages;
