@@ -261,12 +261,14 @@ __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf
 // load by exchanging nibbles of neighbouring tokens (two operations for eight
 // codes) before the conversion.
 //
-// Q (scaled) and P * (V's scale) are rounded once to bf16, the input type's
-// half step; for binary16 inputs (LO) each is the sum of two bf16 values, 16
-// bits over the whole range of the scales.
+// Q (scaled) is the sum of two bf16 values, 16 bits: the scores, and lse, are
+// then as exact as binary32 sums.  P * (V's scale) is rounded once to bf16
+// where both inputs and outputs are bf16 (the output's own rounding is as
+// large); else (LO) it is two bf16 values too, over the whole range of the
+// scales.
 //
 // Bound by HBM, (D + 8) bytes per token and KV head, with the vector units
-// close behind: 212 operations per step, 80 of them conversions of codes.  The
+// close behind: about 210 operations per step, 80 of them conversions of codes.  The
 // four waves of a workgroup are joined through LDS, the parts of a split tile
 // by k_merge.
 
@@ -332,9 +334,9 @@ __device__ __forceinline__ void split_bf16(float x, __bf16& hi, __bf16& lo) {
 
 // The rows' Q as the second operand of K Q^T: lane = 16 * part + row, its
 // D / 4 channels from part * D / 4 on, after RoPE and rotation.
-template <int D, bool LO>
+template <int D>
 __device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
-                                       v8bf (&hi)[D / 32], v8bf (&lo)[LO ? D / 32 : 1]) {
+                                       v8bf (&hi)[D / 32], v8bf (&lo)[D / 32]) {
   constexpr int N = D / 4;
   const int part = lane >> 4;
   const bool ok = row < p.q.ql * a.G;
@@ -376,7 +378,7 @@ __device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, i
       __bf16 x0, x1;
       split_bf16(y[8 * c + e] * a.c, x0, x1);   // scores come out in base 2
       hi[c][e] = x0;
-      if constexpr (LO) lo[c][e] = x1;
+      lo[c][e] = x1;
     }
 }
 
@@ -391,11 +393,10 @@ __device__ __forceinline__ uint32_t dword_of(const typename std::conditional<D =
 // x = s * (K's scale) - ref is one operation, and most tiles rescale nothing.
 constexpr float kSlack = 8.0f;
 
-// The rows' state in a wave: reference and sum, O^T, and Q -- in registers
-// for 16 rows, for 32 in LDS (two waves then fit a SIMD).
-template <int D, int NT, bool LO>
+// The rows' state in a wave: O^T, reference and sum.  (Q is in LDS, read again
+// in every step: in registers it cost a wave per SIMD.)
+template <int D, int NT>
 struct Rows {
-  v8bf qh[NT == 1 ? D / 32 : 1], ql[NT == 1 && LO ? D / 32 : 1];
   v4f o[NT][D / 16];
   float m[NT], l[NT];
   int hi[NT], lo[NT];   // keys that the lane's row sees: [lo, hi)
@@ -409,7 +410,7 @@ struct Rows {
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
 template <int D, int NT, int N, int KT, bool LO>
-__device__ __forceinline__ void few_step(Rows<D, NT, LO>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
+__device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
                                           int g) {
   constexpr int KC = D / 32;
   v4f s[N][KT];
@@ -422,12 +423,8 @@ __device__ __forceinline__ void few_step(Rows<D, NT, LO>& x, const v8bf* sq, con
       const v8bf k = codes8(dword_of<D>(t[i].k, c));
 #pragma unroll
       for (int nt = 0; nt < N; ++nt) {
-        const v8bf qh = NT == 1 ? x.qh[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128];
-        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, qh, s[nt][i], 0, 0, 0);
-        if constexpr (LO) {
-          const v8bf ql = NT == 1 ? x.ql[c % (NT == 1 ? D / 32 : 1)] : sq[(nt * (D / 32) + c) * 128 + 64];
-          s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, ql, s[nt][i], 0, 0, 0);
-        }
+        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, sq[(nt * KC + c) * 128], s[nt][i], 0, 0, 0);
+        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, sq[(nt * KC + c) * 128 + 64], s[nt][i], 0, 0, 0);
       }
     }
     const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
@@ -545,7 +542,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   __shared__ __align__(16) float so[4][16][kStride];
   __shared__ float sm[4][M], sl[4][M];
   __shared__ SchedShared sched;
-  __shared__ __align__(16) v8bf sq_all[NT == 1 ? 1 : NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
+  __shared__ __align__(16) v8bf sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
   // heads fastest: the heads of a page, neighbours in memory, are read together
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
@@ -606,19 +603,17 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   unsigned there[2];
   if (w0 < w1) there[0] = load(w0, ring[0]);
 
-  Rows<D, NT, LO> x;
+  Rows<D, NT> x;
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
-    if constexpr (NT == 1) {
-      load_q<D, LO>(a, p, h, row, lane, x.qh, x.ql);
-    } else if (w == nt) {   // one wave for all four
-      v8bf qh[D / 32], ql[LO ? D / 32 : 1];
-      load_q<D, LO>(a, p, h, row, lane, qh, ql);
+    if (w == nt) {   // one wave for all four
+      v8bf qh[D / 32], ql[D / 32];
+      load_q<D>(a, p, h, row, lane, qh, ql);
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         sq_all[(nt * (D / 32) + c) * 128 + lane] = qh[c];
-        if constexpr (LO) sq_all[(nt * (D / 32) + c) * 128 + 64 + lane] = ql[c];
+        sq_all[(nt * (D / 32) + c) * 128 + 64 + lane] = ql[c];
       }
     }
     const int pos = first + row / a.G;
@@ -630,7 +625,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 #pragma unroll
     for (int e = 0; e < E; ++e) x.o[nt][e] = v4f{0, 0, 0, 0};
   }
-  if constexpr (NT > 1) __syncthreads();
+  __syncthreads();
   auto whole = [&](int b, unsigned there) {
     return b * kStep >= all_lo && b * kStep + kStep <= all_hi && b * kStep + kStep <= p.q.n && there == (1u << KT) - 1;
   };
@@ -714,11 +709,12 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // c), which rounded to 16 bits are the second operand of the next product, and
 // the same query's output, so that rescaling it is a factor per lane.
 //
-// Q (after RoPE, rotation and scale, in binary32) is rounded once to the input
-// type, P * (V's scale) once to it: 2^-8 and 2^-11 relative, the type's own
-// half step, as everything the model feeds in.  In binary16 the V scales are
-// taken relative to the power of two of the largest so far (O is in units of
-// it), so that P * scale neither overflows nor loses small values.
+// Q (after RoPE, rotation and scale, in binary32) is the sum of two values of
+// the input type, so that scores and lse are as exact as binary32 sums; P *
+// (V's scale) is one, 2^-8 or 2^-11 relative, and two (LO) where the output is
+// finer than the input type.  In binary16 the V scales are taken relative to
+// the power of two of the largest so far (O is in units of it), so that P *
+// scale neither overflows nor loses small values.
 //
 // LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
 // bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
@@ -753,7 +749,7 @@ struct Half16<true> {
 
 template <int D, bool F16>
 __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
-                                         typename Half16<F16>::vec (&out)[D / 16]) {
+                                         typename Half16<F16>::vec (&hi)[D / 16], typename Half16<F16>::vec (&lo)[D / 16]) {
   constexpr int N = D / 2;
   const int hh = lane >> 5;
   const bool ok = row < p.q.ql * a.G;
@@ -789,12 +785,17 @@ __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p,
   }
 #pragma unroll
   for (int c = 0; c < N / 8; ++c) {
-    uint4 w;
-    w.x = pack16(y[8 * c] * a.c, y[8 * c + 1] * a.c, F16);
-    w.y = pack16(y[8 * c + 2] * a.c, y[8 * c + 3] * a.c, F16);
-    w.z = pack16(y[8 * c + 4] * a.c, y[8 * c + 5] * a.c, F16);
-    w.w = pack16(y[8 * c + 6] * a.c, y[8 * c + 7] * a.c, F16);
-    out[c] = __builtin_bit_cast(typename Half16<F16>::vec, w);
+    uint32_t x[4], r[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float u = y[8 * c + 2 * e] * a.c, v = y[8 * c + 2 * e + 1] * a.c;   // scores come out in base 2
+      x[e] = pack16(u, v, F16);
+      pin(x[e]);   // what is left over is taken from these bits: another conversion may round a tie the other way
+      r[e] = pack16(u - cache_h2f(static_cast<uint16_t>(x[e] & 0xffff), F16),
+                    v - cache_h2f(static_cast<uint16_t>(x[e] >> 16), F16), F16);
+    }
+    hi[c] = __builtin_bit_cast(typename Half16<F16>::vec, make_uint4(x[0], x[1], x[2], x[3]));
+    lo[c] = __builtin_bit_cast(typename Half16<F16>::vec, make_uint4(r[0], r[1], r[2], r[3]));
   }
 }
 
@@ -819,7 +820,7 @@ __device__ __forceinline__ void each(F&& f) {
 // matrix cores beside the next chunk's probabilities, their LDS operands read
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
-template <int D, bool F16>
+template <int D, bool F16, bool LO>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   typedef Half16<F16> H;
   typedef typename H::vec vec;
@@ -987,8 +988,8 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     entries(b0, b0);
     ask(b0, b0);
   }
-  vec q[KC];
-  load_q32<D, F16>(a, p, h, row, lane, q);
+  vec q[KC], q_lo[KC];
+  load_q32<D, F16>(a, p, h, row, lane, q, q_lo);
   v16f o[MT], s[2];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -1010,7 +1011,10 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) s[c] = H::mfma(k_op(b0, c, kc), q[kc], s[c]);
+    for (int kc = 0; kc < KC; ++kc) {
+      s[c] = H::mfma(k_op(b0, c, kc), q[kc], s[c]);
+      s[c] = H::mfma(k_op(b0, c, kc), q_lo[kc], s[c]);
+    }
     settle(s[c]);
   }
   __syncthreads();   // tile b0's K is read before tile b0 + 2's takes its place
@@ -1074,7 +1078,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
     }
 
-    uint32_t pw[2][8];
+    uint32_t pw[2][8], pl[2][LO ? 8 : 1];
     float ls[4] = {0, 0, 0, 0};
     auto v_scales = [&](int n) { return *reinterpret_cast<const float4*>(&t.vs[8 * n + 4 * hh]); };
     float4 v4 = v_scales(0);   // read a group ahead
@@ -1088,8 +1092,15 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         ls[e] += pr;
         y[e] = pr * vv[e];
       }
-      pw[c][2 * r4] = pack16(y[0], y[1], F16);
-      pw[c][2 * r4 + 1] = pack16(y[2], y[3], F16);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        uint32_t u = pack16(y[2 * e], y[2 * e + 1], F16);
+        if constexpr (LO) pin(u);   // as in load_q32
+        pw[c][2 * r4 + e] = u;
+        if constexpr (LO)
+          pl[c][2 * r4 + e] = pack16(y[2 * e] - cache_h2f(static_cast<uint16_t>(u & 0xffff), F16),
+                                     y[2 * e + 1] - cache_h2f(static_cast<uint16_t>(u >> 16), F16), F16);
+      }
     };
     // products of chunk c: 2 MT of P V (step i / MT, tile i % MT), then the KC
     // score products of chunk c of the next tile (behind the last tile they
@@ -1115,11 +1126,15 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
           constexpr int st = i / MT;
           o[i % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pw[c][4 * st], pw[c][4 * st + 1], pw[c][4 * st + 2],
                                                                      pw[c][4 * st + 3])), o[i % MT]);
+          if constexpr (LO)
+            o[i % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pl[c][4 * st], pl[c][4 * st + 1], pl[c][4 * st + 2],
+                                                                       pl[c][4 * st + 3])), o[i % MT]);
         } else {
           if constexpr (i == 2 * MT)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
           s[c] = H::mfma(op, q[i - 2 * MT], s[c]);
+          s[c] = H::mfma(op, q_lo[i - 2 * MT], s[c]);
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
@@ -1300,16 +1315,16 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   g.tiles = a.R;   // a request of few rows is one tile
   g.merges = g.tiles < a.target ? g.tiles : a.target;
   const dim3 grid(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv));
-  if (a.is_fp16) k_few<D, NT, 2, true><<<grid, dim3(256), 0, s>>>(a);
+  if (a.is_fp16 || a.out_dtype != RA_BF16) k_few<D, NT, 2, true><<<grid, dim3(256), 0, s>>>(a);
   else k_few<D, NT, 2, false><<<grid, dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, M>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
 }
 
-template <int D, bool F16>
+template <int D, bool F16, bool LO>
 hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
   const Grid g = grid_of(a, kRowTile, a.target_rows);
-  k_rows<D, F16><<<dim3(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv)), dim3(256), 0, s>>>(a);
+  k_rows<D, F16, LO><<<dim3(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv)), dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, kRowTile>(a, g, a.target_rows, static_cast<int64_t>(a.max_q) * a.G, s);
 }
@@ -1321,7 +1336,10 @@ hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.G <= kFewRows) e = few<D, 2>(a, s);   // requests of few rows; with more heads than that there are none
   if (e != hipSuccess || most <= kFewRows) return e;
-  return a.is_fp16 ? rows<D, true>(a, s) : rows<D, false>(a, s);
+  // P in one value of the input type where the output is no finer than that
+  const bool lo = a.out_dtype == RA_FP32 || (!a.is_fp16 && a.out_dtype == RA_FP16);
+  if (a.is_fp16) return lo ? rows<D, true, true>(a, s) : rows<D, true, false>(a, s);
+  return lo ? rows<D, false, true>(a, s) : rows<D, false, false>(a, s);
 }
 
 int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }
