@@ -1102,14 +1102,16 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
                                      y[2 * e + 1] - cache_h2f(static_cast<uint16_t>(u >> 16), F16), F16);
       }
     };
-    // products of chunk c: 2 MT of P V (step i / MT, tile i % MT), then the KC
-    // score products of chunk c of the next tile (behind the last tile they
-    // take what lies there and nothing reads them: a second form of this code
-    // costs more than they do)
+    // products of chunk c, in turn: one of the 2 MT of P V (step n / MT, tile n %
+    // MT), one of the KC score products of chunk c of the next tile, whose sum
+    // is one chain (behind the last tile they take what lies there and nothing
+    // reads them: a second form of this code costs more than they do)
+    static_assert(2 * MT == KC, "as many of either");
     constexpr int NP = 2 * MT + KC, kAhead = 4;
     auto operand = [&](int c, int i) {
-      if (i < 2 * MT) return __builtin_bit_cast(vec, buf.v[b & 1][(c * 2 + i / MT) * 2 + hh][(i % MT) * 32 + j]);
-      return k_op(b + 1, c, i - 2 * MT);
+      const int n = i / 2;
+      if (i % 2 == 0) return __builtin_bit_cast(vec, buf.v[b & 1][(c * 2 + n / MT) * 2 + hh][(n % MT) * 32 + j]);
+      return k_op(b + 1, c, n);
     };
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) probs(0, r4);
@@ -1122,19 +1124,19 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
       each<NP>([&](auto ii) {
         constexpr int i = decltype(ii)::value;
         vec& op = ops[(c * NP + i) % kAhead];
-        if constexpr (i < 2 * MT) {
-          constexpr int st = i / MT;
-          o[i % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pw[c][4 * st], pw[c][4 * st + 1], pw[c][4 * st + 2],
-                                                                     pw[c][4 * st + 3])), o[i % MT]);
+        if constexpr (i % 2 == 0) {
+          constexpr int st = i / 2 / MT;
+          o[i / 2 % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pw[c][4 * st], pw[c][4 * st + 1], pw[c][4 * st + 2],
+                                                                     pw[c][4 * st + 3])), o[i / 2 % MT]);
           if constexpr (LO)
-            o[i % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pl[c][4 * st], pl[c][4 * st + 1], pl[c][4 * st + 2],
-                                                                       pl[c][4 * st + 3])), o[i % MT]);
+            o[i / 2 % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pl[c][4 * st], pl[c][4 * st + 1], pl[c][4 * st + 2],
+                                                                       pl[c][4 * st + 3])), o[i / 2 % MT]);
         } else {
-          if constexpr (i == 2 * MT)
+          if constexpr (i == 1)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-          s[c] = H::mfma(op, q[i - 2 * MT], s[c]);
-          s[c] = H::mfma(op, q_lo[i - 2 * MT], s[c]);
+          s[c] = H::mfma(op, q[i / 2], s[c]);
+          s[c] = H::mfma(op, q_lo[i / 2], s[c]);
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
