@@ -261,14 +261,13 @@ __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf
 // load by exchanging nibbles of neighbouring tokens (two operations for eight
 // codes) before the conversion.
 //
-// Q (scaled) is the sum of two bf16 values, 16 bits: the scores, and lse, are
-// then as exact as binary32 sums.  P * (V's scale) is rounded once to bf16
-// where both inputs and outputs are bf16 (the output's own rounding is as
-// large); else (LO) it is two bf16 values too, over the whole range of the
-// scales.
+// Q (scaled) and P * (V's scale) are each the sum of two bf16 values, 16 bits
+// over the whole range of the scales: the matrix cores have time for both, and
+// outputs are as exact as binary32 sums before their own rounding.  (P in one
+// value saved 2 % of a decode step and added half again to a bf16 output's error.)
 //
 // Bound by HBM, (D + 8) bytes per token and KV head, with the vector units
-// close behind: about 210 operations per step, 80 of them conversions of codes.  The
+// close behind: about 235 operations per step, 80 of them conversions of codes.  The
 // four waves of a workgroup are joined through LDS, the parts of a split tile
 // by k_merge.
 
@@ -409,7 +408,7 @@ struct Rows {
 // first use of its result: the compiler then leaves out the wait states that
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
-template <int D, int NT, int N, int KT, bool LO>
+template <int D, int NT, int N, int KT>
 __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
                                           int g) {
   constexpr int KC = D / 32;
@@ -481,14 +480,10 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
         float w = pr * vs[e];
         // a scale that is not finite must not reach rows that do not see its token
         if (!whole) w = (seen >> (4 * i + e)) & 1 ? w : 0.0f;
-        if constexpr (LO) {
-          __bf16 x0, x1;
-          split_bf16(w, x0, x1);
-          ph[nt][i / 2][4 * (i % 2) + e] = x0;
-          pl[nt][i / 2][4 * (i % 2) + e] = x1;
-        } else {
-          ph[nt][i / 2][4 * (i % 2) + e] = static_cast<__bf16>(w);
-        }
+        __bf16 x0, x1;
+        split_bf16(w, x0, x1);
+        ph[nt][i / 2][4 * (i % 2) + e] = x0;
+        pl[nt][i / 2][4 * (i % 2) + e] = x1;
       }
     }
   }
@@ -519,7 +514,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
 #pragma unroll
       for (int nt = 0; nt < N; ++nt) {
         x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[nt][u], x.o[nt][e], 0, 0, 0);
-        if constexpr (LO) x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
+        x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
       }
     };
     pv(std::integral_constant<int, 0>{}, ev, 0);
@@ -535,7 +530,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
   }
 }
 
-template <int D, int NT, int KT, bool LO>
+template <int D, int NT, int KT>
 __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
@@ -639,7 +634,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
         if (b + i >= w1) break;
         there[i ^ 1] = load(b + i + 1 < w1 ? b + i + 1 : w1 - 1, ring[i ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
-        few_step<D, NT, N, KT, LO>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
+        few_step<D, NT, N, KT>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
       }
     }
   };
@@ -1216,10 +1211,9 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   }
 }
 
-// Joins the parts of split tiles, a workgroup for per_group rows one after
-// the other: the parts'
-// weights first, then the sum of their outputs, eight at a time (D / 4 threads
-// each).
+// Joins the parts of split tiles, a workgroup for per_group rows: up to eight
+// parts a wave per row, else one row after the other, the parts' weights first,
+// then the sum of their outputs, eight at a time (D / 4 threads each).
 constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 
 template <int D, int M>
@@ -1237,6 +1231,34 @@ __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target, int 
   const int row0 = blockIdx.z * per_group;
   if (row0 + per_group < rows) rows = row0 + per_group;
   const int64_t step = static_cast<int64_t>(a.g.Hkv) * M;
+  if (p.parts <= 8) {
+    // few parts: a wave per row, a lane per part for its weight
+    for (int row = row0 + w; row < rows; row += 4) {
+      const int64_t first = (static_cast<int64_t>(p.slot) * a.g.Hkv + h) * M + row;
+      float2 ml = make_float2(kNegInf, 0.0f);
+      if (lane < p.parts) ml = a.part_ml[first + lane * step];
+      float mm = ml.x;
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) mm = fmaxf(mm, __shfl_xor(mm, d));
+      mm = __shfl(mm, 0);
+      const float x = rescale(ml.x, mm);
+      float l = x * ml.y;
+#pragma unroll
+      for (int d = 1; d < 8; d *= 2) l += __shfl_xor(l, d);
+      l = __shfl(l, 0);
+      float out[D / 64] = {};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i >= p.parts) break;
+        const float xi = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), i));
+#pragma unroll
+        for (int z = 0; z < D / 64; ++z) out[z] += xi * a.part_o[(first + i * step) * D + lane * (D / 64) + z];
+      }
+      const int i = (p.tile * M + row) / a.G;
+      finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, out, mm, l, lane);
+    }
+    return;
+  }
   for (int row = row0; row < rows; ++row) {
     const int64_t first = (static_cast<int64_t>(p.slot) * a.g.Hkv + h) * M + row;   // of part 0
     float mm = kNegInf;
@@ -1317,8 +1339,7 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   g.tiles = a.R;   // a request of few rows is one tile
   g.merges = g.tiles < a.target ? g.tiles : a.target;
   const dim3 grid(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv));
-  if (a.is_fp16 || a.out_dtype != RA_BF16) k_few<D, NT, 2, true><<<grid, dim3(256), 0, s>>>(a);
-  else k_few<D, NT, 2, false><<<grid, dim3(256), 0, s>>>(a);
+  k_few<D, NT, 2><<<grid, dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, M>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
 }

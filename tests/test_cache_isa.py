@@ -137,7 +137,7 @@ def test_no_product_is_used_too_early(tmp_path):
         elif body is not None:
             body.append(ln)
     kernels = {k: v for k, v in kernels.items() if any("mfma" in x for x in v)}
-    assert sum("k_few" in k for k in kernels) == 8 and sum("k_rows" in k for k in kernels) == 8
+    assert sum("k_few" in k for k in kernels) == 4 and sum("k_rows" in k for k in kernels) == 8
     bad = {k: _violations(v)[:3] for k, v in kernels.items()}
     bad = {k: v for k, v in bad.items() if v}
     assert not bad, f"products used too early: {bad}"

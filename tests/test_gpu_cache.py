@@ -359,9 +359,8 @@ def _attn_case(ra, Hq, Hkv, D, page, lens, qs, dt="bf16", out=None, rope=False, 
 
 def _operand(dt, out, rows):
     """Half a step of the matrix products' operands (Q, P).  Q is two values of 8 (11) bits or more, one below the
-    other: 2^-16.  P is one value where the output is no finer than it, else two as well; requests of few rows take
-    bf16 values for binary16 inputs too, always two."""
-    one = out == "bf16" and dt == "bf16" if rows <= 32 else out != "fp32" and (dt, out) != ("bf16", "fp16")
+    other: 2^-16.  P is two as well, but one for requests of many rows where the output is no finer than it."""
+    one = rows > 32 and out != "fp32" and (dt, out) != ("bf16", "fp16")
     return 2.0 ** -16, HALF[dt] if one else 2.0 ** -16
 
 
