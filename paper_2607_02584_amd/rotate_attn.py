@@ -358,7 +358,7 @@ def cache_workspace_size(p: CacheParams, R: int, T: int, max_q: int) -> int:
 
 
 # The cache calls are made once per layer and token: what is checked stays one
-# comparison per tensor while all is well (a call with its launch takes 6 to 11
+# comparison per tensor while all is well (a call with its launches takes 9 to 16
 # us of host time), the reasons are worked out on the way to the error.
 
 _dtypes = None

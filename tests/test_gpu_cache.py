@@ -408,6 +408,19 @@ def test_attn_decode_types_and_heads(ra, dt, out, Hq, Hkv):
                vhad=out == "fp32", pad=3, seed=Hq, strided=True)
 
 
+@pytest.mark.parametrize("Hq,Hkv,dt", [(48, 1, "bf16"), (20, 1, "fp16"), (33, 1, "fp16"), (34, 2, "bf16")])
+def test_attn_decode_of_large_head_groups(ra, Hq, Hkv, dt):
+    """Groups of 17 to 32 rows, and of more than a request of few rows has."""
+    _attn_case(ra, Hq, Hkv, 128, 64, [1500, 40, 0, 9000], [1, 1, 0, 1], dt, rope=True, seed=Hq)
+
+
+def test_attn_of_many_requests_with_few_and_many_rows(ra):
+    rng = np.random.default_rng(77)
+    lens = rng.integers(1, 300, 80).tolist()
+    qs = [min(n, int(q)) for n, q in zip(lens, rng.choice([0, 1, 1, 1, 5, 60], 80))]
+    _attn_case(ra, 4, 1, 64, 32, lens, qs, "bf16", rope=True, vhad=True, pad=1, seed=77)
+
+
 @pytest.mark.parametrize("R,n", [(1, 20011), (3, 9000), (70, 400), (300, 130)])
 def test_attn_decode_split_and_many(ra, R, n):
     rng = np.random.default_rng(R)
