@@ -705,11 +705,12 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // the same query's output, so that rescaling it is a factor per lane.
 //
 // Q (after RoPE, rotation and scale, in binary32) is the sum of two values of
-// the input type, so that scores and lse are as exact as binary32 sums; P *
-// (V's scale) is one, 2^-8 or 2^-11 relative, and two (LO) where the output is
-// finer than the input type.  In binary16 the V scales are taken relative to
-// the power of two of the largest so far (O is in units of it), so that P *
-// scale neither overflows nor loses small values.
+// the input type, so that scores and lse are as exact as binary32 sums.  P *
+// (V's scale) is bf16 for either input type: a scale may be anything from
+// 2^-100 to 2^127 and a weight anything up to 2^8, whose product binary16 cannot
+// hold beside others (in units of a tile's largest scale it loses the rows that
+// do not see that token).  It is one value, 2^-8 relative, where the output is
+// bf16, and two (LO), 2^-17, where the output is finer.
 //
 // LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
 // bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
@@ -817,14 +818,15 @@ __device__ __forceinline__ void each(F&& f) {
 // scales) one, and two LDS buffers of each suffice.
 template <int D, bool F16, bool LO>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
-  typedef Half16<F16> H;
+  typedef Half16<F16> H;     // K and Q
+  typedef Half16<false> HV;  // V and P
   typedef typename H::vec vec;
+  typedef typename HV::vec vecv;
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
   struct Scales {
     float ks[64], vs[64];
     unsigned long long there;   // keys that are on a page
-    float ref;
   };
   struct Buf {
     uint4 k[2][D / 8][64];
@@ -913,7 +915,6 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     sv = *reinterpret_cast<const Codes*>(pv);
     entries(bk + 1, cv + 1);
   };
-  float ref_s = 0.0f;   // last wave: power of two of the largest V scale so far
   // The staged codes into LDS, in four parts each.  What is written past the
   // last tile replaces tiles that are done with.
   auto put_k = [&](int b, auto part) {
@@ -931,12 +932,12 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     if constexpr (D == 128) {
       const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
                      o23 = odd_of(sv.z, sv.w);
-      dst[2 * c * 32] = make_uint2(H::template codes<c>(e01), H::template codes<c>(e23));
-      dst[(2 * c + 1) * 32] = make_uint2(H::template codes<c>(o01), H::template codes<c>(o23));
+      dst[2 * c * 32] = make_uint2(HV::template codes<c>(e01), HV::template codes<c>(e23));
+      dst[(2 * c + 1) * 32] = make_uint2(HV::template codes<c>(o01), HV::template codes<c>(o23));
     } else {
       const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
       const uint32_t n = c % 2 ? odd_of(t02, t13) : even_of(t02, t13);
-      dst[c * 32] = make_uint2(H::template codes<c / 2>(n), H::template codes<c / 2 + 2>(n));
+      dst[c * 32] = make_uint2(HV::template codes<c / 2>(n), HV::template codes<c / 2 + 2>(n));
     }
   };
   auto put_scales = [&](int b) {
@@ -947,17 +948,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     const bool odd = here && !(vs < __builtin_inff());
     const float k0 = here ? (odd ? vs : ks) : 0.0f;
     const float v0 = here && !odd ? vs : 0.0f;
-    if constexpr (F16) {
-      float mx = v0;
-#pragma unroll
-      for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d));
-      mx = __uint_as_float(__float_as_uint(mx) & 0x7f800000u);
-      ref_s = fmaxf(fmaxf(ref_s, mx), 0x1p-120f);
-      t.vs[lane] = v0 * (1.0f / ref_s);
-      if (lane == 0) t.ref = ref_s;
-    } else {
-      t.vs[lane] = v0;
-    }
+    t.vs[lane] = v0;
     t.ks[lane] = k0;
     const unsigned long long all = __ballot(here);
     if (lane == 0) t.there = all;
@@ -990,7 +981,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   for (int i = 0; i < MT; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[i][r] = 0.0f;
-  float m = kNegInf, l = 0.0f, unit = 0x1p-120f;
+  float m = kNegInf, l = 0.0f;
   put(b0, b0);
   put_scales(b0);
   if (b0 < b1) {
@@ -1000,15 +991,16 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   }
   __syncthreads();
 
-  auto k_op = [&](int b, int c, int kc) { return __builtin_bit_cast(vec, buf.k[b & 1][hh * KC + kc][c * 32 + j]); };
+  auto k_op = [&](int b, int c, int kc) { return buf.k[b & 1][hh * KC + kc][c * 32 + j]; };
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      s[c] = H::mfma(k_op(b0, c, kc), q[kc], s[c]);
-      s[c] = H::mfma(k_op(b0, c, kc), q_lo[kc], s[c]);
+      const vec k = __builtin_bit_cast(vec, k_op(b0, c, kc));
+      s[c] = H::mfma(k, q[kc], s[c]);
+      s[c] = H::mfma(k, q_lo[kc], s[c]);
     }
     settle(s[c]);
   }
@@ -1061,11 +1053,6 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) x[c][r] -= by;
     }
-    if constexpr (F16) {
-      const float next = t.ref;
-      alpha *= unit * (1.0f / next);
-      unit = next;
-    }
     if (__any(alpha != 1.0f)) {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -1089,12 +1076,12 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
       }
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        uint32_t u = pack16(y[2 * e], y[2 * e + 1], F16);
+        uint32_t u = pack16(y[2 * e], y[2 * e + 1], false);
         if constexpr (LO) pin(u);   // as in load_q32
         pw[c][2 * r4 + e] = u;
         if constexpr (LO)
-          pl[c][2 * r4 + e] = pack16(y[2 * e] - cache_h2f(static_cast<uint16_t>(u & 0xffff), F16),
-                                     y[2 * e + 1] - cache_h2f(static_cast<uint16_t>(u >> 16), F16), F16);
+          pl[c][2 * r4 + e] = pack16(y[2 * e] - cache_h2f(static_cast<uint16_t>(u & 0xffff), false),
+                                     y[2 * e + 1] - cache_h2f(static_cast<uint16_t>(u >> 16), false), false);
       }
     };
     // products of chunk c, in turn: one of the 2 MT of P V (step n / MT, tile n %
@@ -1105,12 +1092,11 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     constexpr int NP = 2 * MT + KC, kAhead = 4;
     auto operand = [&](int c, int i) {
       const int n = i / 2;
-      if (i % 2 == 0) return __builtin_bit_cast(vec, buf.v[b & 1][(c * 2 + n / MT) * 2 + hh][(n % MT) * 32 + j]);
-      return k_op(b + 1, c, n);
+      return i % 2 == 0 ? buf.v[b & 1][(c * 2 + n / MT) * 2 + hh][(n % MT) * 32 + j] : k_op(b + 1, c, n);
     };
 #pragma unroll
     for (int r4 = 0; r4 < 4; ++r4) probs(0, r4);
-    vec ops[kAhead];
+    uint4 ops[kAhead];
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) ops[i] = operand(0, i);
     __builtin_amdgcn_sched_barrier(0);
@@ -1118,20 +1104,22 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
       constexpr int c = decltype(cc)::value;
       each<NP>([&](auto ii) {
         constexpr int i = decltype(ii)::value;
-        vec& op = ops[(c * NP + i) % kAhead];
+        uint4& op = ops[(c * NP + i) % kAhead];
         if constexpr (i % 2 == 0) {
           constexpr int st = i / 2 / MT;
-          o[i / 2 % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pw[c][4 * st], pw[c][4 * st + 1], pw[c][4 * st + 2],
-                                                                     pw[c][4 * st + 3])), o[i / 2 % MT]);
-          if constexpr (LO)
-            o[i / 2 % MT] = H::mfma(op, __builtin_bit_cast(vec, make_uint4(pl[c][4 * st], pl[c][4 * st + 1], pl[c][4 * st + 2],
-                                                                       pl[c][4 * st + 3])), o[i / 2 % MT]);
+          const vecv v = __builtin_bit_cast(vecv, op);
+          auto four = [&](const uint32_t* w) {
+            return __builtin_bit_cast(vecv, make_uint4(w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]));
+          };
+          o[i / 2 % MT] = HV::mfma(v, four(pw[c]), o[i / 2 % MT]);
+          if constexpr (LO) o[i / 2 % MT] = HV::mfma(v, four(pl[c]), o[i / 2 % MT]);
         } else {
           if constexpr (i == 1)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-          s[c] = H::mfma(op, q[i / 2], s[c]);
-          s[c] = H::mfma(op, q_lo[i / 2], s[c]);
+          const vec k = __builtin_bit_cast(vec, op);
+          s[c] = H::mfma(k, q[i / 2], s[c]);
+          s[c] = H::mfma(k, q_lo[i / 2], s[c]);
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
@@ -1167,12 +1155,6 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
 
   // out through LDS, 8 rows of each wave at a time
   l += lane_xor<32>(l);
-  if constexpr (F16) {
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o[i][r] *= unit;
-  }
   constexpr int kStride = D + 4;
   static_assert(sizeof(buf) >= NW * 8 * kStride * sizeof(float), "the output rows pass through the tiles' LDS");
   float* so = reinterpret_cast<float*>(&buf) + w * 8 * kStride;
@@ -1359,8 +1341,8 @@ hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.G <= kFewRows) e = few<D, 2>(a, s);   // requests of few rows; with more heads than that there are none
   if (e != hipSuccess || most <= kFewRows) return e;
-  // P in one value of the input type where the output is no finer than that
-  const bool lo = a.out_dtype == RA_FP32 || (!a.is_fp16 && a.out_dtype == RA_FP16);
+  // P in one bf16 value where the output is no finer than that
+  const bool lo = a.out_dtype != RA_BF16;
   if (a.is_fp16) return lo ? rows<D, true, true>(a, s) : rows<D, true, false>(a, s);
   return lo ? rows<D, false, true>(a, s) : rows<D, false, false>(a, s);
 }

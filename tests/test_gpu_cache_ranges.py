@@ -1,0 +1,109 @@
+"""The 4-bit paged KV cache where magnitudes lie far apart, against plain numpy in 64 bits (tests/cache_ref.py)."""
+import numpy as np
+import pytest
+
+import cache_ref as ref
+import test_gpu_cache as base
+from test_gpu_cache import DT, HALF, _f64, _filled, _i32, _params, ra  # noqa: F401  (ra: the fixture)
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+PAIR = 2.0 ** -17    # of a value held as two bf16 values: half a step of the second, which is at most half a step of the first
+
+
+def _scales(cache, p):
+    """K and V scales [pages, Hkv, 2, page] of page bytes, as a view."""
+    at = p.page_size * p.D
+    return cache.reshape(p.num_pages, p.Hkv, -1)[:, :, at:].view(np.float32).reshape(p.num_pages, p.Hkv, 2, p.page_size)
+
+
+def _dense(cache, table, p, n):
+    slots = [int(table[0, t // p.page_size]) * p.page_size + t % p.page_size for t in range(n)]
+    kc, ks, vc, vs = ref.rows(cache, slots, p.page_size, p.Hkv, p.D)
+    return ref.value(kc) * ks[..., None].astype(np.float64), ref.value(vc) * vs[..., None].astype(np.float64)
+
+
+def _run(ra, p, q, cache, table, n, out):
+    m = q.shape[0]
+    o, lse = torch.full(q.shape, 5.0, dtype=DT[out], device="cuda"), torch.full(q.shape[:2], 5.0, device="cuda")
+    ra.cache_attn(p, q, torch.from_numpy(cache).cuda(), _i32(table), _i32([0, m]), _i32([n]), m, o,
+                  ra.cache_workspace(p, 1, m, m), lse=lse)
+    return o, lse
+
+
+def _want(p, q, cache, table, n, rows=slice(None)):
+    """Outputs, lse and what the bound takes of one request's queries."""
+    k, v = _dense(cache, table, p, n)
+    G, H = p.Hq // p.Hkv, ref.hadamard(p.D) / np.sqrt(p.D)
+    x = _f64(q)
+    scale = p.sm_scale or p.D ** -0.5
+    want, lse = np.zeros(x.shape), np.zeros(x.shape[:2])
+    size_v, size_s = np.zeros(x.shape), np.zeros(x.shape[:2])
+    for h in range(p.Hq):
+        y = x[:, h] @ H if p.rotation else x[:, h]
+        y, z, av, a = ref.attn(y, k[:, h // G], v[:, h // G], bool(p.causal), p.window, scale)
+        want[:, h] = y @ H if p.v_rotation else y
+        size_v[:, h] = np.abs(av).sum(1, keepdims=True) / np.sqrt(p.D) if p.v_rotation else av
+        lse[:, h], size_s[:, h] = z, a
+    return [x[rows] for x in (want, lse, size_v, size_s)]
+
+
+def _check(o, lse, want, out, n, many):
+    """test_gpu_cache's bounds with two values of bf16 for Q and, but for bf16 outputs of many rows, for P; nothing
+    else for small weights or values.  Binary16 outputs below 2^-14 round by up to 2^-25."""
+    want, want_lse, size_v, size_s = want
+    e = HALF["bf16"] if many and out == "bf16" else PAIR
+    ds = (PAIR + (want.shape[2] + 8) * 2.0 ** -24) * size_s + 2.0 ** -21
+    acc = (n / 16 + 64) * 2.0 ** -24
+    rel = np.expm1(2 * ds) + e + 2 * acc
+    bound = size_v * rel[..., None] + (np.abs(want) + size_v * rel[..., None]) * HALF[out] + 1e-30
+    bound += 2.0 ** -25 if out == "fp16" else 0.0
+    err = np.abs(_f64(o) - want)
+    assert (err <= bound).all(), f"outputs off by {np.nanmax(err / bound):.3g} of the bound"
+    lim = ds + acc + 2.0 ** -22 * (1 + np.abs(want_lse))
+    d = np.abs(_f64(lse) - want_lse)
+    assert (d <= lim).all(), f"lse off by {np.nanmax(d / lim):.3g} of the bound"
+
+
+# rows of a request that the kernel for few rows takes (24), and of one for many (80)
+@pytest.mark.parametrize("q_len", [12, 40])
+@pytest.mark.parametrize("dt,out", [("fp16", "fp16"), ("fp16", "fp32"), ("fp16", "bf16"), ("bf16", "bf16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("D,vhad", [(128, False), (64, True)])
+def test_attn_large_values_that_a_row_does_not_see(ra, q_len, dt, out, D, vhad):
+    """V of 6e4 in tokens behind a row and left of its window, beside V of 0.05: rows that do not see them are right, and
+    the same bits as with ordinary tokens there."""
+    rng = np.random.default_rng(q_len + D)
+    n, window = 100, 30
+    p = _params(ra, 4, 2, D, 16, 12, 10, vhad=vhad, dt=dt, out=out, window=window)
+    cache, table = _filled(ra, p, rng, [n])
+    sc = _scales(cache, p)
+    sc[:, :, 1] = 0.05 / 6 * rng.uniform(0.5, 1.0, sc[:, :, 1].shape)
+    first = n - q_len
+    left = first - window + 4                     # the first few rows see it, as they see the tokens around it
+    other = cache.copy()
+    for t in (0, left, n - 2, n - 1):
+        _scales(other, p)[table[0, t // 16], :, 1, t % 16] = 6e4 / 6
+    q = torch.tensor(rng.standard_normal((q_len, 4, D))).to(DT[dt]).cuda()
+    rows = slice(5, q_len - 2)
+    ordinary, large = (_run(ra, p, q, c, table, n, out) for c in (cache, other))
+    _check(large[0][rows], large[1][rows], _want(p, q, other, table, n, rows), out, n, q_len > 16)
+    assert torch.equal(ordinary[0][rows], large[0][rows]) and torch.equal(ordinary[1], large[1])
+
+
+@pytest.mark.parametrize("q_len", [20, 40])
+@pytest.mark.parametrize("dt,out", [("fp16", "fp16"), ("fp16", "fp32"), ("bf16", "fp32")])
+def test_attn_a_long_tail_of_small_weights(ra, q_len, dt, out):
+    """One key takes nearly all of the softmax and has V = 0: the output is the other 20000 keys', 2^-23 to 2^-27 each."""
+    rng = np.random.default_rng(q_len)
+    n, D = 20000, 64
+    p = _params(ra, 1, 1, D, 64, n // 64 + 2, n // 64 + 2, dt=dt, out=out, causal=False)
+    cache, table = _filled(ra, p, rng, [n])
+    sc = _scales(cache, p)
+    sc[:, :, 0] = 0.0
+    sc[table[0, 0], :, :, 0] = 1.0, 0.0
+    k, _ = _dense(cache, table, p, 1)
+    x = np.log(2.0) * np.linspace(23, 27, q_len)[:, None] * k[0, 0] / (k[0, 0] ** 2).sum() * np.sqrt(D)
+    q = torch.tensor(x[:, None]).to(DT[dt]).cuda()
+    o, lse = _run(ra, p, q, cache, table, n, out)
+    _check(o, lse, _want(p, q, cache, table, n), out, n, q_len > 32)
