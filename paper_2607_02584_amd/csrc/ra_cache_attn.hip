@@ -696,7 +696,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // --------------------------------------------------------- many rows per request --
 //
 // Bound by the matrix cores and the softmax beside them.  NW waves of 32 rows
-// share tiles of 64 keys in LDS, as 16-bit values of the codes (exact), scales
+// share tiles of 64 keys in LDS, as bf16 values of the codes (exact), scales
 // apart: each wave loads its share of the next tile's codes while the present
 // one is computed, and converts them into the other LDS buffer at its end.
 // S^T = K Q^T and O^T += V^T P^T on the 32x32x16 product: a lane holds one
@@ -704,13 +704,14 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // c), which rounded to 16 bits are the second operand of the next product, and
 // the same query's output, so that rescaling it is a factor per lane.
 //
-// Q (after RoPE, rotation and scale, in binary32) is the sum of two values of
-// the input type, so that scores and lse are as exact as binary32 sums.  P *
-// (V's scale) is bf16 for either input type: a scale may be anything from
-// 2^-100 to 2^127 and a weight anything up to 2^8, whose product binary16 cannot
-// hold beside others (in units of a tile's largest scale it loses the rows that
-// do not see that token).  It is one value, 2^-8 relative, where the output is
-// bf16, and two (LO), 2^-17, where the output is finer.
+// Q (after RoPE, rotation and scale, in binary32) is the sum of two bf16
+// values, within 2^-17 of each element.  P * (V's scale) is one, within 2^-8,
+// where the output is bf16, and two (LO) where the output is finer: two there
+// too took prompts of 26k tokens from 2.1 to 2.6 ms.  Both are bf16 for binary16
+// inputs as well, whose range holds neither a scaled Q (the softmax scale is
+// the caller's) nor a weight up to 2^8 times a scale from 2^-100 to 2^127: in
+// units of a tile's largest scale, binary16 loses the rows that do not see that
+// token.
 //
 // LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
 // bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
@@ -718,34 +719,16 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // order), an octet holds keys 16 s + 4 hh + {0..3, 8..11} of step s.
 
 typedef float v16f __attribute__((ext_vector_type(16)));
-typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
-template <bool F16>
-struct Half16 {
-  typedef v8bf vec;
-  static __device__ __forceinline__ v16f mfma(vec a, vec b, v16f c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
-  }
-  template <int B>
-  static __device__ __forceinline__ uint32_t codes(uint32_t w) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, 1.0f, B));
-  }
-};
-template <>
-struct Half16<true> {
-  typedef v8h vec;
-  static __device__ __forceinline__ v16f mfma(vec a, vec b, v16f c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-  }
-  template <int B>
-  static __device__ __forceinline__ uint32_t codes(uint32_t w) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, B));
-  }
-};
+__device__ __forceinline__ v16f mfma32(v8bf a, v8bf b, v16f c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+template <int B>
+__device__ __forceinline__ uint32_t codes2_bits(uint32_t w) { return __builtin_bit_cast(uint32_t, codes2<B>(w)); }
 
 template <int D, bool F16>
 __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
-                                         typename Half16<F16>::vec (&hi)[D / 16], typename Half16<F16>::vec (&lo)[D / 16]) {
+                                         v8bf (&hi)[D / 16], v8bf (&lo)[D / 16]) {
   constexpr int N = D / 2;
   const int hh = lane >> 5;
   const bool ok = row < p.q.ql * a.G;
@@ -785,13 +768,13 @@ __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p,
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const float u = y[8 * c + 2 * e] * a.c, v = y[8 * c + 2 * e + 1] * a.c;   // scores come out in base 2
-      x[e] = pack16(u, v, F16);
+      x[e] = pack16(u, v, false);
       pin(x[e]);   // what is left over is taken from these bits: another conversion may round a tie the other way
-      r[e] = pack16(u - cache_h2f(static_cast<uint16_t>(x[e] & 0xffff), F16),
-                    v - cache_h2f(static_cast<uint16_t>(x[e] >> 16), F16), F16);
+      r[e] = pack16(u - cache_h2f(static_cast<uint16_t>(x[e] & 0xffff), false),
+                    v - cache_h2f(static_cast<uint16_t>(x[e] >> 16), false), false);
     }
-    hi[c] = __builtin_bit_cast(typename Half16<F16>::vec, make_uint4(x[0], x[1], x[2], x[3]));
-    lo[c] = __builtin_bit_cast(typename Half16<F16>::vec, make_uint4(r[0], r[1], r[2], r[3]));
+    hi[c] = __builtin_bit_cast(v8bf, make_uint4(x[0], x[1], x[2], x[3]));
+    lo[c] = __builtin_bit_cast(v8bf, make_uint4(r[0], r[1], r[2], r[3]));
   }
 }
 
@@ -818,10 +801,6 @@ __device__ __forceinline__ void each(F&& f) {
 // scales) one, and two LDS buffers of each suffice.
 template <int D, bool F16, bool LO>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
-  typedef Half16<F16> H;     // K and Q
-  typedef Half16<false> HV;  // V and P
-  typedef typename H::vec vec;
-  typedef typename HV::vec vecv;
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
   struct Scales {
@@ -922,7 +901,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     if constexpr (c < D / 32) {
       const uint32_t x = dword_of<D>(sk, c);
       buf.k[b & 1][(lane >> 4) * (D / 32) + c][mine + (lane & 15)] =
-          make_uint4(H::template codes<0>(x), H::template codes<1>(x), H::template codes<2>(x), H::template codes<3>(x));
+          make_uint4(codes2_bits<0>(x), codes2_bits<1>(x), codes2_bits<2>(x), codes2_bits<3>(x));
     }
   };
   auto put_v = [&](int b, auto part) {   // channels E / 4 * part .. of the lane's chunk
@@ -932,12 +911,12 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     if constexpr (D == 128) {
       const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
                      o23 = odd_of(sv.z, sv.w);
-      dst[2 * c * 32] = make_uint2(HV::template codes<c>(e01), HV::template codes<c>(e23));
-      dst[(2 * c + 1) * 32] = make_uint2(HV::template codes<c>(o01), HV::template codes<c>(o23));
+      dst[2 * c * 32] = make_uint2(codes2_bits<c>(e01), codes2_bits<c>(e23));
+      dst[(2 * c + 1) * 32] = make_uint2(codes2_bits<c>(o01), codes2_bits<c>(o23));
     } else {
       const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
       const uint32_t n = c % 2 ? odd_of(t02, t13) : even_of(t02, t13);
-      dst[c * 32] = make_uint2(HV::template codes<c / 2>(n), HV::template codes<c / 2 + 2>(n));
+      dst[c * 32] = make_uint2(codes2_bits<c / 2>(n), codes2_bits<c / 2 + 2>(n));
     }
   };
   auto put_scales = [&](int b) {
@@ -974,7 +953,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     entries(b0, b0);
     ask(b0, b0);
   }
-  vec q[KC], q_lo[KC];
+  v8bf q[KC], q_lo[KC];
   load_q32<D, F16>(a, p, h, row, lane, q, q_lo);
   v16f o[MT], s[2];
 #pragma unroll
@@ -998,9 +977,9 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const vec k = __builtin_bit_cast(vec, k_op(b0, c, kc));
-      s[c] = H::mfma(k, q[kc], s[c]);
-      s[c] = H::mfma(k, q_lo[kc], s[c]);
+      const v8bf k = __builtin_bit_cast(v8bf, k_op(b0, c, kc));
+      s[c] = mfma32(k, q[kc], s[c]);
+      s[c] = mfma32(k, q_lo[kc], s[c]);
     }
     settle(s[c]);
   }
@@ -1107,19 +1086,19 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         uint4& op = ops[(c * NP + i) % kAhead];
         if constexpr (i % 2 == 0) {
           constexpr int st = i / 2 / MT;
-          const vecv v = __builtin_bit_cast(vecv, op);
+          const v8bf v = __builtin_bit_cast(v8bf, op);
           auto four = [&](const uint32_t* w) {
-            return __builtin_bit_cast(vecv, make_uint4(w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]));
+            return __builtin_bit_cast(v8bf, make_uint4(w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]));
           };
-          o[i / 2 % MT] = HV::mfma(v, four(pw[c]), o[i / 2 % MT]);
-          if constexpr (LO) o[i / 2 % MT] = HV::mfma(v, four(pl[c]), o[i / 2 % MT]);
+          o[i / 2 % MT] = mfma32(v, four(pw[c]), o[i / 2 % MT]);
+          if constexpr (LO) o[i / 2 % MT] = mfma32(v, four(pl[c]), o[i / 2 % MT]);
         } else {
           if constexpr (i == 1)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-          const vec k = __builtin_bit_cast(vec, op);
-          s[c] = H::mfma(k, q[i / 2], s[c]);
-          s[c] = H::mfma(k, q_lo[i / 2], s[c]);
+          const v8bf k = __builtin_bit_cast(v8bf, op);
+          s[c] = mfma32(k, q[i / 2], s[c]);
+          s[c] = mfma32(k, q_lo[i / 2], s[c]);
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);

@@ -107,3 +107,21 @@ def test_attn_a_long_tail_of_small_weights(ra, q_len, dt, out):
     q = torch.tensor(x[:, None]).to(DT[dt]).cuda()
     o, lse = _run(ra, p, q, cache, table, n, out)
     _check(o, lse, _want(p, q, cache, table, n), out, n, q_len > 32)
+
+
+@pytest.mark.parametrize("q_len", [12, 40])
+@pytest.mark.parametrize("dt,out,D,had", [("fp16", "fp16", 128, True), ("fp16", "fp32", 64, False), ("bf16", "fp32", 128, False)])
+@pytest.mark.parametrize("gain,sm_scale", [(3000.0, 64.0), (1e-4, 0.0), (1.0, 1e-5)])
+def test_attn_queries_whose_scaled_values_leave_binary16(ra, q_len, dt, out, D, had, gain, sm_scale):
+    """Queries times the softmax scale above 65504 against small keys, and below 2^-14 against large ones."""
+    rng = np.random.default_rng(q_len + D)
+    n = 300
+    p = _params(ra, 4, 2, D, 32, 12, 10, had=had, dt=dt, out=out, sm_scale=sm_scale)
+    cache, table = _filled(ra, p, rng, [n], poison=False)
+    sc = _scales(cache, p)
+    # scores of about 4
+    sc[:, :, 0] *= 4 / ((sm_scale or D ** -0.5) * gain * D ** 0.5)
+    q = torch.tensor(rng.standard_normal((q_len, 4, D)) * gain).to(DT[dt]).cuda()
+    assert torch.isfinite(q).all()
+    o, lse = _run(ra, p, q, cache, table, n, out)
+    _check(o, lse, _want(p, q, cache, table, n), out, n, q_len > 16)
