@@ -325,9 +325,9 @@ int rotate_attn_fwd(const ra_params* p, int fallback, const void* q, const void*
  * to nearest, ties to the even code, and scale = a / 6 (times 1/sqrt(D) where
  * rotated) in binary32.  Codes are those of 64-bit arithmetic: quotients within
  * 2^-18 of a border are taken again in binary64.  A row with a < 2^-100
- * is kept as zeros; one that is not finite has NaN for its scale, and every
- * query that sees it gives NaN (nothing else does: masked and padding rows may
- * hold anything).
+ * is kept as zeros; one that is not finite, or whose sums leave binary32, has
+ * NaN for its scale, and every query that sees it gives NaN (nothing else does:
+ * masked and padding rows may hold anything).
  *
  * Page: for each KV head, page_size * (D + 8) bytes: K codes, V codes, K
  * scales, V scales (ra_cache_sizes has the offsets).  For token t of the page

@@ -317,11 +317,12 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
   turn<float, D, ROPE, HAD>(x, cs, y, lane);
   uint32_t m = 0;
   if constexpr (HAD) {
-    // (one element that is not finite leaves none that is)
+    // NaN where any is (a sum that leaves binary32 makes infinities, which cancel to NaN in some channels only)
     float f = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; i += 2) f = fmaxf(fmaxf(f, fabsf(y[i])), fabsf(y[i + 1]));
-    m = y[0] == y[0] ? __float_as_uint(f) : 0x7fc00000u;
+    for (int i = 0; i < 8; i += 2)
+      f = __builtin_elementwise_maximum(__builtin_elementwise_maximum(f, fabsf(y[i])), fabsf(y[i + 1]));
+    m = __float_as_uint(f) & 0x7fffffffu;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {

@@ -125,3 +125,37 @@ def test_attn_queries_whose_scaled_values_leave_binary16(ra, q_len, dt, out, D, 
     assert torch.isfinite(q).all()
     o, lse = _run(ra, p, q, cache, table, n, out)
     _check(o, lse, _want(p, q, cache, table, n), out, n, q_len > 16)
+
+
+# ----------------------------------------------------------------- append --
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("rope", [False, True])
+def test_append_rows_whose_rotation_overflows_are_not_finite(ra, D, rope):
+    """Finite rows whose sums leave binary32 in a stage of the rotation: infinities cancel to NaN in half of the
+    channels, the others are 0.  The scale is NaN, of K and of V, and the tokens beside them are as they were."""
+    T, Hkv, page = 40, 2, 16
+    p = _params(ra, 2, Hkv, D, page, 4, 4, had=True, vhad=True, out="fp32")
+    rng = np.random.default_rng(D)
+    x = rng.standard_normal((T, 2 * Hkv, D))
+    bad = np.zeros(D)
+    block = np.arange(D // 8)
+    bad[0::8], bad[1::8] = 3e38, -3e38
+    bad *= np.repeat(np.where(block % 4 == 3, -1.0, 1.0), 8)
+    rows = [3, 17, 38]
+    x[rows, 0], x[rows, -1] = bad, bad            # K of head 0, V of the last head
+    xd = torch.tensor(x).to(torch.bfloat16).cuda()
+    assert torch.isfinite(xd).all()
+    table = ref.rope_table(64, D)
+    table[:] = [1.0, 0.0]                          # turned by nothing, so that the same sums come up
+    cache = torch.zeros((4, ra.cache_layout(p)["page_bytes"]), dtype=torch.uint8, device="cuda")
+    pos = np.arange(T)
+    ra.cache_append(p, xd[:, :Hkv], xd[:, Hkv:], _i32(pos), cache, positions=_i32(pos) if rope else None,
+                    rope=torch.from_numpy(table).cuda() if rope else None)
+    kc, ks, vc, vs = ref.rows(cache.cpu().numpy(), pos, page, Hkv, D)
+    want = np.zeros((2, T, Hkv), bool)
+    want[0, rows, 0], want[1, rows, -1] = True, True
+    assert (np.isnan(ks) == want[0]).all() and (np.isnan(vs) == want[1]).all()
+    H = ref.hadamard(D)
+    for c, src, w in ((kc, xd[:, :Hkv], want[0]), (vc, xd[:, Hkv:], want[1])):
+        assert (ref.value(c) == ref.value(ref.codes(_f64(src) @ H)[0]))[~w].all()
