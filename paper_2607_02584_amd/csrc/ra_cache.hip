@@ -351,9 +351,10 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
       lo[i] = copysignf((fabsf(t) + 192.0f) - 192.0f, t);   // multiples of 2^-16
     }
   }
-  uint32_t code = dead ? 0u : pack_fp4(lo);
+  uint32_t code = dead ? 0u : pack_fp4(ROPE || HAD ? hi : lo);
   if constexpr (ROPE || HAD) {
-    if (__any(!dead && code != pack_fp4(hi))) {
+    // (magnitudes: they only differ in sign around 0, which is no border)
+    if (__any(!dead && ((code ^ pack_fp4(lo)) & 0x77777777u))) {
       double z[8];
       turn<double, D, ROPE, HAD>(x, cs, z, lane);
       double zm = 0.0;

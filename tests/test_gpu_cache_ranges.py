@@ -159,3 +159,40 @@ def test_append_rows_whose_rotation_overflows_are_not_finite(ra, D, rope):
     H = ref.hadamard(D)
     for c, src, w in ((kc, xd[:, :Hkv], want[0]), (vc, xd[:, Hkv:], want[1])):
         assert (ref.value(c) == ref.value(ref.codes(_f64(src) @ H)[0]))[~w].all()
+
+
+def test_append_of_zeros_costs_what_other_values_cost(ra):
+    """Heads of 96 padded to 128, RoPE without rotation: exact zeros are no border, so nothing is done again in
+    binary64 for them (which takes 1.8 times as long).  Best of several runs, so that other work does not count."""
+    T, Hkv, D, page = 20000, 8, 128, 64
+    pages = T // page + 1
+    p = _params(ra, Hkv, Hkv, D, page, pages, pages)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    k, v = (torch.randn(T, Hkv, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    pos = torch.arange(T, dtype=torch.int32, device="cuda")
+    rope = torch.from_numpy(ref.rope_table(pages * page, D)).cuda()
+    cache = torch.empty((pages, ra.cache_layout(p)["page_bytes"]), dtype=torch.uint8, device="cuda")
+    padded = k.clone()
+    padded[..., 96:] = 0
+
+    def best(x):
+        times = []
+        for _ in range(12):
+            a, b = torch.cuda.Event(True), torch.cuda.Event(True)
+            a.record()
+            for _ in range(20):
+                ra.cache_append(p, x, v, pos, cache, positions=pos, rope=rope)
+            b.record()
+            b.synchronize()
+            times.append(a.elapsed_time(b))
+        return min(times)
+    best(k)
+    assert best(padded) < 1.3 * best(k)
+    slots = np.arange(0, T, 97)
+    kc, _, _, _ = ref.rows(cache.cpu().numpy(), slots, page, Hkv, D)
+    want, _ = ref.codes(ref.turn(_f64(padded)[slots], ref.rope_table(pages * page, D)[slots]))
+    want_k, _ = ref.codes(ref.turn(_f64(k)[slots], ref.rope_table(pages * page, D)[slots]))
+    assert (ref.value(kc) == ref.value(want_k)).all()      # k came last
+    ra.cache_append(p, padded, v, pos, cache, positions=pos, rope=rope)
+    kc, _, _, _ = ref.rows(cache.cpu().numpy(), slots, page, Hkv, D)
+    assert (ref.value(kc) == ref.value(want)).all()
