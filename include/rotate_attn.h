@@ -323,8 +323,9 @@ int rotate_attn_fwd(const ra_params* p, int fallback, const void* q, const void*
  * matrix, without 1/sqrt(D), where rotated) with a = max |y| is kept as E2M1
  * floats (0, .5, 1, 1.5, 2, 3, 4, 6 and a sign), code = E2M1(6 y / a) rounded
  * to nearest, ties to the even code, and scale = a / 6 (times 1/sqrt(D) where
- * rotated) in binary32.  Codes are those of 64-bit arithmetic: quotients within
- * 2^-18 of a border are taken again in binary64.  A row with a < 2^-100
+ * rotated) in binary32.  Codes are those of 64-bit arithmetic: quotients nearer
+ * to a border than binary32 can be off (2^-14 for rotated rows, 2^-18 for others)
+ * are taken again in binary64.  A row with a < 2^-100
  * is kept as zeros; one that is not finite, or whose sums leave binary32, has
  * NaN for its scale, and every query that sees it gives NaN (nothing else does:
  * masked and padding rows may hold anything).

@@ -263,13 +263,29 @@ __global__ __launch_bounds__(kPlanThreads) void k_place(PlanArgs a) {
 // Which code a value gets is decided as 64 bits decide it.  16-bit inputs that
 // are not turned meet borders exactly (x / a = 1/8, 5/12, ...), where 6x / a
 // rounded in binary32 can fall on either side: such a quotient is off by less
-// than 2^-21 and another one is at least 2^-13 away from the border, so it is
+// than 2^-20 and another one is at least 2^-14.6 away from the border, so it is
 // first rounded to multiples of 2^-16, which puts it back on it.  Turned
-// values meet borders only by chance: where 6y / a +- 2^-18 rounds to two codes
-// the wave does the row again in binary64 (1 in 100 waves).  The roundings of
-// the seven stages leave 6y / a off by about 2^-22 (rms; they are of random
-// sign, each at most 2^-24 of a partial sum), a sixteenth of that margin.
-constexpr float kNear = 0x1p-18f;
+// values meet borders only by chance: where 6y / a +- near_border() rounds to
+// two codes the wave does the row again in binary64.
+//
+// near_border bounds what binary32 can do to a quotient t of at most 5 (u = 2^-24).
+// A rounding in stage k of the 7 is at most u |z|.  The 2^(7-k) values z of that
+// stage that reach an output reach as many outputs, whose mean square is theirs
+// times 2^(7-k): a is at least the norm of these z, and their roundings move the
+// output by at most u 2^((7-k)/2) a; all stages together by 24.9 u a.  RoPE's
+// three roundings per value have a norm of at most (1 + sqrt 2) u times the
+// row's, which a is not below, and reach an output through sqrt(128) of that:
+// 27.3 u a.  With c u a for y and for a, 2 u t for the division and the product
+// and 4 u for the sum with the margin, t is off by (11 c + 14) u:
+//   rotated 288 u, after RoPE 589 u; RoPE alone (c = 2.42, a at least a pair's larger one) 41 u.
+// The rms is about 4 u; rows made for it reach 80 u.
+// The margin sends 1 wave in 34 (1 in 17 after RoPE) through binary64: append
+// of 21845 tokens, K and V rotated, 40 us; a margin of 64 u took 37 and gave such
+// rows other codes.
+template <bool ROPE, bool HAD>
+__host__ __device__ constexpr float near_border() {
+  return !HAD ? 0x1p-18f : ROPE ? 0x1.3p-15f : 0x1.3p-16f;   // 64 u, 608 u, 304 u
+}
 
 // (lane: the lane's block of channels; a rotated row in binary32 comes times row_sign(lane))
 template <typename F, int D, bool ROPE, bool HAD>
@@ -344,7 +360,7 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
   for (int i = 0; i < 8; ++i) {
     const float t = y[i] * inv;
     if constexpr (ROPE || HAD) {
-      const float by = copysignf(kNear, t);
+      const float by = copysignf(near_border<ROPE, HAD>(), t);
       hi[i] = t + by;
       lo[i] = t - by;
     } else {
@@ -364,17 +380,18 @@ __device__ __forceinline__ uint32_t quantise(const float (&x)[8], const float (&
       zm = fmax(zm, lane_xor<2>(zm));
       zm = fmax(zm, lane_xor<7>(zm));
       if constexpr (D == 128) zm = fmax(zm, lane_xor<8>(zm));
-      // the code is 2 |t| rounded by its own step; borders and ties as above
-      float fix[8];
+      // 6 |z| against the borders times the maximum: no division, and a tie stays one
+      constexpr double border[7] = {0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0};
+      code = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const double t = dead ? 0.0 : z[i] * 6.0 / zm, u = fabs(t);
-        const float q = (u > 0.25 ? 0.5f : 0.0f) + (u >= 0.75 ? 0.5f : 0.0f) + (u > 1.25 ? 0.5f : 0.0f) +
-                        (u >= 1.75 ? 0.5f : 0.0f) + (u > 2.5 ? 1.0f : 0.0f) + (u >= 3.5 ? 1.0f : 0.0f) +
-                        (u > 5.0 ? 2.0f : 0.0f);
-        fix[i] = t < 0.0 ? -q : q;
+        const double u = fabs(z[i]) * 6.0;
+        uint32_t c = z[i] < 0.0 ? 8u : 0u;
+#pragma unroll
+        for (int k = 0; k < 7; ++k) c += k % 2 ? u >= border[k] * zm : u > border[k] * zm;
+        code |= c << (4 * i);
       }
-      code = dead ? 0u : pack_fp4(fix);
+      code = dead ? 0u : code;
     }
   }
   return code;

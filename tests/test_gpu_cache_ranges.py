@@ -196,3 +196,48 @@ def test_append_of_zeros_costs_what_other_values_cost(ra):
     ra.cache_append(p, padded, v, pos, cache, positions=pos, rope=rope)
     kc, _, _, _ = ref.rows(cache.cpu().numpy(), slots, page, Hkv, D)
     assert (ref.value(kc) == ref.value(want)).all()
+
+
+def _bf16(x):
+    return torch.tensor(np.asarray(x)).to(torch.bfloat16).double().numpy()
+
+
+def test_append_codes_of_rows_made_for_the_roundings_of_binary32(ra):
+    """Rows whose stage roundings all push one quotient the same way.  x_0 is about 1 (chosen so that a rounded 6 / a is
+    high too); x_1, x_2, x_4, .. lie just below half a step of it, so that each stage loses them, added in output 0 (the
+    maximum) and subtracted in output 127; the second half makes 6 y_127 / a end up just below the border 5 and keeps
+    the other outputs away from borders.  In binary32 it comes out 72 * 2^-24 above 5.  Three tokens without a slot
+    between them, so that no wave has two of them."""
+    rng = np.random.default_rng(0)
+    T, D, page, u = 4000, 128, 64, 2.0 ** -24
+    x = np.zeros((T, D))
+    first = rng.choice([1.0000440, 1.0002294, 1.0002739, 1.0004641, 1.0010260, 1.0011904], T) + rng.uniform(-1e-7, 1e-7, T)
+    first = first.astype(np.float32).astype(np.float64)   # the cosine of pair 0
+    x[:, 0] = 1
+    x[:, [2, 4, 8, 16, 32]] = 0.99609375 * u
+    x[:, 1] = 0.9921875 * u
+    lost = 5 * 0.99609375 * u + x[:, 1] * first
+    x[:, 64 + 2 ** np.arange(6)] = _bf16(4e-4 * 2.0 ** np.arange(6))
+    x[:, 71] = _bf16(rng.uniform(-3, 3, T) * u)
+    turned = x[:, 65:].sum(1)                     # of opposite signs in the two outputs
+    q = 5 * (1 - rng.uniform(0, 1e-8, T))
+    rest = (6 * (first - lost + turned) - q * (first + lost + turned)) / (6 + q)
+    for d in (64, 67, 69, 70):                    # signs alike in both outputs
+        x[:, d] = _bf16(rest)
+        rest = rest - x[:, d]
+    table = np.zeros((T, D // 2, 2), np.float32)
+    table[:, 0, 0], table[:, 1:, 0] = first, 1.0
+    pages = -(-T // page)
+    p = _params(ra, 1, 1, D, page, pages, 1, had=True)
+    k = torch.zeros(T, 4, 1, D, dtype=torch.bfloat16, device="cuda")
+    k[:, 0, 0] = torch.tensor(x).cuda()
+    assert (_f64(k[:, 0, 0]) == x).all()
+    pos = torch.full((T, 4), -1, dtype=torch.int32, device="cuda")
+    pos[:, 0] = torch.arange(T)
+    k, pos = k.flatten(0, 1), pos.flatten()
+    cache = torch.zeros((pages, ra.cache_layout(p)["page_bytes"]), dtype=torch.uint8, device="cuda")
+    ra.cache_append(p, k, k, pos, cache, positions=pos, rope=torch.from_numpy(table).cuda())
+    kc, _, _, _ = ref.rows(cache.cpu().numpy(), np.arange(T), page, 1, D)
+    want, _ = ref.codes(ref.turn(x[:, None], table) @ ref.hadamard(D))
+    bad = (ref.value(kc) != ref.value(want)).any((1, 2))
+    assert not bad.any(), f"{bad.sum()} rows"
