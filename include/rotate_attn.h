@@ -410,7 +410,8 @@ int rotate_attn_cache_read(const ra_cache_params* p, int32_t T, const void* cach
  * row of rope (NULL: q comes with its positions applied).  q is [T][Hq][D],
  * strided like k above; query head n reads KV head n / (Hq / Hkv).  o is
  * contiguous [T][Hq][D]; lse (may be NULL) is [T][Hq] binary32, the natural
- * logarithm of the softmax's denominator.  A query that sees no key gives 0
+ * logarithm of the softmax's denominator (of the keys alone: a V that is not
+ * finite makes outputs NaN, not lse).  A query that sees no key gives 0
  * and lse -infinity.  Rows outside q_start[0] .. q_start[R] are left as they
  * were.  max_q bounds the queries of a request (ones past it are not
  * computed); R, T and max_q fix the grid, so a captured graph may hold them

@@ -805,7 +805,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
   struct Scales {
     float ks[64], vs[64];
-    unsigned long long there;   // keys that are on a page
+    unsigned long long there, plain;   // keys that are on a page; those of them with a finite V
   };
   struct Buf {
     uint4 k[2][D / 8][64];
@@ -922,15 +922,16 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   auto put_scales = [&](int b) {
     if (!do_s) return;
     Scales& t = buf.sc[b & 1];
-    // a token whose scale is not finite acts through its score alone, so that
-    // it reaches the rows that see it and no others
-    const bool odd = here && !(vs < __builtin_inff());
-    const float k0 = here ? (odd ? vs : ks) : 0.0f;
-    const float v0 = here && !odd ? vs : 0.0f;
-    t.vs[lane] = v0;
-    t.ks[lane] = k0;
-    const unsigned long long all = __ballot(here);
-    if (lane == 0) t.there = all;
+    // a V scale that is not finite is left out of the sums, which it would
+    // enter times 0 for rows that do not see its token
+    const bool plain = here && fabsf(vs) < __builtin_inff();
+    t.vs[lane] = plain ? vs : 0.0f;
+    t.ks[lane] = here ? ks : 0.0f;
+    const unsigned long long all = __ballot(here), fine = __ballot(plain);
+    if (lane == 0) {
+      t.there = all;
+      t.plain = fine;
+    }
   };
   auto pin_staged = [&] {
     if constexpr (D == 128) {
@@ -1004,10 +1005,19 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         x[c][r + 3] = __fmaf_rn(s[c][r + 3], k4.w, -base);
       }
     }
-    const unsigned long long there = t.there;
-    if (key0 < all_lo || key0 + kBlock > all_hi || there != ~0ull) {
+    const unsigned long long plain = t.plain;
+    if (key0 < all_lo || key0 + kBlock > all_hi || plain != ~0ull) {
+      unsigned long long on = t.there & bits_below(row_hi - key0) & ~bits_below(row_lo - key0);
+      // rows that see a V that is not finite are NaN from here on (their lse is that of the keys)
+      if (__any((on & ~plain) != 0)) {
+        const float by = on & ~plain ? __builtin_nanf("") : 1.0f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[i][r] *= by;
+      }
       // the lane's keys of the tile, its own first: bit 32 c + 8 (r / 4) + r % 4
-      const unsigned long long on = (there & bits_below(row_hi - key0) & ~bits_below(row_lo - key0)) >> (4 * hh);
+      on >>= 4 * hh;
       const unsigned half[2] = {static_cast<unsigned>(on), static_cast<unsigned>(on >> 32)};
 #pragma unroll
       for (int c = 0; c < 2; ++c)

@@ -241,3 +241,26 @@ def test_append_codes_of_rows_made_for_the_roundings_of_binary32(ra):
     want, _ = ref.codes(ref.turn(x[:, None], table) @ ref.hadamard(D))
     bad = (ref.value(kc) != ref.value(want)).any((1, 2))
     assert not bad.any(), f"{bad.sum()} rows"
+
+
+@pytest.mark.parametrize("q_len,n", [(12, 150), (40, 150), (1, 9000), (70, 9000)])
+@pytest.mark.parametrize("D,dt,vhad", [(128, "bf16", False), (64, "fp16", True)])
+def test_attn_lse_is_of_the_keys_alone(ra, q_len, n, D, dt, vhad):
+    """A token whose V alone is not finite: NaN outputs of the rows that see it, their lse as if it were finite,
+    whichever kernel takes the request and however its keys are split; other rows the same bits."""
+    rng = np.random.default_rng(n + q_len)
+    p = _params(ra, 4, 2, D, 16, n // 16 + 3, n // 16 + 2, vhad=vhad, dt=dt, window=n - q_len // 2)
+    cache, table = _filled(ra, p, rng, [n])
+    q = torch.tensor(rng.standard_normal((q_len, 4, D))).to(DT[dt]).cuda()
+    bad = [3, n - 1 - q_len // 3]            # out of the later rows' window, behind the earlier rows
+    odd = cache.copy()
+    for t, v in zip(bad, (np.nan, np.inf)):
+        _scales(odd, p)[table[0, t // 16], :, 1, t % 16] = v
+    plain, got = (_run(ra, p, q, c, table, n, dt) for c in (cache, odd))
+    pos = n - q_len + np.arange(q_len)
+    sees = np.zeros(q_len, bool)
+    for t in bad:
+        sees |= (t <= pos) & (t > pos - p.window)
+    assert torch.isnan(got[0][sees]).all()
+    assert torch.equal(got[0][~sees], plain[0][~sees])
+    assert torch.isfinite(got[1]).all() and torch.equal(got[1], plain[1])
