@@ -415,7 +415,8 @@ int rotate_attn_cache_read(const ra_cache_params* p, int32_t T, const void* cach
  * and lse -infinity.  Rows outside q_start[0] .. q_start[R] are left as they
  * were.  max_q bounds the queries of a request (ones past it are not
  * computed); R, T and max_q fix the grid, so a captured graph may hold them
- * larger than a replay needs.
+ * larger than a replay needs.  R * Hkv + T * Hq / 128 must stay below 2^24 - 4096
+ * (work-items of one launch).
  * Workspace: cache_workspace_size bytes, 256-byte aligned; its contents do not
  * matter before or after. */
 int rotate_attn_cache_workspace_size(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, size_t* bytes);

@@ -102,6 +102,16 @@ int check_counts(int32_t R, int32_t T) {
   return RA_OK;
 }
 
+// A launch holds 2^32 work-items along the grid, 256 per workgroup: a request's
+// tiles of 128 rows (or its only one) for every KV head, and up to 1024 + Hkv
+// more for the parts of split ones.  Rows of a request then stay below 2^31, too.
+int check_pieces(const ra_cache_params* p, int32_t R, int32_t T) {
+  const int64_t pieces = static_cast<int64_t>(R) * p->Hkv + static_cast<int64_t>(T) * p->Hq / 128;
+  if (pieces >= (1 << 24) - 4096)
+    return set_error(RA_ERR_UNSUPPORTED, "R * Hkv + T * Hq / 128 must stay below 2^24 - 4096");
+  return RA_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -123,6 +133,7 @@ int rotate_attn_cache_workspace_size(const ra_cache_params* p, int32_t R, int32_
   int rc = validate(p);
   if (rc) return rc;
   if ((rc = check_counts(R, T))) return rc;
+  if ((rc = check_pieces(p, R, T))) return rc;
   if (max_q < 0) return set_error(RA_ERR_INVALID, "max_q must be >= 0");
   if (!bytes) return set_error(RA_ERR_INVALID, "bytes is NULL");
   size_t ml;
@@ -226,6 +237,7 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
   int rc = validate(p);
   if (rc) return rc;
   if ((rc = check_counts(R, T))) return rc;
+  if ((rc = check_pieces(p, R, T))) return rc;
   if (max_q < 0) return set_error(RA_ERR_INVALID, "max_q must be >= 0");
   if (R == 0 || T == 0 || max_q == 0) return RA_OK;
   if (max_q > T) max_q = T;
