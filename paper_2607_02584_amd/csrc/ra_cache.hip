@@ -258,7 +258,8 @@ __global__ __launch_bounds__(kPlanThreads) void k_place(PlanArgs a) {
 //   code_i = E2M1(6 y_i / a)  (nearest, ties to the even code),  scale = a / 6 / sqrt(D).
 // D / 8 lanes hold a row, 8 channels each; the larger stages of H and the
 // maximum move registers between lanes.  Bound by HBM: 4 bytes in and 1 1/16
-// out per channel of K and V together, at some 17 operations per value.
+// out per channel of K and V together, at some 28 vector operations per value
+// where both are rotated (12 of them the rotation).
 //
 // Which code a value gets is decided as 64 bits decide it.  16-bit inputs that
 // are not turned meet borders exactly (x / a = 1/8, 5/12, ...), where 6x / a

@@ -252,19 +252,21 @@ __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf
 
 // ------------------------------------------------------ few rows per request --
 //
-// A wave takes 16 NT rows and its own part of the keys, 32 per step, all in
-// registers: per 16 keys one load each of K codes, V codes and their scales,
-// S^T = K Q^T (keys as rows, so that a lane holds one query's scores), and
-// O^T += V^T P^T, for which the lane's four keys of two 16-key tiles are
-// already the eight that the product's second operand wants from it.  V's
-// first operand, eight keys of one channel, comes from the four tokens per
+// A wave takes 16 NT rows and its own part of the keys, 32 per step, in
+// registers (NT = 2 at D = 128 spills 8 of its 256): per 16 keys one load each
+// of K codes, V codes and their scales, S^T = K Q^T (keys as rows, so that a
+// lane holds one query's scores), and O^T += V^T P^T, for which the lane's four
+// keys of two 16-key tiles are already the eight that the product's second
+// operand wants from it.  V's first operand, eight keys of one channel, comes from the four tokens per
 // load by exchanging nibbles of neighbouring tokens (two operations for eight
 // codes) before the conversion.
 //
-// Q (scaled) and P * (V's scale) are each the sum of two bf16 values, 16 bits
-// over the whole range of the scales: the matrix cores have time for both, and
-// outputs are as exact as binary32 sums before their own rounding.  (P in one
-// value saved 2 % of a decode step and added half again to a bf16 output's error.)
+// Q (scaled) and P * (V's scale) are each the sum of two bf16 values, within
+// 2^-17 of each element over the whole range of the scales: the matrix cores
+// have time for both.  Binary32 outputs come out 5e-6 off (relative, over 130k
+// keys), lse 4e-5 at most; binary32 products throughout give 6e-7 and 3e-6,
+// which 16-bit outputs do not show.  (P in one value saved 2 % of a decode step
+// and added half again to a bf16 output's error.)
 //
 // Bound by HBM, (D + 8) bytes per token and KV head, with the vector units
 // close behind: about 235 operations per step, 80 of them conversions of codes.  The
@@ -706,8 +708,9 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 //
 // Q (after RoPE, rotation and scale, in binary32) is the sum of two bf16
 // values, within 2^-17 of each element.  P * (V's scale) is one, within 2^-8,
-// where the output is bf16, and two (LO) where the output is finer: two there
-// too took prompts of 26k tokens from 2.1 to 2.6 ms.  Both are bf16 for binary16
+// where the output is bf16, which is then 2.3e-3 off (relative) instead of
+// 1.7e-3, and two (LO) where the output is finer, 5e-6 off before its rounding:
+// prompts of 26k tokens take 2.0 ms with one and 2.5 ms with two.  Both are bf16 for binary16
 // inputs as well, whose range holds neither a scaled Q (the softmax scale is
 // the caller's) nor a weight up to 2^8 times a scale from 2^-100 to 2^127: in
 // units of a tile's largest scale, binary16 loses the rows that do not see that
