@@ -62,7 +62,15 @@ def _uses(t, regs):
     if "mfma" not in t:
         return bool(_regs(t) & regs)
     dst, a, b, c = [_regs(x) for x in t.split(None, 1)[1].split(",")[:4]]
-    return bool((a | b) & regs) or (bool(c & regs) and c != regs) or (bool(dst & regs) and dst != regs)
+    return bool((a | b) & regs) or (c != regs and (bool(c & regs) or (bool(dst & regs) and dst != regs)))
+
+
+def _takes_over(t, regs):
+    """The next product of a chain (its sum may go to other registers, which is in order), or a new result."""
+    if "mfma" not in t:
+        return False
+    dst, _, _, c = [_regs(x) for x in t.split(None, 1)[1].split(",")[:4]]
+    return c == regs or dst == regs
 
 
 def _nearest(blocks, succ, name, at, regs, need):
@@ -84,8 +92,8 @@ def _nearest(blocks, succ, name, at, regs, need):
             if _uses(t, regs):
                 best = d if best is None else min(best, d)
                 break
-            if "mfma" in t and _regs(t.split(",")[0]) == regs:
-                break                    # the next product of a chain, or a new result
+            if _takes_over(t, regs):
+                break
             d += int(t.split()[1], 0) + 1 if t.startswith("s_nop") else 1
             if t.startswith(("s_branch", "s_cbranch")):
                 todo.append((t.split()[-1], 0, d))
@@ -148,6 +156,9 @@ def test_the_walk_takes_a_chain_as_one():
     chain = [P16, "\tv_mfma_f32_16x16x32_bf16 v[2:5], v[6:9], v[10:13], v[2:5]", "\ts_nop 7", "\tv_mul_f32_e32 v0, v1, v3"]
     assert not _too_near(chain)
     assert _too_near(chain[:2] + ["\ts_nop 6"] + chain[3:])
+    moved = [P16, "\tv_mfma_f32_16x16x32_bf16 v[4:7], v[6:9], v[10:13], v[2:5]", "\ts_nop 7", "\tv_mul_f32_e32 v0, v1, v5"]
+    assert not _too_near(moved)
+    assert _too_near(moved[:2] + ["\ts_nop 6"] + moved[3:])
 
 
 @needs_hipcc
