@@ -416,10 +416,11 @@ int rotate_attn_cache_read(const ra_cache_params* p, int32_t T, const void* cach
  * were.  max_q bounds the queries of a request (ones past it are not
  * computed); R, T and max_q fix the grid, so a captured graph may hold them
  * larger than a replay needs.
- * Precision: sums and statistics are binary32; the scaled queries, and the
- * weights times V's scales, go to the matrix cores as two bf16 values (2^-17 of
- * each), but the latter as one (2^-8) where o is bf16 and the request has more
- * than 32 rows (queries times Hq / Hkv): ask for FP16 or FP32 outputs for more.
+ * Precision: sums and statistics are binary32.  With FP32 outputs o and lse are
+ * as exact as binary32 arithmetic throughout.  With 16-bit ones the scaled
+ * queries, and the weights times V's scales, go to the matrix cores as two bf16
+ * values (2^-17 of each), but the latter as one (2^-8) where o is bf16 and the
+ * request has more than 32 rows (queries times Hq / Hkv).
  * Limits: R * Hkv + T * Hq / 128 must stay below 2^24 - 4096
  * (work-items of one launch).
  * Workspace: cache_workspace_size bytes, 256-byte aligned; its contents do not

@@ -20,7 +20,7 @@ namespace {
 
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef unsigned v4u __attribute__((ext_vector_type(4)));
+typedef _Float16 v8h __attribute__((ext_vector_type(8)));
 
 constexpr float kNegInf = -__builtin_inff();
 constexpr float kLn2 = 0.693147180559945309417232121458f;
@@ -253,7 +253,7 @@ __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf
 // ------------------------------------------------------ few rows per request --
 //
 // A wave takes 16 NT rows and its own part of the keys, 32 per step, in
-// registers (NT = 2 at D = 128 spills 8 of its 256): per 16 keys one load each
+// registers (NT = 2 at D = 128 spills 12 of its 256): per 16 keys one load each
 // of K codes, V codes and their scales, S^T = K Q^T (keys as rows, so that a
 // lane holds one query's scores), and O^T += V^T P^T, for which the lane's four
 // keys of two 16-key tiles are already the eight that the product's second
@@ -263,10 +263,10 @@ __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf
 //
 // Q (scaled) and P * (V's scale) are each the sum of two bf16 values, within
 // 2^-17 of each element over the whole range of the scales: the matrix cores
-// have time for both.  Binary32 outputs come out 5e-6 off (relative, over 130k
-// keys), lse 4e-5 at most; binary32 products throughout give 6e-7 and 3e-6,
-// which 16-bit outputs do not show.  (P in one value saved 2 % of a decode step
-// and added half again to a bf16 output's error.)
+// have time for both.  Outputs are 5e-6 off before their rounding (relative, over
+// 130k keys) and lse 4e-5 at most; binary32 products throughout give 6e-7 and
+// 3e-6, which 16-bit outputs do not show.  (P in one value saved 2 % of a decode
+// step and added half again to a bf16 output's error.)
 //
 // Bound by HBM, (D + 8) bytes per token and KV head, with the vector units
 // close behind: about 235 operations per step, 80 of them conversions of codes.  The
@@ -320,24 +320,67 @@ __device__ __forceinline__ v2bf codes2(uint32_t w) { return __builtin_amdgcn_cvt
 __device__ __forceinline__ v8bf join(v2bf a, v2bf b, v2bf c, v2bf d) {
   return v8bf{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-__device__ __forceinline__ v8bf codes8(uint32_t w) { return join(codes2<0>(w), codes2<1>(w), codes2<2>(w), codes2<3>(w)); }
 
 constexpr uint32_t kLow = 0x0f0f0f0fu;
 // nibbles of two tokens: channel pairs' even / odd channels, token 0 low
 __device__ __forceinline__ uint32_t even_of(uint32_t a, uint32_t b) { return (a & kLow) | ((b << 4) & ~kLow); }
 __device__ __forceinline__ uint32_t odd_of(uint32_t a, uint32_t b) { return ((a >> 4) & kLow) | (b & ~kLow); }
 
-// x = hi + lo, both bf16
-__device__ __forceinline__ void split_bf16(float x, __bf16& hi, __bf16& lo) {
-  hi = static_cast<__bf16>(x);
-  lo = static_cast<__bf16>(x - static_cast<float>(hi));
+// ---- binary32 outputs (FINE) ----
+//
+// Two bf16 values of Q and P would show in binary32 outputs.  There Q is two
+// binary16 values, 2^-23 of each element (and 2^-39 of the row's largest), of
+// the row times the power of two that brings its largest to [2^14, 2^15); K's
+// codes are exact in either type, and the power goes back with K's scale.  P *
+// (V's scale), whose range no row bounds, is three bf16 values.  Outputs are
+// then 4e-7 off and lse 4e-6 at most, no more than with binary32 products; 64
+// requests of 564k keys take 140 us (135 with two bf16 values of both), prompts
+// of 26k tokens 3.0 ms (2.5).
+__device__ __forceinline__ float row_power(float largest) {
+  const int up = 141 - static_cast<int>((__float_as_uint(largest) >> 23) & 0xff);
+  return __uint_as_float(static_cast<uint32_t>(127 + (up > 120 ? 120 : up)) << 23);
+}
+__device__ __forceinline__ float inverse_power(float power) { return __uint_as_float((254u << 23) - __float_as_uint(power)); }
+
+// x = hi + lo, both of the 16-bit type, for each of eight values.  What is left
+// over is taken from hi's bits: another conversion may round a tie the other way.
+__device__ __forceinline__ void split8(const float* x, bool fp16, uint4& hi, uint4& lo) {
+  uint32_t h[4], l[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    h[e] = pack16(x[2 * e], x[2 * e + 1], fp16);
+    pin(h[e]);
+    l[e] = pack16(x[2 * e] - cache_h2f(static_cast<uint16_t>(h[e] & 0xffff), fp16),
+                  x[2 * e + 1] - cache_h2f(static_cast<uint16_t>(h[e] >> 16), fp16), fp16);
+  }
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+  lo = make_uint4(l[0], l[1], l[2], l[3]);
+}
+
+// codes, two per 32 bits, as either 16-bit type
+template <bool F16, int B>
+__device__ __forceinline__ uint32_t codes2_bits(uint32_t w) {
+  if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, 1.0f, B));
+  else return __builtin_bit_cast(uint32_t, codes2<B>(w));
+}
+template <bool F16>
+__device__ __forceinline__ uint4 codes8(uint32_t w) {
+  return make_uint4(codes2_bits<F16, 0>(w), codes2_bits<F16, 1>(w), codes2_bits<F16, 2>(w), codes2_bits<F16, 3>(w));
+}
+template <bool FINE>
+__device__ __forceinline__ v4f score16(uint4 k, uint4 q, v4f c) {
+  if constexpr (FINE)
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(v8h, k), __builtin_bit_cast(v8h, q), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(v8bf, k), __builtin_bit_cast(v8bf, q), c, 0, 0, 0);
 }
 
 // The rows' Q as the second operand of K Q^T: lane = 16 * part + row, its
-// D / 4 channels from part * D / 4 on, after RoPE and rotation.
-template <int D>
-__device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
-                                       v8bf (&hi)[D / 32], v8bf (&lo)[D / 32]) {
+// D / 4 channels from part * D / 4 on, after RoPE and rotation.  Returns what
+// the row's scores are to be multiplied by.
+template <int D, bool FINE>
+__device__ __forceinline__ float load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
+                                        uint4 (&hi)[D / 32], uint4 (&lo)[D / 32]) {
   constexpr int N = D / 4;
   const int part = lane >> 4;
   const bool ok = row < p.q.ql * a.G;
@@ -373,14 +416,20 @@ __device__ __forceinline__ void load_q(const CacheAttnArgs& a, const Piece& p, i
     butterfly_lanes<32>(y, lane);
   }
 #pragma unroll
-  for (int c = 0; c < D / 32; ++c)
+  for (int e = 0; e < N; ++e) y[e] *= a.c;   // scores come out in base 2
+  float power = 1.0f;
+  if constexpr (FINE) {
+    float m = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      __bf16 x0, x1;
-      split_bf16(y[8 * c + e] * a.c, x0, x1);   // scores come out in base 2
-      hi[c][e] = x0;
-      lo[c][e] = x1;
-    }
+    for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(y[e]));
+    m = fmaxf(m, lane_xor<16>(m));
+    power = row_power(fmaxf(m, lane_xor<32>(m)));
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] *= power;
+  }
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) split8(y + 8 * c, FINE, hi[c], lo[c]);
+  return inverse_power(power);
 }
 
 template <int D>
@@ -400,6 +449,7 @@ template <int D, int NT>
 struct Rows {
   v4f o[NT][D / 16];
   float m[NT], l[NT];
+  float back[NT];       // FINE: what scores are multiplied by
   int hi[NT], lo[NT];   // keys that the lane's row sees: [lo, hi)
 };
 
@@ -410,8 +460,8 @@ struct Rows {
 // first use of its result: the compiler then leaves out the wait states that
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
-template <int D, int NT, int N, int KT>
-__device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
+template <int D, int NT, int N, int KT, bool FINE>
+__device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
                                           int g) {
   constexpr int KC = D / 32;
   v4f s[N][KT];
@@ -421,11 +471,11 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
     for (int nt = 0; nt < N; ++nt) s[nt][i] = v4f{0, 0, 0, 0};
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      const v8bf k = codes8(dword_of<D>(t[i].k, c));
+      const uint4 k = codes8<FINE>(dword_of<D>(t[i].k, c));
 #pragma unroll
       for (int nt = 0; nt < N; ++nt) {
-        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, sq[(nt * KC + c) * 128], s[nt][i], 0, 0, 0);
-        s[nt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, sq[(nt * KC + c) * 128 + 64], s[nt][i], 0, 0, 0);
+        s[nt][i] = score16<FINE>(k, sq[(nt * KC + c) * 128], s[nt][i]);
+        s[nt][i] = score16<FINE>(k, sq[(nt * KC + c) * 128 + 64], s[nt][i]);
       }
     }
     const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
@@ -433,10 +483,11 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
     for (int nt = 0; nt < N; ++nt) {
       const float base = x.m[nt] == kNegInf ? 0.0f : x.m[nt];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[nt][i][e] = __fmaf_rn(s[nt][i][e], ks[e], -base);
+      for (int e = 0; e < 4; ++e) s[nt][i][e] = __fmaf_rn(s[nt][i][e], FINE ? ks[e] * x.back[nt] : ks[e], -base);
     }
   }
-  v8bf ph[N][KT / 2], pl[N][KT / 2];
+  constexpr int PN = FINE ? 3 : 2;
+  v8bf pw[N][KT / 2][PN];
 #pragma unroll
   for (int nt = 0; nt < N; ++nt) {
     unsigned seen = 0xffff;   // bit 4 i + e: this lane's row sees key 16 i + 4 g + e of the step
@@ -482,10 +533,12 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
         float w = pr * vs[e];
         // a scale that is not finite must not reach rows that do not see its token
         if (!whole) w = (seen >> (4 * i + e)) & 1 ? w : 0.0f;
-        __bf16 x0, x1;
-        split_bf16(w, x0, x1);
-        ph[nt][i / 2][4 * (i % 2) + e] = x0;
-        pl[nt][i / 2][4 * (i % 2) + e] = x1;
+#pragma unroll
+        for (int z = 0; z < PN; ++z) {   // w = their sum
+          const __bf16 y = static_cast<__bf16>(w);
+          pw[nt][i / 2][z][4 * (i % 2) + e] = y;
+          w -= static_cast<float>(y);
+        }
       }
     }
   }
@@ -514,10 +567,10 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
       if constexpr (D == 128) v = join(codes2<B>(n[0]), codes2<B>(n[1]), codes2<B>(n[2]), codes2<B>(n[3]));
       else v = join(codes2<B>(n[0]), codes2<B + 2>(n[0]), codes2<B>(n[1]), codes2<B + 2>(n[1]));
 #pragma unroll
-      for (int nt = 0; nt < N; ++nt) {
-        x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, ph[nt][u], x.o[nt][e], 0, 0, 0);
-        x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pl[nt][u], x.o[nt][e], 0, 0, 0);
-      }
+      for (int nt = 0; nt < N; ++nt)
+#pragma unroll
+        for (int z = 0; z < PN; ++z)
+          x.o[nt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, pw[nt][u][z], x.o[nt][e], 0, 0, 0);
     };
     pv(std::integral_constant<int, 0>{}, ev, 0);
     pv(std::integral_constant<int, 0>{}, od, 1);
@@ -532,14 +585,15 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const v8bf* sq, const T
   }
 }
 
-template <int D, int NT, int KT>
-__global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
+template <int D, int NT, int KT, bool FINE>
+__device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
   __shared__ __align__(16) float so[4][16][kStride];
   __shared__ float sm[4][M], sl[4][M];
   __shared__ SchedShared sched;
-  __shared__ __align__(16) v8bf sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
+  __shared__ __align__(16) uint4 sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
+  __shared__ float sback[FINE ? M : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
   // heads fastest: the heads of a page, neighbours in memory, are read together
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
@@ -605,8 +659,9 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   for (int nt = 0; nt < NT; ++nt) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
     if (w == nt) {   // one wave for all four
-      v8bf qh[D / 32], ql[D / 32];
-      load_q<D>(a, p, h, row, lane, qh, ql);
+      uint4 qh[D / 32], ql[D / 32];
+      const float back = load_q<D, FINE>(a, p, h, row, lane, qh, ql);
+      if (FINE && lane < 16) sback[nt * 16 + lane] = back;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         sq_all[(nt * (D / 32) + c) * 128 + lane] = qh[c];
@@ -623,6 +678,8 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
     for (int e = 0; e < E; ++e) x.o[nt][e] = v4f{0, 0, 0, 0};
   }
   __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) x.back[nt] = FINE ? sback[nt * 16 + (lane & 15)] : 1.0f;
   auto whole = [&](int b, unsigned there) {
     return b * kStep >= all_lo && b * kStep + kStep <= all_hi && b * kStep + kStep <= p.q.n && there == (1u << KT) - 1;
   };
@@ -636,7 +693,7 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
         if (b + i >= w1) break;
         there[i ^ 1] = load(b + i + 1 < w1 ? b + i + 1 : w1 - 1, ring[i ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
-        few_step<D, NT, N, KT>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
+        few_step<D, NT, N, KT, FINE>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
       }
     }
   };
@@ -695,6 +752,15 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
   }
 }
 
+template <int D, int NT, int KT>
+__global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
+  few_rows<D, NT, KT, false>(a);
+}
+template <int D, int NT, int KT>
+__global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
+  few_rows<D, NT, KT, true>(a);
+}
+
 // --------------------------------------------------------- many rows per request --
 //
 // Bound by the matrix cores and the softmax beside them.  NW waves of 32 rows
@@ -709,12 +775,12 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 // Q (after RoPE, rotation and scale, in binary32) is the sum of two bf16
 // values, within 2^-17 of each element.  P * (V's scale) is one, within 2^-8,
 // where the output is bf16, which is then 2.3e-3 off (relative) instead of
-// 1.7e-3, and two (LO) where the output is finer, 5e-6 off before its rounding:
-// prompts of 26k tokens take 2.0 ms with one and 2.5 ms with two.  Both are bf16 for binary16
-// inputs as well, whose range holds neither a scaled Q (the softmax scale is
-// the caller's) nor a weight up to 2^8 times a scale from 2^-100 to 2^127: in
-// units of a tile's largest scale, binary16 loses the rows that do not see that
-// token.
+// 1.7e-3, and two (LO) where it is binary16: prompts of 26k tokens take 2.0 ms
+// with one and 2.5 ms with two.  (Binary32 outputs: FINE, above.)  Both are bf16
+// for binary16 inputs as well, whose range holds neither a scaled Q (the softmax
+// scale is the caller's) nor a weight up to 2^8 times a scale from 2^-100 to
+// 2^127: in units of a tile's largest scale, binary16 loses the rows that do not
+// see that token.
 //
 // LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
 // bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
@@ -723,15 +789,20 @@ __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
 
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-__device__ __forceinline__ v16f mfma32(v8bf a, v8bf b, v16f c) {
-  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+__device__ __forceinline__ v16f mfma32(uint4 a, uint4 b, v16f c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, a), __builtin_bit_cast(v8bf, b), c, 0, 0, 0);
 }
-template <int B>
-__device__ __forceinline__ uint32_t codes2_bits(uint32_t w) { return __builtin_bit_cast(uint32_t, codes2<B>(w)); }
+template <bool FINE>
+__device__ __forceinline__ v16f score32(uint4 k, uint4 q, v16f c) {
+  if constexpr (FINE)
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(v8h, k), __builtin_bit_cast(v8h, q), c, 0, 0, 0);
+  else return mfma32(k, q, c);
+}
 
-template <int D, bool F16>
-__device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
-                                         v8bf (&hi)[D / 16], v8bf (&lo)[D / 16]) {
+// As load_q, D / 2 channels per lane.
+template <int D, bool F16, bool FINE>
+__device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
+                                          uint4 (&hi)[D / 16], uint4 (&lo)[D / 16]) {
   constexpr int N = D / 2;
   const int hh = lane >> 5;
   const bool ok = row < p.q.ql * a.G;
@@ -766,19 +837,19 @@ __device__ __forceinline__ void load_q32(const CacheAttnArgs& a, const Piece& p,
     butterfly_lanes<32>(y, lane);
   }
 #pragma unroll
-  for (int c = 0; c < N / 8; ++c) {
-    uint32_t x[4], r[4];
+  for (int e = 0; e < N; ++e) y[e] *= a.c;   // scores come out in base 2
+  float power = 1.0f;
+  if constexpr (FINE) {
+    float m = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float u = y[8 * c + 2 * e] * a.c, v = y[8 * c + 2 * e + 1] * a.c;   // scores come out in base 2
-      x[e] = pack16(u, v, false);
-      pin(x[e]);   // what is left over is taken from these bits: another conversion may round a tie the other way
-      r[e] = pack16(u - cache_h2f(static_cast<uint16_t>(x[e] & 0xffff), false),
-                    v - cache_h2f(static_cast<uint16_t>(x[e] >> 16), false), false);
-    }
-    hi[c] = __builtin_bit_cast(v8bf, make_uint4(x[0], x[1], x[2], x[3]));
-    lo[c] = __builtin_bit_cast(v8bf, make_uint4(r[0], r[1], r[2], r[3]));
+    for (int e = 0; e < N; ++e) m = fmaxf(m, fabsf(y[e]));
+    power = row_power(fmaxf(m, lane_xor<32>(m)));
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] *= power;
   }
+#pragma unroll
+  for (int c = 0; c < N / 8; ++c) split8(y + 8 * c, FINE, hi[c], lo[c]);
+  return inverse_power(power);
 }
 
 // The lowest n bits (n below 0: none, above 64: all).
@@ -802,8 +873,10 @@ __device__ __forceinline__ void each(F&& f) {
 // matrix cores beside the next chunk's probabilities, their LDS operands read
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
-template <int D, bool F16, bool LO>
-__global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
+// TERMS: bf16 values that hold P * (V's scale); three come with binary16 pairs of Q.
+template <int D, bool F16, int TERMS>
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
+  constexpr bool FINE = TERMS == 3;
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
   struct Scales {
@@ -904,7 +977,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     if constexpr (c < D / 32) {
       const uint32_t x = dword_of<D>(sk, c);
       buf.k[b & 1][(lane >> 4) * (D / 32) + c][mine + (lane & 15)] =
-          make_uint4(codes2_bits<0>(x), codes2_bits<1>(x), codes2_bits<2>(x), codes2_bits<3>(x));
+          codes8<FINE>(x);
     }
   };
   auto put_v = [&](int b, auto part) {   // channels E / 4 * part .. of the lane's chunk
@@ -914,12 +987,12 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     if constexpr (D == 128) {
       const uint32_t e01 = even_of(sv.x, sv.y), e23 = even_of(sv.z, sv.w), o01 = odd_of(sv.x, sv.y),
                      o23 = odd_of(sv.z, sv.w);
-      dst[2 * c * 32] = make_uint2(codes2_bits<c>(e01), codes2_bits<c>(e23));
-      dst[(2 * c + 1) * 32] = make_uint2(codes2_bits<c>(o01), codes2_bits<c>(o23));
+      dst[2 * c * 32] = make_uint2(codes2_bits<false, c>(e01), codes2_bits<false, c>(e23));
+      dst[(2 * c + 1) * 32] = make_uint2(codes2_bits<false, c>(o01), codes2_bits<false, c>(o23));
     } else {
       const uint32_t t02 = (sv.x & 0xffffu) | (sv.y << 16), t13 = (sv.x >> 16) | (sv.y & 0xffff0000u);
       const uint32_t n = c % 2 ? odd_of(t02, t13) : even_of(t02, t13);
-      dst[c * 32] = make_uint2(codes2_bits<c / 2>(n), codes2_bits<c / 2 + 2>(n));
+      dst[c * 32] = make_uint2(codes2_bits<false, c / 2>(n), codes2_bits<false, c / 2 + 2>(n));
     }
   };
   auto put_scales = [&](int b) {
@@ -957,8 +1030,8 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     entries(b0, b0);
     ask(b0, b0);
   }
-  v8bf q[KC], q_lo[KC];
-  load_q32<D, F16>(a, p, h, row, lane, q, q_lo);
+  uint4 q[KC], q_lo[KC];
+  const float back = load_q32<D, F16, FINE>(a, p, h, row, lane, q, q_lo);
   v16f o[MT], s[2];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -981,9 +1054,9 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
-      const v8bf k = __builtin_bit_cast(v8bf, k_op(b0, c, kc));
-      s[c] = mfma32(k, q[kc], s[c]);
-      s[c] = mfma32(k, q_lo[kc], s[c]);
+      const uint4 k = k_op(b0, c, kc);
+      s[c] = score32<FINE>(k, q[kc], s[c]);
+      s[c] = score32<FINE>(k, q_lo[kc], s[c]);
     }
     settle(s[c]);
   }
@@ -1001,7 +1074,8 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
     for (int c = 0; c < 2; ++c) {
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
-        const float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
+        float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
+        if constexpr (FINE) k4.x *= back, k4.y *= back, k4.z *= back, k4.w *= back;
         x[c][r] = __fmaf_rn(s[c][r], k4.x, -base);
         x[c][r + 1] = __fmaf_rn(s[c][r + 1], k4.y, -base);
         x[c][r + 2] = __fmaf_rn(s[c][r + 2], k4.z, -base);
@@ -1052,7 +1126,7 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         for (int r = 0; r < 16; ++r) o[i][r] *= alpha;
     }
 
-    uint32_t pw[2][8], pl[2][LO ? 8 : 1];
+    uint32_t pw[2][TERMS][8];
     float ls[4] = {0, 0, 0, 0};
     auto v_scales = [&](int n) { return *reinterpret_cast<const float4*>(&t.vs[8 * n + 4 * hh]); };
     float4 v4 = v_scales(0);   // read a group ahead
@@ -1067,14 +1141,17 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         y[e] = pr * vv[e];
       }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        uint32_t u = pack16(y[2 * e], y[2 * e + 1], false);
-        if constexpr (LO) pin(u);   // as in load_q32
-        pw[c][2 * r4 + e] = u;
-        if constexpr (LO)
-          pl[c][2 * r4 + e] = pack16(y[2 * e] - cache_h2f(static_cast<uint16_t>(u & 0xffff), false),
-                                     y[2 * e + 1] - cache_h2f(static_cast<uint16_t>(u >> 16), false), false);
-      }
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int z = 0; z < TERMS; ++z) {   // y = the sum of the terms
+          uint32_t u = pack16(y[2 * e], y[2 * e + 1], false);
+          if (z + 1 < TERMS) {
+            pin(u);   // what is left over is taken from these bits, not from a second conversion
+            y[2 * e] -= cache_h2f(static_cast<uint16_t>(u & 0xffff), false);
+            y[2 * e + 1] -= cache_h2f(static_cast<uint16_t>(u >> 16), false);
+          }
+          pw[c][z][2 * r4 + e] = u;
+        }
     };
     // products of chunk c, in turn: one of the 2 MT of P V (step n / MT, tile n %
     // MT), one of the KC score products of chunk c of the next tile, whose sum
@@ -1099,19 +1176,17 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
         uint4& op = ops[(c * NP + i) % kAhead];
         if constexpr (i % 2 == 0) {
           constexpr int st = i / 2 / MT;
-          const v8bf v = __builtin_bit_cast(v8bf, op);
-          auto four = [&](const uint32_t* w) {
-            return __builtin_bit_cast(v8bf, make_uint4(w[4 * st], w[4 * st + 1], w[4 * st + 2], w[4 * st + 3]));
-          };
-          o[i / 2 % MT] = mfma32(v, four(pw[c]), o[i / 2 % MT]);
-          if constexpr (LO) o[i / 2 % MT] = mfma32(v, four(pl[c]), o[i / 2 % MT]);
+#pragma unroll
+          for (int z = 0; z < TERMS; ++z) {
+            const uint32_t* w = pw[c][z] + 4 * st;
+            o[i / 2 % MT] = mfma32(op, make_uint4(w[0], w[1], w[2], w[3]), o[i / 2 % MT]);
+          }
         } else {
           if constexpr (i == 1)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-          const v8bf k = __builtin_bit_cast(v8bf, op);
-          s[c] = mfma32(k, q[i / 2], s[c]);
-          s[c] = mfma32(k, q_lo[i / 2], s[c]);
+          s[c] = score32<FINE>(op, q[i / 2], s[c]);
+          s[c] = score32<FINE>(op, q_lo[i / 2], s[c]);
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
@@ -1183,6 +1258,15 @@ __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
       }
     }
   }
+}
+
+template <int D, bool F16, bool LO>
+__global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
+  many_rows<D, F16, LO ? 2 : 1>(a);
+}
+template <int D, bool F16>
+__global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
+  many_rows<D, F16, 3>(a);
 }
 
 // Joins the parts of split tiles, a workgroup for per_group rows: up to eight
@@ -1313,15 +1397,20 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   g.tiles = a.R;   // a request of few rows is one tile
   g.merges = g.tiles < a.target ? g.tiles : a.target;
   const dim3 grid(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv));
-  k_few<D, NT, 2><<<grid, dim3(256), 0, s>>>(a);
+  if (a.out_dtype == RA_FP32) k_fine_few<D, NT, 2><<<grid, dim3(256), 0, s>>>(a);
+  else k_few<D, NT, 2><<<grid, dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, M>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
 }
 
-template <int D, bool F16, bool LO>
+template <int D, bool F16>
 hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
   const Grid g = grid_of(a, kRowTile, a.target_rows);
-  k_rows<D, F16, LO><<<dim3(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv)), dim3(256), 0, s>>>(a);
+  const dim3 grid(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv));
+  // P in as many bf16 values as the output shows
+  if (a.out_dtype == RA_FP32) k_fine_rows<D, F16><<<grid, dim3(256), 0, s>>>(a);
+  else if (a.out_dtype == RA_FP16) k_rows<D, F16, true><<<grid, dim3(256), 0, s>>>(a);
+  else k_rows<D, F16, false><<<grid, dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, kRowTile>(a, g, a.target_rows, static_cast<int64_t>(a.max_q) * a.G, s);
 }
@@ -1333,10 +1422,7 @@ hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
   hipError_t e = hipSuccess;
   if (a.G <= kFewRows) e = few<D, 2>(a, s);   // requests of few rows; with more heads than that there are none
   if (e != hipSuccess || most <= kFewRows) return e;
-  // P in one bf16 value where the output is no finer than that
-  const bool lo = a.out_dtype != RA_BF16;
-  if (a.is_fp16) return lo ? rows<D, true, true>(a, s) : rows<D, true, false>(a, s);
-  return lo ? rows<D, false, true>(a, s) : rows<D, false, false>(a, s);
+  return a.is_fp16 ? rows<D, true>(a, s) : rows<D, false>(a, s);
 }
 
 int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }

@@ -264,3 +264,48 @@ def test_attn_lse_is_of_the_keys_alone(ra, q_len, n, D, dt, vhad):
     assert torch.isnan(got[0][sees]).all()
     assert torch.equal(got[0][~sees], plain[0][~sees])
     assert torch.isfinite(got[1]).all() and torch.equal(got[1], plain[1])
+
+
+def _binary32(p, q, cache, table, n):
+    """The definition in elementary binary32 operations (torch, on the host): outputs and lse."""
+    f = torch.float32
+    k, v = (torch.tensor(x).to(f) for x in _dense(cache, table, p, n))
+    H = torch.tensor(ref.hadamard(p.D) / np.sqrt(p.D)).to(f)
+    x, G, m = q.cpu().to(f), p.Hq // p.Hkv, q.shape[0]
+    pos, key = n - m + torch.arange(m)[:, None], torch.arange(n)[None, :]
+    out, lse = torch.empty(m, p.Hq, p.D), torch.empty(m, p.Hq)
+    for h in range(p.Hq):
+        y = x[:, h] @ H if p.rotation else x[:, h]
+        s = (y @ k[:, h // G].T.contiguous()) * np.float32(p.D ** -0.5)
+        s = torch.where(key <= pos, s, -torch.inf)
+        top = s.max(1, keepdim=True).values
+        w = torch.exp(s - top)
+        l = w.sum(1, keepdim=True)
+        y = (w @ v[:, h // G].contiguous()) / l
+        out[:, h] = y @ H if p.v_rotation else y
+        lse[:, h] = (top + torch.log(l))[:, 0]
+    return out.double().numpy(), lse.double().numpy()
+
+
+@pytest.mark.parametrize("q_len,n", [(1, 700), (6, 700), (13, 300), (40, 300), (150, 700), (1, 20000), (20, 9000)])
+@pytest.mark.parametrize("D,dt,had,vhad,gain", [(128, "bf16", True, False, 1.5), (64, "fp16", False, True, 4.0),
+                                                (128, "fp16", False, False, 3e-3)])
+def test_attn_binary32_outputs_are_as_exact_as_binary32_arithmetic(ra, q_len, n, D, dt, had, vhad, gain):
+    """Error against 64 bits at most twice that of binary32 operations throughout (there are as many roundings, in
+    other places) and a rounding of the result; lse likewise.  Queries of a request differ by 2^40 in size."""
+    rng = np.random.default_rng(n + q_len)
+    p = _params(ra, 4, 2, D, 32, -(-n // 32) + 2, -(-n // 32) + 1, had=had, vhad=vhad, dt=dt, out="fp32")
+    cache, table = _filled(ra, p, rng, [n])
+    x = rng.standard_normal((q_len, 4, D)) * gain
+    if dt == "bf16" and q_len > 1:
+        x[0] *= 2.0 ** -40
+    q = torch.tensor(x).to(DT[dt]).cuda()
+    o, lse = _run(ra, p, q, cache, table, n, "fp32")
+    want = _want(p, q, cache, table, n)
+    _check(o, lse, want, "fp32", n, False)
+    plain, plain_lse = _binary32(p, q, cache, table, n)
+    rms = lambda a, b: np.sqrt(((a - b) ** 2).mean() / (b ** 2).mean())
+    assert rms(_f64(o), want[0]) <= 2 * rms(plain, want[0]) + 2.0 ** -24
+    # lse: in units of a rounding of scores as large as these
+    unit = 2.0 ** -24 * (1 + np.abs(want[1]).max() + want[3].max())
+    assert np.abs(_f64(lse) - want[1]).max() <= 2 * np.abs(plain_lse - want[1]).max() + 4 * unit
