@@ -432,6 +432,77 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
                            const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/* ---- pages: requests that begin alike, are rolled back, or run on and on ----
+ *
+ * A page may be held by several requests.  page_refs[page] counts its holders
+ * beyond the first: 0 for a page of one request, and for a free one.  cache_plan
+ * neither reads nor writes it (a page from the stack has one holder), but its
+ * `release` gives back every page of a request: requests that share pages, or
+ * whose window lost some, are ended by cache_trim instead.
+ *
+ * Each operator takes the tables as they are and leaves them as `out` says: NULL,
+ * or the same pointer again, is in place; an array of its own gets the whole new state (so
+ * that a step which still reads the old tables goes on).  Arrays must not overlap
+ * otherwise.  Nothing is allocated; sizes and launches depend on R, n and the
+ * params alone, so that a captured graph follows the tables.  Calls on the same tables,
+ * cache or workspace must be ordered by the caller (one stream, or events).
+ *
+ * status[0] is 0, or tells why the call was refused as a whole -- bit 0: a
+ * length or number of a request that is impossible, bit 2: too few free pages, bit 3:
+ * free_count impossible, bit 4 (compact): a page number on the stack that is none, or is there
+ * twice.  Then nothing has changed.  status[1 .. 3] say what was done (if
+ * status[0] is 0).  Table entries that are no page (-1: a page that a window lost) are
+ * passed over everywhere.
+ * Workspace: cache_pages_workspace_size bytes, 256-byte aligned; its contents do
+ * not matter before or after. */
+typedef struct ra_cache_tables {
+  int32_t* seq_lens;     /* [R] cached tokens */
+  int32_t* block_table;  /* [R][max_blocks] */
+  int32_t* page_refs;    /* [num_pages] */
+  int32_t* free_pages;   /* [num_pages], the top of the stack at free_count - 1 */
+  int32_t* free_count;   /* [1] */
+} ra_cache_tables;
+
+int rotate_attn_cache_pages_workspace_size(const ra_cache_params* p, int32_t R, size_t* bytes);
+
+/* Requests that begin as others do.  For each of n pairs request children[i],
+ * which holds no tokens, gets the first L tokens of request parents[i], L = lens[i]
+ * (lens may be NULL: all of them).  Full pages are shared: the child's table names them and
+ * they have one holder more.  Where L does not end with a page, the page it ends in
+ * is copied into one from the top of the stack, in order of the pairs.  A child is named
+ * once; parents may be named often, and are as they were before the call (a parent that is a child
+ * of the same call has no tokens).  Entries of a child behind its pages keep what they
+ * held.  status[1]: pages taken, [2]: entries that share a page, [3]: the longest request. */
+int rotate_attn_cache_fork(const ra_cache_params* p, int32_t R, int32_t n, const int32_t* parents,
+                           const int32_t* children, const int32_t* lens, const ra_cache_tables* tables,
+                           const ra_cache_tables* out, void* cache, void* workspace, size_t workspace_bytes,
+                           int32_t* status, void* stream);
+
+/* Tokens and pages given back.  Request r keeps its first keep[r] tokens (all of
+ * them where keep[r] is negative, or keep is NULL; 0 ends it).  Pages behind them
+ * are let go and their entries become -1.  With sinks >= 0 (which needs a window) so are the pages
+ * whose tokens all lie at `sinks` or behind and before any that a query at
+ * position keep[r] or later sees: block j with j * page_size >= sinks and
+ * (j + 1) * page_size <= keep[r] - window + 1.  Such a request is not rolled back
+ * further than the window allows.  A page that nobody holds any more goes back on the
+ * stack, in ascending order of page numbers.  Where keep[r] ends inside a page that
+ * had other holders when the call began, the request gets a copy of it in a page
+ * from the top of the stack, in order of the requests (before any page is given back), so that what it appends is its own.
+ * status[1]: pages taken for copies, [2]: pages given back, [3]: the longest request. */
+int rotate_attn_cache_trim(const ra_cache_params* p, int32_t R, const int32_t* keep, int32_t sinks,
+                           const ra_cache_tables* tables, const ra_cache_tables* out, void* cache, void* workspace,
+                           size_t workspace_bytes, int32_t* status, void* stream);
+
+/* The pages in use moved to the front of the cache.  With k = num_pages -
+ * free_count of them, the i-th in use at k or behind moves to the i-th free one
+ * before k, with its holders; entries of the requests' tables (up to their
+ * lengths) follow.  The stack then holds k .. num_pages - 1, k at its top.  Pages
+ * are in use where they are not on the stack, whether or not a table here
+ * names them.  status[1]: pages moved, [2]: k, [3]: 0. */
+int rotate_attn_cache_compact(const ra_cache_params* p, int32_t R, const ra_cache_tables* tables,
+                              const ra_cache_tables* out, void* cache, void* workspace, size_t workspace_bytes,
+                              int32_t* status, void* stream);
+
 /* Status code -> static text; and the thread-local message of the last failure
  * on the calling thread (library utilities, no paper passage). */
 const char* rotate_attn_error_string(int status);

@@ -5,9 +5,11 @@
 
 #include <cmath>
 #include <cstdio>
+#include <initializer_list>
 
 #include "../../include/rotate_attn.h"
 #include "ra_cache.h"
+#include "ra_cache_pages.h"
 
 namespace {
 
@@ -109,6 +111,80 @@ int check_pieces(const ra_cache_params* p, int32_t R, int32_t T) {
   const int64_t pieces = static_cast<int64_t>(R) * p->Hkv + static_cast<int64_t>(T) * p->Hq / 128;
   if (pieces >= (1 << 24) - 4096)
     return set_error(RA_ERR_UNSUPPORTED, "R * Hkv + T * Hq / 128 must stay below 2^24 - 4096");
+  return RA_OK;
+}
+
+struct Input {
+  const int32_t* at;
+  int64_t n;
+};
+
+// Tables of an operator on pages: every array is there, and its new state is
+// kept in place or in an array that overlaps none of the others, `inputs` included.
+int page_tables(const ra_cache_params* p, int32_t R, const ra_cache_tables* in, const ra_cache_tables* out, void* cache,
+                void* workspace, size_t workspace_bytes, int32_t* status, std::initializer_list<Input> inputs,
+                ra::PageTables* t) {
+  int rc = validate(p);
+  if (rc) return rc;
+  if ((rc = check_counts(R, 0))) return rc;
+  if (!in) return set_error(RA_ERR_INVALID, "tables is NULL");
+  if (!out) out = in;
+  const int32_t* const a[5] = {in->seq_lens, in->block_table, in->page_refs, in->free_pages, in->free_count};
+  int32_t* const b[5] = {out->seq_lens, out->block_table, out->page_refs, out->free_pages, out->free_count};
+  const int64_t pages = p->num_pages;
+  const int64_t size[6] = {R, static_cast<int64_t>(R) * p->max_blocks, pages, pages, 1, 4};
+  for (int i = 0; i < 5; ++i)
+    if ((!a[i] || !b[i]) && size[i]) return set_error(RA_ERR_INVALID, "NULL tensor pointer");
+  if (!status || !cache) return set_error(RA_ERR_INVALID, "NULL tensor pointer");
+  auto at = [](const void* x) { return reinterpret_cast<uintptr_t>(x); };
+  const size_t need = ra::cache_pages_workspace_bytes(R, p->num_pages);
+  // what is written, against everything else
+  for (int i = 0; i < 6; ++i) {
+    const int32_t* w = i < 5 ? b[i] : status;
+    const uintptr_t lo = at(w), hi = lo + 4 * size[i];
+    auto meets = [&](const void* x, uint64_t bytes) { return at(x) < hi && lo < at(x) + bytes; };
+    for (int j = 0; j < 6; ++j) {
+      const int32_t* const before = j < 5 ? a[j] : status;
+      const int32_t* const after = j < 5 ? b[j] : status;
+      const uint64_t bytes = 4 * size[j];
+      if (meets(before, bytes) && !(i == j && before == w))
+        return set_error(RA_ERR_INVALID, "tables overlap: a new state is kept in place or in an array of its own");
+      if (i != j && meets(after, bytes))
+        return set_error(RA_ERR_INVALID, "tables overlap: a new state is kept in place or in an array of its own");
+    }
+    for (const Input& x : inputs)
+      if (x.at && meets(x.at, 4 * static_cast<uint64_t>(x.n)))
+        return set_error(RA_ERR_INVALID, "an input overlaps a table that is written");
+    if (meets(cache, static_cast<uint64_t>(page_bytes(p)) * p->num_pages) || (workspace && meets(workspace, need)))
+      return set_error(RA_ERR_INVALID, "tables overlap the cache or the workspace");
+  }
+  if (!aligned(cache, 128)) return set_error(RA_ERR_INVALID, "cache must be 128-byte aligned");
+  if (!workspace) return set_error(RA_ERR_WORKSPACE, "workspace is NULL");
+  if (!aligned(workspace, 256)) return set_error(RA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (workspace_bytes < need) {
+    char msg[96];
+    std::snprintf(msg, sizeof msg, "workspace too small: need %zu bytes", need);
+    return set_error(RA_ERR_WORKSPACE, msg);
+  }
+  t->seq_in = a[0];
+  t->table_in = a[1];
+  t->refs_in = a[2];
+  t->free_in = a[3];
+  t->count_in = a[4];
+  t->seq = b[0];
+  t->table = b[1];
+  t->refs = b[2];
+  t->free = b[3];
+  t->count = b[4];
+  t->status = status;
+  t->cache = static_cast<uint8_t*>(cache);
+  t->ws = static_cast<int*>(workspace);
+  t->page_bytes = page_bytes(p);
+  t->R = R;
+  t->max_blocks = p->max_blocks;
+  t->num_pages = p->num_pages;
+  t->page = p->page_size;
+  t->page_log = log2_of(p->page_size);
   return RA_OK;
 }
 
@@ -287,6 +363,54 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
   a.vhad = p->v_rotation == RA_VROT_HADAMARD;
   a.target = a.target_rows = 0;
   return hip_status(ra::launch_cache_attn(a, p->D, static_cast<hipStream_t>(stream)), "cache_attn");
+}
+
+int rotate_attn_cache_pages_workspace_size(const ra_cache_params* p, int32_t R, size_t* bytes) {
+  int rc = validate(p);
+  if (rc) return rc;
+  if ((rc = check_counts(R, 0))) return rc;
+  if (!bytes) return set_error(RA_ERR_INVALID, "bytes is NULL");
+  *bytes = ra::cache_pages_workspace_bytes(R, p->num_pages);
+  return RA_OK;
+}
+
+int rotate_attn_cache_fork(const ra_cache_params* p, int32_t R, int32_t n, const int32_t* parents,
+                           const int32_t* children, const int32_t* lens, const ra_cache_tables* tables,
+                           const ra_cache_tables* out, void* cache, void* workspace, size_t workspace_bytes,
+                           int32_t* status, void* stream) {
+  if (n < 0 || n > R) return set_error(RA_ERR_INVALID, "n must be in [0, R]: every child is another request");
+  if (n && (!parents || !children)) return set_error(RA_ERR_INVALID, "NULL tensor pointer");
+  ra::ForkArgs a;
+  const int rc = page_tables(p, R, tables, out, cache, workspace, workspace_bytes, status,
+                             {{parents, n}, {children, n}, {lens, n}}, &a.t);
+  if (rc) return rc;
+  a.parents = parents;
+  a.children = children;
+  a.lens = lens;
+  a.n = n;
+  return hip_status(ra::launch_cache_fork(a, static_cast<hipStream_t>(stream)), "cache_fork");
+}
+
+int rotate_attn_cache_trim(const ra_cache_params* p, int32_t R, const int32_t* keep, int32_t sinks,
+                           const ra_cache_tables* tables, const ra_cache_tables* out, void* cache, void* workspace,
+                           size_t workspace_bytes, int32_t* status, void* stream) {
+  if (p && sinks >= 0 && !p->window) return set_error(RA_ERR_INVALID, "sinks are kept beside a window: there is none");
+  ra::TrimArgs a;
+  const int rc = page_tables(p, R, tables, out, cache, workspace, workspace_bytes, status, {{keep, R}}, &a.t);
+  if (rc) return rc;
+  a.keep = keep;
+  a.sinks = sinks;
+  a.window = p->window;
+  return hip_status(ra::launch_cache_trim(a, static_cast<hipStream_t>(stream)), "cache_trim");
+}
+
+int rotate_attn_cache_compact(const ra_cache_params* p, int32_t R, const ra_cache_tables* tables,
+                              const ra_cache_tables* out, void* cache, void* workspace, size_t workspace_bytes,
+                              int32_t* status, void* stream) {
+  ra::PageTables t;
+  const int rc = page_tables(p, R, tables, out, cache, workspace, workspace_bytes, status, {}, &t);
+  if (rc) return rc;
+  return hip_status(ra::launch_cache_compact(t, static_cast<hipStream_t>(stream)), "cache_compact");
 }
 
 }  // extern "C"

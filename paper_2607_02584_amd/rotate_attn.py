@@ -62,6 +62,10 @@ class CacheSizes(ctypes.Structure):
                 ("v_codes", ctypes.c_int64), ("k_scales", ctypes.c_int64), ("v_scales", ctypes.c_int64)]
 
 
+class CacheTables(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("seq_lens", "block_table", "page_refs", "free_pages", "free_count")]
+
+
 _lib = None
 
 
@@ -79,6 +83,7 @@ def lib():
         P = ctypes.c_void_p
         PP = ctypes.POINTER(Params)
         CP, I, S = ctypes.POINTER(CacheParams), ctypes.c_int32, ctypes.c_int64
+        TP = ctypes.POINTER(CacheTables)
         sig = {
             "rotate_attn_layout": [PP, ctypes.POINTER(Layout)],
             "rotate_attn_workspace_size": [PP, ctypes.c_int, ctypes.POINTER(ctypes.c_size_t)],
@@ -99,6 +104,10 @@ def lib():
             "rotate_attn_cache_plan": [CP, I, I] + [P] * 13,
             "rotate_attn_cache_append": [CP, I, P, S, S, P, S, S, P, P, P, I, P, P],
             "rotate_attn_cache_read": [CP, I, P, P, P, P, P],
+            "rotate_attn_cache_pages_workspace_size": [CP, I, ctypes.POINTER(ctypes.c_size_t)],
+            "rotate_attn_cache_fork": [CP, I, I, P, P, P, TP, TP, P, P, ctypes.c_size_t, P, P],
+            "rotate_attn_cache_trim": [CP, I, P, I, TP, TP, P, P, ctypes.c_size_t, P, P],
+            "rotate_attn_cache_compact": [CP, I, TP, TP, P, P, ctypes.c_size_t, P, P],
             "rotate_attn_cache_attn": [CP, I, I, I, P, S, S, P, P, P, P, P, I, P, P, P, ctypes.c_size_t, P],
         }
         for name, args in sig.items():
@@ -507,9 +516,69 @@ def cache_attn(p, q, cache, block_table, q_start, seq_lens, max_q, o, ws, lse=No
         _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
 
 
+def _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out, table_out,
+                 refs_out, free_out, count_out):
+    """R, the device, and (tables, out, cache, workspace, its bytes, status) as the library takes them."""
+    dt = _cache_dtypes()
+    i32, R = dt["i32"], seq_lens.numel()
+    pages, dev = _cache_pages(p, cache, dt["u8"]), cache.device
+    one = (("seq_lens", seq_lens, seq_out, (R,)), ("block_table", block_table, table_out, (R, p.max_blocks)),
+           ("page_refs", page_refs, refs_out, (p.num_pages,)), ("free_pages", free_pages, free_out, (p.num_pages,)),
+           ("free_count", free_count, count_out, (1,)))
+    before = [_cache_tensor(t, name, i32, shape, dev) for name, t, _, shape in one]
+    after = [at if o is None else _cache_tensor(o, name + "'s new state", i32, shape, dev)
+             for at, (name, _, o, shape) in zip(before, one)]
+    nws = _nbytes(ws)
+    return R, dev, (CacheTables(*before), CacheTables(*after), pages, _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev),
+                    nws, _cache_tensor(status, "status", i32, (4,), dev))
+
+
+def cache_fork(p, parents, children, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status,
+               lens=None, seq_out=None, table_out=None, refs_out=None, free_out=None, count_out=None, stream=None):
+    """Requests children[i], which hold nothing, begin with the first lens[i] (all,
+    where None) tokens of parents[i]: full pages are shared, the page that the
+    tokens end in is copied (all int32; rotate_attn.h has the rules).  Tables are
+    updated in place unless arrays for their new state are given."""
+    R, dev, rest = _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out,
+                                table_out, refs_out, free_out, count_out)
+    i32, n = _cache_dtypes()["i32"], parents.numel()
+    _cache_call(lib().rotate_attn_cache_fork, "rotate_attn_cache_fork", dev, stream, ctypes.byref(p), R, n,
+                _cache_tensor(parents, "parents", i32, (n,), dev), _cache_tensor(children, "children", i32, (n,), dev),
+                None if lens is None else _cache_tensor(lens, "lens", i32, (n,), dev), *rest)
+
+
+def cache_trim(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, keep=None, sinks=-1,
+               seq_out=None, table_out=None, refs_out=None, free_out=None, count_out=None, stream=None):
+    """Requests keep their first keep[r] tokens (all where negative, 0 ends them);
+    with sinks >= 0 they also lose the pages between the first `sinks` tokens and
+    the params' window.  Pages that nobody holds any more go back on the stack."""
+    R, dev, rest = _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out,
+                                table_out, refs_out, free_out, count_out)
+    _cache_call(lib().rotate_attn_cache_trim, "rotate_attn_cache_trim", dev, stream, ctypes.byref(p), R,
+                None if keep is None else _cache_tensor(keep, "keep", _cache_dtypes()["i32"], (R,), dev), sinks, *rest)
+
+
+def cache_compact(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out=None,
+                  table_out=None, refs_out=None, free_out=None, count_out=None, stream=None):
+    """Moves the pages in use to the front of the cache; tables, holders and the
+    stack of free pages follow."""
+    R, dev, rest = _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out,
+                                table_out, refs_out, free_out, count_out)
+    _cache_call(lib().rotate_attn_cache_compact, "rotate_attn_cache_compact", dev, stream, ctypes.byref(p), R, *rest)
+
+
+def cache_pages_workspace(p: CacheParams, R: int, device="cuda"):
+    """Workspace of cache_fork, cache_trim and cache_compact."""
+    import torch
+    n = ctypes.c_size_t()
+    _check(lib().rotate_attn_cache_pages_workspace_size(ctypes.byref(p), R, ctypes.byref(n)),
+           "rotate_attn_cache_pages_workspace_size")
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
 def alloc_cache(p: CacheParams, R: int, device="cuda"):
-    """The state of R requests: pages, block table, lengths and the stack of free
-    pages, all free."""
+    """The state of R requests: pages, block table, lengths, the stack of free
+    pages, all free, and the pages' further holders, none."""
     import torch
     i32 = dict(dtype=torch.int32, device=device)
     return dict(
@@ -518,6 +587,7 @@ def alloc_cache(p: CacheParams, R: int, device="cuda"):
         seq_lens=torch.zeros(R, **i32),
         free_pages=torch.arange(int(p.num_pages) - 1, -1, -1, **i32),
         free_count=torch.full((1,), int(p.num_pages), **i32),
+        page_refs=torch.zeros(int(p.num_pages), **i32),
     )
 
 
