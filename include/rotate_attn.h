@@ -432,6 +432,42 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
                            const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
                            size_t workspace_bytes, void* stream);
 
+/* The same under a window beside which the first `sinks` tokens of a request stay
+ * visible: query at position p sees key j <= p where j > p - window or j < sinks
+ * (without a window, or with sinks = 0, what cache_attn sees; causal only).  Pages
+ * between the two are not read, and their table entries may be -1
+ * (cache_trim).  Arguments, workspace, precision and limits are those of cache_attn. */
+int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_t R, int32_t T, int32_t max_q,
+                                 const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* cache,
+                                 const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
+                                 const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* Attention of requests whose first tokens are the same: these are read once for
+ * all queries of a group.  Group g is the requests group_start[g] .. group_start[g + 1] - 1
+ * (ascending; requests outside of all groups are attended to alone), which hold
+ * the same tokens at positions below prefix_lens[g], in the same pages or in copies;
+ * they are read through the table of the group's first request, so that no more of a
+ * prefix is shared than that request holds.  Outputs are those of cache_attn
+ * for any prefix_lens (0: nothing shared), except for the order of sums.
+ * positions[t] is the position of token t (cache_plan's; the last ones of its request's
+ * seq_lens).  Causal attention without a window.  R, T and groups (at most R) fix the
+ * grid; lengths, groups and prefixes are device data.  Values there that do not
+ * fit touch nothing outside the tensors and the workspace.
+ * Limits: 2 * (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096, T * Hq / Hkv
+ * below 2^29.  Precision as cache_attn's, rows of a prefix being those of all its queries: with bf16
+ * outputs weights times V's scales are one bf16 value (2^-8) where a prefix, or a
+ * request's own keys, have more than 16 rows (queries times Hq / Hkv).
+ * Workspace: cache_shared_workspace_size bytes (about 2 T Hq (4 D + 8), partial
+ * outputs of every row), 256-byte aligned; its contents do not matter before or after. */
+int rotate_attn_cache_shared_workspace_size(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T, size_t* bytes);
+int rotate_attn_cache_attn_shared(const ra_cache_params* p, int32_t R, int32_t T, int32_t groups, const void* q,
+                                  int64_t q_token_stride, int64_t q_head_stride, const void* cache,
+                                  const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
+                                  const int32_t* positions, const int32_t* group_start, const int32_t* prefix_lens,
+                                  const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
 /* ---- pages: requests that begin alike, are rolled back, or run on and on ----
  *
  * A page may be held by several requests.  page_refs[page] counts its holders

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "librotate_attn.so")
 SOURCES = ["ra_attn_e2m3.hip", "ra_attn_e2m3_debug.hip", "ra_attn_int4.hip", "ra_host.cpp", "ra_producer.hip",
-           "ra_fp16.hip", "ra_cache.hip", "ra_cache_attn.hip", "ra_cache_pages.hip",
+           "ra_fp16.hip", "ra_cache.hip", "ra_cache_attn.hip", "ra_cache_sinks.hip", "ra_cache_shared.hip", "ra_cache_pages.hip",
            "ra_cache_host.cpp"]
 ARCH = os.environ.get("RA_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

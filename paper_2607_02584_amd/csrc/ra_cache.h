@@ -87,12 +87,24 @@ struct CacheAttnArgs {
   int rope_rows, R, T, max_q, Hq, G, max_blocks;
   int causal, window, is_fp16, out_dtype, had, vhad;
   int target, target_rows;          // pieces of work per KV head aimed at (set by the launch)
+  // first tokens that stay visible beside a window
+  int sinks;
+  // prefixes that requests share
+  int groups;
+  const int* group_start;           // [groups + 1]
+  const int* prefix_lens;           // [groups]
+  const int* positions;             // [T]
+  int2* info;                       // [groups + R] where the parts of a prefix or request are (set by the launch)
+  int64_t part_rows;                // rows of part_o for each KV head
 };
 
 hipError_t launch_cache_plan(const PlanArgs& a, hipStream_t s);
 hipError_t launch_cache_append(const AppendArgs& a, int D, bool hadk, bool hadv, hipStream_t s);
 hipError_t launch_cache_read(const ReadArgs& a, int D, bool hadk, bool hadv, hipStream_t s);
 hipError_t launch_cache_attn(const CacheAttnArgs& a, int D, hipStream_t s);
+hipError_t launch_cache_attn_sinks(const CacheAttnArgs& a, int D, hipStream_t s);
+hipError_t launch_cache_attn_shared(const CacheAttnArgs& a, int D, void* workspace, hipStream_t s);
+size_t cache_shared_bytes(int D, int Hkv, int G, int R, int groups, int T);
 // bytes of workspace that launch_cache_attn's part_o and part_ml take
 size_t cache_attn_partial_bytes(int D, int Hkv, int G, int max_q, size_t* ml_offset);
 

@@ -39,10 +39,21 @@ constexpr float kLn2 = 0.693147180559945309417232121458f;
 // and the workspace follow from that.
 constexpr int kBlock = 64;        // keys
 
+// Which keys a call's rows see:
+//   kAll     the request's, cut by causality and a window
+//   kSinks   those, and its first `sinks` tokens whatever the window
+//   kShared  those of a prefix that a group of requests holds together, and the request's behind it.
+//            Piece by piece either is a request of its own here: numbers below `groups` are
+//            the groups' prefixes (rows: the queries of all the group's requests), the
+//            others the requests' own keys.
+enum Keys { kAll, kSinks, kShared };
+
 // The two kernels share a call's requests by their number of rows: up to
 // kFewRows a request is bound by its keys (k_few), above by the matrix cores
 // (k_rows).
 constexpr int kFewRows = 32;
+// with shared prefixes: rows of one 16-row product
+constexpr int kFewShared = 16;
 // blocks of the least part: a step of 32 keys for each of the four waves of
 // k_few, twice; for k_rows enough to pay for a partial output of M rows
 template <int M>
@@ -52,11 +63,57 @@ struct Request {
   int q0, ql, n;    // first query row, queries to compute (max_q at most), cached tokens
   int first;        // position of the first query
   int tiles, blocks;
+  int lo, table;    // kShared: the first key, and the request whose table names the pages
 };
 
-template <int M>
+// The request's group, -1 for none: the last one that begins at r or before, if it holds r.
+__device__ __forceinline__ int group_of(const CacheAttnArgs& a, int r) {
+  int x = -1, y = a.groups;   // group_start[x] <= r < group_start[y]
+  while (y - x > 1) {
+    const int m = (x + y) >> 1;
+    if (a.group_start[m] <= r) x = m; else y = m;
+  }
+  return x >= 0 && r < a.group_start[x + 1] ? x : -1;
+}
+// Tokens that group g shares: no more than its first request, whose table is read, holds.
+__device__ __forceinline__ int prefix_of(const CacheAttnArgs& a, int g) {
+  const int r0 = a.group_start[g];
+  if (r0 < 0 || r0 >= a.R) return 0;
+  int n = a.prefix_lens[g];
+  const int most = a.max_blocks << a.g.page_log, held = a.seq_lens[r0];
+  n = n < held ? n : held;
+  return n < 0 ? 0 : n > most ? most : n;
+}
+
+template <int M, Keys K>
 __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int r) {
   Request x;
+  x.lo = 0;
+  x.table = r;
+  if constexpr (K == kShared) {
+    const int g = r < a.groups ? r : group_of(a, r - a.groups);
+    const int prefix = g < 0 ? 0 : prefix_of(a, g);
+    int r0 = r - a.groups, r1 = r0 + 1;
+    if (r < a.groups) {
+      r0 = a.group_start[g];
+      r1 = a.group_start[g + 1];
+      r0 = r0 < 0 ? 0 : r0 > a.R ? a.R : r0;
+      r1 = r1 < r0 ? r0 : r1 > a.R ? a.R : r1;
+    }
+    x.table = r0 < a.R ? r0 : 0;
+    const int q0 = a.q_start[r0], q1 = a.q_start[r1], most = a.max_blocks << a.g.page_log;
+    x.q0 = q0 < 0 ? 0 : q0 > a.T ? a.T : q0;
+    x.ql = (q1 < x.q0 ? x.q0 : q1 > a.T ? a.T : q1) - x.q0;
+    const int n = r < a.groups ? prefix : a.seq_lens[r0];
+    x.n = n < 0 ? 0 : n > most ? most : n;
+    x.first = x.n - x.ql;   // (of a prefix not used: positions are given)
+    x.lo = r < a.groups ? 0 : prefix < x.n ? prefix : x.n;
+    const int rows = r < a.groups && x.n == 0 ? 0 : x.ql * a.G;
+    x.tiles = (rows <= kFewShared) == (M <= kFewShared) ? (rows + M - 1) / M : 0;
+    x.blocks = (x.n + kBlock - 1) / kBlock - x.lo / kBlock;
+    if (x.n <= x.lo) x.blocks = 0;
+    return x;
+  }
   int q0 = a.q_start[r], q1 = a.q_start[r + 1];
   const int most = a.max_blocks << a.g.page_log;
   int n = a.seq_lens[r];
@@ -77,18 +134,24 @@ __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int r) {
     keys = keys < tile ? keys : tile;
   }
   x.blocks = (keys + kBlock - 1) / kBlock;
+  if constexpr (K == kSinks) {
+    // with the blocks of the first tokens (of no more than there are)
+    const int all = (x.n + kBlock - 1) / kBlock, more = (a.sinks + kBlock - 1) / kBlock;
+    x.blocks = x.blocks + more < all ? x.blocks + more : all;
+  }
   return x;
 }
 
 struct Piece {
   Request q;
-  int r, tile, part, parts, slot;   // slot: place in the workspace of part 0 of this tile
+  int r, tile, part, parts, slot;   // slot: place in the workspace of part 0 of this tile (kShared: of the request, in rows)
 };
 
+template <Keys K>
 struct SchedShared {
   float w[4];
   int s[4][2];
-  int hit[10];
+  int hit[K == kShared ? 12 : 10];
 };
 
 // Inclusive sum over a wave by register moves (row shifts, then the rows' last
@@ -130,9 +193,10 @@ __device__ __forceinline__ unsigned part_blocks(float W, int target) {
 // parts); false past the end.  All 256 threads of the workgroup call it.  Up to
 // 64 requests every wave finds it alone, from one load of the lengths; above,
 // 256 requests at a time through LDS.
-template <int M>
-__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool merge, int target,
+template <int M, Keys K>
+__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared<K>& sh, int x, bool merge, int target,
                                            Piece* out) {
+  const int N = K == kShared ? a.R + a.groups : a.R;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   auto parts_of = [&](const Request& q, unsigned C) {
     return q.tiles ? (q.blocks ? static_cast<int>((q.blocks + C - 1) / C) : 1) : 0;
@@ -143,26 +207,37 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
     out->parts = n;
     out->tile = merge ? at : at / n;
     out->part = merge ? 0 : at - out->tile * n;
-    out->slot = slot + out->tile * n;
+    out->slot = K == kShared ? slot : slot + out->tile * n;
+    if (K != kShared) {
+      out->q.lo = 0;
+      out->q.table = r;
+    }
   };
-  if (a.R <= 64) {
+  // what a request takes of the workspace: with shared prefixes every row of every part, else tiles that are split
+  auto space_of = [&](const Request& q, int n) {
+    if (K == kShared) return q.tiles ? q.ql * a.G * n : 0;
+    return n > 1 ? q.tiles * n : 0;
+  };
+  if (N <= 64) {
     Request q = {};
-    if (lane < a.R) q = request_of<M>(a, lane);
+    if (lane < N) q = request_of<M, K>(a, lane);
     const float W = wave_total(static_cast<float>(q.tiles) * static_cast<float>(q.blocks));
     const int n = parts_of(q, part_blocks<M>(W, target));
-    const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
+    const int split = space_of(q, n), mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
     const int from = wave_sums(mine) - mine, slot = wave_sums(split) - split;
     const unsigned long long hit = __ballot(x >= from && x < from + mine);
     if (!hit) return false;
     const int r = __builtin_ctzll(hit);
     auto take = [&](int v) { return __builtin_amdgcn_readlane(v, r); };
-    finish(r, x - take(from), take(n), take(slot), {take(q.q0), take(q.ql), take(q.n), take(q.first), take(q.tiles), take(q.blocks)});
+    finish(r, x - take(from), take(n), take(slot),
+           {take(q.q0), take(q.ql), take(q.n), take(q.first), take(q.tiles), take(q.blocks), K == kShared ? take(q.lo) : 0,
+            K == kShared ? take(q.table) : 0});
     return true;
   }
   float W = 0.0f;
   Request q0 = {};
-  for (int r = tid; r < a.R; r += 256) {
-    const Request q = request_of<M>(a, r);
+  for (int r = tid; r < N; r += 256) {
+    const Request q = request_of<M, K>(a, r);
     if (r == tid) q0 = q;
     W += static_cast<float>(q.tiles) * static_cast<float>(q.blocks);
   }
@@ -172,12 +247,12 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
   __syncthreads();
   const unsigned C = part_blocks<M>((sh.w[0] + sh.w[1]) + (sh.w[2] + sh.w[3]), target);
   int base = 0, slot = 0;
-  for (int r0 = 0; r0 < a.R; r0 += 256) {
+  for (int r0 = 0; r0 < N; r0 += 256) {
     const int r = r0 + tid;
     Request q = {};
-    if (r < a.R) q = r0 == 0 ? q0 : request_of<M>(a, r);
+    if (r < N) q = r0 == 0 ? q0 : request_of<M, K>(a, r);
     const int n = parts_of(q, C);
-    const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
+    const int split = space_of(q, n), mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
     const int s0 = wave_sums(mine), s1 = wave_sums(split);
     if (lane == 63) {
       sh.s[w][0] = s0;
@@ -196,9 +271,9 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
     }
     const int from = base + p0 + s0 - mine;
     if (x >= from && x < from + mine) {
-      const int found[10] = {r, x - from, n, slot + p1 + s1 - split, q.q0, q.ql, q.n, q.first, q.tiles, q.blocks};
+      const int found[12] = {r, x - from, n, slot + p1 + s1 - split, q.q0, q.ql, q.n, q.first, q.tiles, q.blocks, q.lo, q.table};
 #pragma unroll
-      for (int i = 0; i < 10; ++i) sh.hit[i] = found[i];
+      for (int i = 0; i < (K == kShared ? 12 : 10); ++i) sh.hit[i] = found[i];
     }
     base += t0;
     slot += t1;
@@ -208,7 +283,8 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
   // the same in every lane, and known to be: loops and addresses stay scalar
   auto take = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.hit[i]); };
   if (take(0) < 0) return false;
-  finish(take(0), take(1), take(2), take(3), {take(4), take(5), take(6), take(7), take(8), take(9)});
+  finish(take(0), take(1), take(2), take(3), {take(4), take(5), take(6), take(7), take(8), take(9), K == kShared ? take(10) : 0,
+                                              K == kShared ? take(11) : 0});
   return true;
 }
 
@@ -251,6 +327,55 @@ __device__ __forceinline__ void finish_row(const CacheAttnArgs& a, int row_token
 
 // 2^(m - M) for a partial result whose maximum is m, 0 where it saw no key.
 __device__ __forceinline__ float rescale(float m, float M) { return m == kNegInf ? 0.0f : exp2f(m - M); }
+
+// The blocks of keys that a tile goes through, numbered without gaps.  kSinks:
+// those of the first tokens, then those of the window, `skip` blocks on.
+template <Keys K>
+struct Span {
+  int first, total;   // numbers first .. total - 1 (kSinks: from 0)
+  int sinks, skip;    // blocks of the first tokens, and of the gap behind them
+  __device__ __forceinline__ Span(const CacheAttnArgs& a, int lo, int hi) {
+    first = lo / kBlock;
+    total = hi > lo ? (hi + kBlock - 1) / kBlock : first;
+    sinks = skip = 0;
+    if constexpr (K == kSinks) {
+      const int s = a.sinks < hi ? a.sinks : hi;
+      sinks = s > 0 ? (s + kBlock - 1) / kBlock : 0;
+      skip = first > sinks ? first - sinks : 0;
+      total = total - skip > sinks ? total - skip : sinks;
+      first = 0;
+    }
+  }
+  // of a number in units of 1 / per block
+  __device__ __forceinline__ int real(int x, int per) const {
+    if constexpr (K == kSinks) return x < sinks * per ? x : x + skip * per;
+    return x;
+  }
+  // how many numbers lie before block b
+  __device__ __forceinline__ int before(int b) const {
+    if constexpr (K == kSinks) return b <= sinks ? b : b - skip > sinks ? b - skip : sinks;
+    return b;
+  }
+};
+
+// Place in the workspace of a row's part, kShared: parts of requests of few rows from the
+// front, of many from the back; -1 where lengths on the device do not fit the call.
+template <bool MANY>
+__device__ __forceinline__ int64_t shared_at(const CacheAttnArgs& a, int base, int parts, int part, int rows, int row, int h) {
+  const int64_t i = static_cast<int64_t>(base) + static_cast<int64_t>(part) * rows + row;
+  if (base < 0 || part < 0 || part >= parts || i < 0 || i >= a.part_rows) return -1;
+  return (MANY ? a.part_rows - 1 - i : i) * a.g.Hkv + h;
+}
+// A piece's rows' positions come with the call where their requests differ.
+__device__ __forceinline__ int row_position(const CacheAttnArgs& a, const Piece& p, int row) {
+  if (p.r >= a.groups) return p.q.first + row / a.G;
+  return row < p.q.ql * a.G ? a.positions[p.q.q0 + row / a.G] : 0x3fffffff;
+}
+// The first piece of a request notes where its parts are, for the rows' joining.
+template <bool MANY>
+__device__ __forceinline__ void note_parts(const CacheAttnArgs& a, const Piece& p, int h) {
+  if (h == 0 && p.tile == 0 && p.part == 0 && threadIdx.x == 0) a.info[p.r] = make_int2(p.slot, MANY ? -p.parts : p.parts);
+}
 
 // ------------------------------------------------------ few rows per request --
 //
@@ -380,7 +505,7 @@ __device__ __forceinline__ v4f score16(uint4 k, uint4 q, v4f c) {
 // The rows' Q as the second operand of K Q^T: lane = 16 * part + row, its
 // D / 4 channels from part * D / 4 on, after RoPE and rotation.  Returns what
 // the row's scores are to be multiplied by.
-template <int D, bool FINE>
+template <int D, bool FINE, Keys K>
 __device__ __forceinline__ float load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
                                         uint4 (&hi)[D / 32], uint4 (&lo)[D / 32]) {
   constexpr int N = D / 4;
@@ -401,7 +526,7 @@ __device__ __forceinline__ float load_q(const CacheAttnArgs& a, const Piece& p, 
     }
   }
   if (a.rope) {
-    int pos = p.q.first + i;
+    int pos = K == kShared ? row_position(a, p, row) : p.q.first + i;
     pos = pos < 0 ? 0 : pos >= a.rope_rows ? a.rope_rows - 1 : pos;
     const float2* cs = reinterpret_cast<const float2*>(a.rope + static_cast<int64_t>(pos) * D) + part * (N / 2);
 #pragma unroll
@@ -462,9 +587,9 @@ struct Rows {
 // first use of its result: the compiler then leaves out the wait states that
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
-template <int D, int NT, int N, int KT, bool FINE>
+template <int D, int NT, int N, int KT, bool FINE, Keys K>
 __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
-                                          int g) {
+                                          int g, int sinks) {
   constexpr int KC = D / 32;
   v4f s[N][KT];
 #pragma unroll
@@ -500,7 +625,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const 
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const int key = key0 + 16 * i + 4 * g + e;
-          const bool on = ((there >> i) & 1) && key < x.hi[nt] && key >= x.lo[nt];
+          const bool on = ((there >> i) & 1) && key < x.hi[nt] && (key >= x.lo[nt] || (K == kSinks && key < sinks));
           seen |= static_cast<unsigned>(on) << (4 * i + e);
           s[nt][i][e] = on ? s[nt][i][e] : kNegInf;
         }
@@ -587,33 +712,36 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const 
   }
 }
 
-template <int D, int NT, int KT, bool FINE>
+template <int D, int NT, int KT, bool FINE, Keys K = kAll>
 __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
   __shared__ __align__(16) float so[4][16][kStride];
   __shared__ float sm[4][M], sl[4][M];
-  __shared__ SchedShared sched;
+  __shared__ SchedShared<K> sched;
   __shared__ __align__(16) uint4 sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
   __shared__ float sback[FINE ? M : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
   // heads fastest: the heads of a page, neighbours in memory, are read together
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M>(a, sched, x0, false, a.target, &p)) return;
+  if (!find_piece<M, K>(a, sched, x0, false, a.target, &p)) return;
+  if constexpr (K == kShared) note_parts<false>(a, p, h);
+  const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;   // of this tile
   const int first = p.q.first;
   const int i0 = p.tile * M / a.G, i1 = (p.tile * M + rows - 1) / a.G;
   // keys that any row of the tile sees, and this part of them
-  int hi = p.q.n, lo = 0;
-  if (a.causal) hi = first + i1 + 1;
+  int hi = p.q.n, lo = p.q.lo;
+  if (a.causal && !prefix) hi = first + i1 + 1;
   if (hi < 0) hi = 0;
   if (a.window) lo = first + i0 - a.window + 1 > 0 ? first + i0 - a.window + 1 : 0;
   // bounds that every row of the tile sees
-  const int all_hi = a.causal ? first + i0 + 1 : p.q.n;
-  const int all_lo = a.window ? first + i1 - a.window + 1 : 0;
-  const int bl = lo / kBlock, bh = hi > lo ? (hi + kBlock - 1) / kBlock : bl;
+  int all_hi = a.causal ? first + i0 + 1 : p.q.n;
+  const int all_lo = a.window ? first + i1 - a.window + 1 : p.q.lo;
+  const Span<K> span(a, lo, hi);
+  const int bl = span.first, bh = span.total;
   const int per = (bh - bl + p.parts - 1) / p.parts;
   const int b0 = bl + p.part * per, b1 = b0 + per < bh ? b0 + per : bh;
   const int wper = (b1 - b0) > 0 ? ((b1 - b0) * S + 3) / 4 : 0;
@@ -621,10 +749,10 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
 
   // Page numbers of 64 tiles of 16 keys at a time, one per lane, and of the 64 after them.
   const int page_shift = a.g.page_log - 4;
-  const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
+  const int* row_table = a.block_table + static_cast<int64_t>(K == kShared ? p.q.table : p.r) * a.max_blocks;
   const int last16 = (p.q.n + 15) / 16;   // tiles that hold cached tokens
   auto ids_from = [&](int t16) {   // (looked at when used, so that nothing waits here)
-    const int t = t16 + lane;
+    const int t = span.real(t16 + lane, kBlock / 16);
     return row_table[(t < last16 ? t : last16 - 1) >> page_shift];
   };
   int ids = -1, ids_next = -1;
@@ -641,7 +769,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
       // an entry that is no page leaves its keys out (those behind the end are masked)
       const bool page = static_cast<unsigned>(id) < static_cast<unsigned>(a.g.num_pages);
       there |= static_cast<unsigned>(page) << i;
-      load_tile<D>(a, t[i], page ? id : 0, h, (b * KT + i) * 16, lane);
+      load_tile<D>(a, t[i], page ? id : 0, h, (span.real(b, S) * KT + i) * 16, lane);
     }
     if (((at + KT) & 63) == 0 && b + 1 < w1) {   // the next step begins the next 64
       ids = ids_next;
@@ -662,7 +790,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
     if (w == nt) {   // one wave for all four
       uint4 qh[D / 32], ql[D / 32];
-      const float back = load_q<D, FINE>(a, p, h, row, lane, qh, ql);
+      const float back = load_q<D, FINE, K>(a, p, h, row, lane, qh, ql);
       if (FINE && lane < 16) sback[nt * 16 + lane] = back;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
@@ -670,10 +798,10 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
         sq_all[(nt * (D / 32) + c) * 128 + 64 + lane] = ql[c];
       }
     }
-    const int pos = first + row / a.G;
+    const int pos = K == kShared ? row_position(a, p, row) : first + row / a.G;
     x.hi[nt] = a.causal ? pos + 1 : p.q.n;
     if (x.hi[nt] > p.q.n) x.hi[nt] = p.q.n;
-    x.lo[nt] = a.window ? pos - a.window + 1 : 0;
+    x.lo[nt] = a.window ? pos - a.window + 1 : p.q.lo;
     x.m[nt] = kNegInf;
     x.l[nt] = 0.0f;
 #pragma unroll
@@ -682,8 +810,22 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
   __syncthreads();
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) x.back[nt] = FINE ? sback[nt * 16 + (lane & 15)] : 1.0f;
+  if constexpr (K == kShared) {
+    static_assert(NT == 1, "one product's rows");
+    if (prefix) {
+      all_hi = x.hi[0];
+      auto least = [&](int o) { all_hi = o < all_hi ? o : all_hi; };
+      least(lane_xor<1>(all_hi));
+      least(lane_xor<2>(all_hi));
+      least(lane_xor<4>(all_hi));
+      least(lane_xor<8>(all_hi));
+      all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    }
+  }
   auto whole = [&](int b, unsigned there) {
-    return b * kStep >= all_lo && b * kStep + kStep <= all_hi && b * kStep + kStep <= p.q.n && there == (1u << KT) - 1;
+    const int key = span.real(b, S) * kStep;
+    return (key >= all_lo || (K == kSinks && key + kStep <= a.sinks)) && key + kStep <= all_hi && key + kStep <= p.q.n &&
+           there == (1u << KT) - 1;
   };
   // Behind the last step the last one is asked for again, so that every step
   // waits for its own loads alone.
@@ -695,7 +837,8 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
         if (b + i >= w1) break;
         there[i ^ 1] = load(b + i + 1 < w1 ? b + i + 1 : w1 - 1, ring[i ^ 1]);
         __builtin_amdgcn_sched_barrier(0);
-        few_step<D, NT, N, KT, FINE>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), (b + i) * kStep, g);
+        few_step<D, NT, N, KT, FINE, K>(x, sq_all + lane, ring[i], there[i], whole(b + i, there[i]), span.real(b + i, S) * kStep, g,
+                                        a.sinks);
       }
     }
   };
@@ -741,11 +884,15 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
 #pragma unroll
         for (int z = 0; z < D / 64; ++z) y[z] += f * so[i][rr][lane * (D / 64) + z];
       }
-      if (p.parts == 1) {
+      if (K != kShared && p.parts == 1) {
         const int i = (p.tile * M + row) / a.G;
         finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + row - i * a.G, y, mm, ll, lane);
       } else {
-        const int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + row;
+        int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + row;
+        if constexpr (K == kShared) {
+          at = shared_at<false>(a, p.slot, p.parts, p.part, p.q.ql * a.G, row, h);
+          if (at < 0) continue;
+        }
 #pragma unroll
         for (int z = 0; z < D / 64; ++z) a.part_o[at * D + lane * (D / 64) + z] = y[z];
         if (lane == 0) a.part_ml[at] = make_float2(mm, ll);
@@ -793,7 +940,7 @@ __device__ __forceinline__ v16f score32(uint4 k, uint4 q, v16f c) {
 }
 
 // As load_q, D / 2 channels per lane.
-template <int D, bool F16, bool FINE>
+template <int D, bool F16, bool FINE, Keys K>
 __device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
                                           uint4 (&hi)[D / 16], uint4 (&lo)[D / 16]) {
   constexpr int N = D / 2;
@@ -814,7 +961,7 @@ __device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p
     }
   }
   if (a.rope) {
-    int pos = p.q.first + i;
+    int pos = K == kShared ? row_position(a, p, row) : p.q.first + i;
     pos = pos < 0 ? 0 : pos >= a.rope_rows ? a.rope_rows - 1 : pos;
     const float2* cs = reinterpret_cast<const float2*>(a.rope + static_cast<int64_t>(pos) * D) + hh * (N / 2);
 #pragma unroll
@@ -867,7 +1014,7 @@ __device__ __forceinline__ void each(F&& f) {
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
 // TERMS: bf16 values that hold P * (V's scale); three come with binary16 pairs of Q.
-template <int D, bool F16, int TERMS>
+template <int D, bool F16, int TERMS, Keys K = kAll>
 __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
   constexpr bool FINE = TERMS == 3;
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
@@ -882,41 +1029,56 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
     Scales sc[2];
   };
   __shared__ __align__(16) Buf buf;
-  __shared__ SchedShared sched;
+  __shared__ SchedShared<K> sched;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
   // heads fastest: workgroups go round the 8 XCDs, so a head's keys stay in few L2s
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M>(a, sched, x0, false, a.target_rows, &p)) return;
+  if (!find_piece<M, K>(a, sched, x0, false, a.target_rows, &p)) return;
+  if constexpr (K == kShared) note_parts<true>(a, p, h);
+  const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
   if (a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
   const int first = p.q.first;
   const int i0 = p.tile * M / a.G, i1 = (p.tile * M + rows - 1) / a.G;
-  int hi = p.q.n, lo = 0;
-  if (a.causal) hi = first + i1 + 1;
+  int hi = p.q.n, lo = p.q.lo;
+  if (a.causal && !prefix) hi = first + i1 + 1;
   if (hi < 0) hi = 0;
   if (a.window) lo = first + i0 - a.window + 1 > 0 ? first + i0 - a.window + 1 : 0;
-  const int bl = lo / kBlock, bh = hi > lo ? (hi + kBlock - 1) / kBlock : bl;
+  const Span<K> span(a, lo, hi);
+  const int bl = span.first, bh = span.total;
   const int per = (bh - bl + p.parts - 1) / p.parts;
   const int b0 = bl + p.part * per, b1 = b0 + per < bh ? b0 + per : bh;
   // bounds that every row of this wave sees, and its lane's row
   const int wrow = p.tile * M + w * 32, row = wrow + j;
   const int wi0 = wrow / a.G, wi1 = wrow + 31 < p.tile * M + rows - 1 ? (wrow + 31) / a.G : i1;
-  const int all_hi = a.causal ? first + wi0 + 1 : p.q.n;
-  const int all_lo = a.window ? first + wi1 - a.window + 1 : 0;
+  int all_hi = a.causal ? first + wi0 + 1 : p.q.n;
+  const int all_lo = a.window ? first + wi1 - a.window + 1 : p.q.lo;
   // tiles from t1 on hold no key that a row of this wave sees; a wave behind the rows of the tile has none at all
-  int t1 = a.causal ? (first + wi1 + kBlock) / kBlock : b1;
+  int t1 = a.causal && !prefix ? span.before((first + wi1 + kBlock) / kBlock) : b1;
   if (t1 > b1) t1 = b1;
   if (w * 32 >= rows || t1 < b0) t1 = b0;
-  const int pos = first + row / a.G;
+  const int pos = K == kShared ? row_position(a, p, row) : first + row / a.G;
   int row_hi = a.causal ? pos + 1 : p.q.n;
   if (row_hi > p.q.n) row_hi = p.q.n;
-  const int row_lo = a.window ? pos - a.window + 1 : 0;
+  const int row_lo = a.window ? pos - a.window + 1 : p.q.lo;
+  if constexpr (K == kShared) {
+    if (prefix) {
+      all_hi = row_hi;
+      auto least = [&](int o) { all_hi = o < all_hi ? o : all_hi; };
+      least(lane_xor<1>(all_hi));
+      least(lane_xor<2>(all_hi));
+      least(lane_xor<4>(all_hi));
+      least(lane_xor<8>(all_hi));
+      least(lane_xor<16>(all_hi));
+      all_hi = __builtin_amdgcn_readfirstlane(all_hi);
+    }
+  }
 
   const int page = a.g.page, page_log = a.g.page_log;
-  const int* row_table = a.block_table + static_cast<int64_t>(p.r) * a.max_blocks;
+  const int* row_table = a.block_table + static_cast<int64_t>(K == kShared ? p.q.table : p.r) * a.max_blocks;
   const uint8_t* head_base = a.g.cache + static_cast<int64_t>(h) * head_bytes<D>(page);
   const int kb = page * D / 2;
   // Loads run ahead of their use: what is read here (page numbers one tile
@@ -934,7 +1096,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
   float ks = 0.0f, vs = 0.0f;
   bool here = false;
   int id_k = 0, id_v = 0, id_s = 0;   // table entries of the tiles asked for next
-  auto within = [&](int b) { return b < b1 ? b : b1 - 1; };
+  auto within = [&](int b) { return span.real(b < b1 ? b : b1 - 1, 1); };   // block of keys of a tile's number
   auto entries = [&](int bk, int bv) {
     id_k = entry_of(within(bk) * kBlock + mine);
     id_v = entry_of(within(bv) * kBlock + mine);
@@ -945,9 +1107,8 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
   // entry behind a load would wait for that load.  Past the last tile it is
   // asked for again, so that there are no branches to wait at.
   auto ask = [&](int bk, int bv) {
-    bk = within(bk);
-    const int cv = within(bv);
-    const int tk = (bk * kBlock + mine) & (page - 1), tv = (cv * kBlock + mine) & (page - 1);
+    const int ck = within(bk), cv = within(bv);
+    const int tk = (ck * kBlock + mine) & (page - 1), tv = (cv * kBlock + mine) & (page - 1);
     const int g = ((lane >> 4) & 1) * 2 + hh;   // V: lane = chunk + 16 * (half of the octet) + 32 * hh, tokens 4 g ..
     const uint8_t* pk = page_at(__builtin_amdgcn_readfirstlane(id_k)) + tk * (D / 2) + lane * (D / 8);
     const uint8_t* pv =
@@ -961,7 +1122,8 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
     }
     sk = *reinterpret_cast<const Codes*>(pk);
     sv = *reinterpret_cast<const Codes*>(pv);
-    entries(bk + 1, cv + 1);
+    if constexpr (K == kSinks) entries(bk + 1, bv + 1);
+    else entries(ck + 1, cv + 1);
   };
   // The staged codes into LDS, in four parts each.  What is written past the
   // last tile replaces tiles that are done with.
@@ -1024,7 +1186,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
     ask(b0, b0);
   }
   uint4 q[KC], q_lo[KC];
-  const float back = load_q32<D, F16, FINE>(a, p, h, row, lane, q, q_lo);
+  const float back = load_q32<D, F16, FINE, K>(a, p, h, row, lane, q, q_lo);
   v16f o[MT], s[2];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -1060,7 +1222,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
     // higher priority, the products behind it at the lower one
     __builtin_amdgcn_s_setprio(1);
     const Scales& t = buf.sc[b & 1];
-    const int key0 = b * kBlock;
+    const int key0 = span.real(b, 1) * kBlock;
     const float base = m == kNegInf ? 0.0f : m;
     float x[2][16], mx = kNegInf;
 #pragma unroll
@@ -1076,8 +1238,10 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
       }
     }
     const unsigned long long plain = t.plain;
-    if (key0 < all_lo || key0 + kBlock > all_hi || plain != ~0ull) {
-      unsigned long long on = t.there & bits_below(row_hi - key0) & ~bits_below(row_lo - key0);
+    if ((key0 < all_lo && !(K == kSinks && key0 + kBlock <= a.sinks)) || key0 + kBlock > all_hi || plain != ~0ull) {
+      unsigned long long late = ~bits_below(row_lo - key0);
+      if constexpr (K == kSinks) late |= bits_below(a.sinks - key0);
+      unsigned long long on = t.there & bits_below(row_hi - key0) & late;
       // rows that see a V that is not finite are NaN from here on (their lse is that of the keys)
       if (__any((on & ~plain) != 0)) {
         const float by = on & ~plain ? __builtin_nanf("") : 1.0f;
@@ -1240,11 +1404,15 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
       float y[D / 64];
 #pragma unroll
       for (int z = 0; z < D / 64; ++z) y[z] = so[k * kStride + lane * (D / 64) + z];
-      if (p.parts == 1) {
+      if (K != kShared && p.parts == 1) {
         const int i = (p.tile * M + rr) / a.G;
         finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + rr - i * a.G, y, mm, ll, lane);
       } else {
-        const int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + rr;
+        int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + rr;
+        if constexpr (K == kShared) {
+          at = shared_at<true>(a, p.slot, p.parts, p.part, p.q.ql * a.G, p.tile * M + rr, h);
+          if (at < 0) continue;
+        }
 #pragma unroll
         for (int z = 0; z < D / 64; ++z) a.part_o[at * D + lane * (D / 64) + z] = y[z];
         if (lane == 0) a.part_ml[at] = make_float2(mm, ll);
@@ -1258,15 +1426,15 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
 // then the sum of their outputs, eight at a time (D / 4 threads each).
 constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 
-template <int D, int M>
+template <int D, int M, Keys K = kAll>
 __device__ __forceinline__ void join_tiles(const CacheAttnArgs& a, int target, int per_group) {
   constexpr int W = D / 4, NG = 256 / W;
-  __shared__ SchedShared sched;
+  __shared__ SchedShared<K> sched;
   __shared__ float f[kMostParts];
   __shared__ float red[8];
   __shared__ __align__(16) float4 sum[NG][W];
   Piece p;
-  if (!find_piece<M>(a, sched, blockIdx.x, true, target, &p)) return;
+  if (!find_piece<M, K>(a, sched, blockIdx.x, true, target, &p)) return;
   if (M > kFewRows && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // as k_rows numbers them
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y;
   int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
@@ -1365,6 +1533,77 @@ Grid grid_of(const CacheAttnArgs& a, int M, int target) {
 }
 
 int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }
+
+// ---------------------------------------------------------------- kernels --
+
+template <int D, int NT, int KT, Keys K>
+__global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
+  few_rows<D, NT, KT, false, K>(a);
+}
+template <int D, int NT, int KT, Keys K>
+__global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
+  few_rows<D, NT, KT, true, K>(a);
+}
+
+template <int D, bool F16, bool LO, Keys K>
+__global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
+  many_rows<D, F16, LO ? 2 : 1, K>(a);
+}
+template <int D, bool F16, Keys K>
+__global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
+  many_rows<D, F16, 3, K>(a);
+}
+
+template <int D, int M, Keys K>
+__global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target, int per_group) {
+  join_tiles<D, M, K>(a, target, per_group);
+}
+
+template <int D, int M, Keys K>
+hipError_t merge(const CacheAttnArgs& a, const Grid& g, int target, int64_t rows, hipStream_t s) {
+  if (rows > M) rows = M;
+  // a workgroup per row while those are few enough to run at once
+  const int per_group = g.merges * a.g.Hkv * rows <= 4096 ? 1 : M > kFewRows ? 16 : 8;
+  k_merge<D, M, K><<<dim3(static_cast<unsigned>(g.merges), a.g.Hkv, static_cast<unsigned>((rows + per_group - 1) / per_group)),
+                  dim3(256), 0, s>>>(a, target, per_group);
+  return hipGetLastError();
+}
+
+template <int D, int NT, Keys K>
+hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
+  constexpr int M = 16 * NT;
+  Grid g;
+  g.tiles = a.R;   // a request of few rows is one tile
+  g.merges = g.tiles < a.target ? g.tiles : a.target;
+  const dim3 grid(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv));
+  if (a.out_dtype == RA_FP32) k_fine_few<D, NT, 2, K><<<grid, dim3(256), 0, s>>>(a);
+  else k_few<D, NT, 2, K><<<grid, dim3(256), 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : merge<D, M, K>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
+}
+
+template <int D, bool F16, Keys K>
+hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
+  const Grid g = grid_of(a, kRowTile, a.target_rows);
+  const dim3 grid(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv));
+  // P in as many bf16 values as the output shows
+  if (a.out_dtype == RA_FP32) k_fine_rows<D, F16, K><<<grid, dim3(256), 0, s>>>(a);
+  else if (a.out_dtype == RA_FP16) k_rows<D, F16, true, K><<<grid, dim3(256), 0, s>>>(a);
+  else k_rows<D, F16, false, K><<<grid, dim3(256), 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess ? e : merge<D, kRowTile, K>(a, g, a.target_rows, static_cast<int64_t>(a.max_q) * a.G, s);
+}
+
+template <int D, Keys K>
+hipError_t attn_d(const CacheAttnArgs& a, hipStream_t s) {
+  const int64_t most = static_cast<int64_t>(a.max_q) * a.G;
+  if (most <= 16) return few<D, 1, K>(a, s);
+  hipError_t e = hipSuccess;
+  if (a.G <= kFewRows) e = few<D, 2, K>(a, s);   // requests of few rows; with more heads than that there are none
+  if (e != hipSuccess || most <= kFewRows) return e;
+  return a.is_fp16 ? rows<D, true, K>(a, s) : rows<D, false, K>(a, s);
+}
+
 
 }  // namespace
 }  // namespace ra

@@ -119,6 +119,98 @@ struct Input {
   int64_t n;
 };
 
+int check_workspace(const void* workspace, size_t workspace_bytes, size_t need) {
+  if (!workspace) return set_error(RA_ERR_WORKSPACE, "workspace is NULL");
+  if (!aligned(workspace, 256)) return set_error(RA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
+  if (workspace_bytes < need) {
+    char msg[96];
+    std::snprintf(msg, sizeof msg, "workspace too small: need %zu bytes", need);
+    return set_error(RA_ERR_WORKSPACE, msg);
+  }
+  return RA_OK;
+}
+
+// The tensors of an attention call, and what of the kernels' arguments follows from them.
+int attn_tensors(const ra_cache_params* p, int32_t R, int32_t T, const void* q, int64_t q_token_stride,
+                 int64_t q_head_stride, const void* cache, const int32_t* block_table, const int32_t* q_start,
+                 const int32_t* seq_lens, const float* rope, int32_t rope_rows, void* o, float* lse, ra::CacheAttnArgs* x) {
+  int rc;
+  if (!q || !cache || !block_table || !q_start || !seq_lens || !o) return set_error(RA_ERR_INVALID, "NULL tensor pointer");
+  if ((rc = check_rows("q", q, q_token_stride, q_head_stride))) return rc;
+  if ((rc = check_rope(p, rope, rope_rows))) return rc;
+  if (!aligned(cache, 128)) return set_error(RA_ERR_INVALID, "cache must be 128-byte aligned");
+  if (!aligned(o, 16)) return set_error(RA_ERR_INVALID, "o must be 16-byte aligned");
+  ra::CacheAttnArgs a = {};
+  a.g = geom(p, const_cast<void*>(cache));
+  a.q = static_cast<const uint16_t*>(q);
+  a.q_ts = q_token_stride;
+  a.q_hs = q_head_stride;
+  a.block_table = block_table;
+  a.q_start = q_start;
+  a.seq_lens = seq_lens;
+  a.rope = rope;
+  a.rope_rows = rope_rows;
+  a.o = o;
+  a.lse = lse;
+  const double scale = p->sm_scale == 0.0f ? 1.0 / std::sqrt(static_cast<double>(p->D)) : p->sm_scale;
+  const double norm = p->rotation == RA_ROT_HADAMARD ? 1.0 / std::sqrt(static_cast<double>(p->D)) : 1.0;
+  a.c = static_cast<float>(scale * norm * 1.4426950408889634);   // base 2
+  a.R = R;
+  a.T = T;
+  a.Hq = p->Hq;
+  a.G = p->Hq / p->Hkv;
+  a.max_blocks = p->max_blocks;
+  a.causal = p->causal;
+  a.window = p->window;
+  a.is_fp16 = p->in_dtype == RA_FP16;
+  a.out_dtype = p->out_dtype;
+  a.had = p->rotation == RA_ROT_HADAMARD;
+  a.vhad = p->v_rotation == RA_VROT_HADAMARD;
+  *x = a;
+  return RA_OK;
+}
+
+// What cache_attn and cache_attn_sinks take; x->T is 0 where there is nothing to do.
+int attn_args(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, const void* q, int64_t q_token_stride,
+              int64_t q_head_stride, const void* cache, const int32_t* block_table, const int32_t* q_start,
+              const int32_t* seq_lens, const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
+              size_t workspace_bytes, ra::CacheAttnArgs* x) {
+  int rc = validate(p);
+  if (rc) return rc;
+  if ((rc = check_counts(R, T))) return rc;
+  if ((rc = check_pieces(p, R, T))) return rc;
+  if (max_q < 0) return set_error(RA_ERR_INVALID, "max_q must be >= 0");
+  x->T = 0;
+  if (R == 0 || T == 0 || max_q == 0) return RA_OK;
+  if (max_q > T) max_q = T;
+  if ((rc = attn_tensors(p, R, T, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope, rope_rows,
+                         o, lse, x)))
+    return rc;
+  size_t ml;
+  const size_t need = ra::cache_attn_partial_bytes(p->D, p->Hkv, x->G, max_q, &ml);
+  if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
+  x->part_o = static_cast<float*>(workspace);
+  x->part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ml);
+  x->max_q = max_q;
+  return RA_OK;
+}
+
+// Sizes of cache_attn_shared: as check_pieces, with every row once in a prefix and once in its request, whose places in
+// the workspace are 32-bit numbers.
+int check_shared(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T) {
+  int rc = validate(p);
+  if (rc) return rc;
+  if ((rc = check_counts(R, T))) return rc;
+  if (groups < 0 || groups > R) return set_error(RA_ERR_INVALID, "groups must be in [0, R]");
+  if (!p->causal) return set_error(RA_ERR_UNSUPPORTED, "shared prefixes need causal attention");
+  if (p->window) return set_error(RA_ERR_UNSUPPORTED, "shared prefixes cannot be under a window");
+  const int64_t rows = 2 * static_cast<int64_t>(T) * (p->Hq / p->Hkv);
+  const int64_t pieces = (2 * (static_cast<int64_t>(R) + groups) + rows / 128) * p->Hkv;
+  if (pieces >= (1 << 24) - 4096 || rows >= (1 << 30))
+    return set_error(RA_ERR_UNSUPPORTED, "2 * (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096, T * Hq / Hkv below 2^29");
+  return RA_OK;
+}
+
 // Tables of an operator on pages: every array is there, and its new state is
 // kept in place or in an array that overlaps none of the others, `inputs` included.
 int page_tables(const ra_cache_params* p, int32_t R, const ra_cache_tables* in, const ra_cache_tables* out, void* cache,
@@ -159,13 +251,7 @@ int page_tables(const ra_cache_params* p, int32_t R, const ra_cache_tables* in, 
       return set_error(RA_ERR_INVALID, "tables overlap the cache or the workspace");
   }
   if (!aligned(cache, 128)) return set_error(RA_ERR_INVALID, "cache must be 128-byte aligned");
-  if (!workspace) return set_error(RA_ERR_WORKSPACE, "workspace is NULL");
-  if (!aligned(workspace, 256)) return set_error(RA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (workspace_bytes < need) {
-    char msg[96];
-    std::snprintf(msg, sizeof msg, "workspace too small: need %zu bytes", need);
-    return set_error(RA_ERR_WORKSPACE, msg);
-  }
+  if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
   t->seq_in = a[0];
   t->table_in = a[1];
   t->refs_in = a[2];
@@ -310,59 +396,60 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
                            const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
                            const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
                            size_t workspace_bytes, void* stream) {
-  int rc = validate(p);
-  if (rc) return rc;
-  if ((rc = check_counts(R, T))) return rc;
-  if ((rc = check_pieces(p, R, T))) return rc;
-  if (max_q < 0) return set_error(RA_ERR_INVALID, "max_q must be >= 0");
-  if (R == 0 || T == 0 || max_q == 0) return RA_OK;
-  if (max_q > T) max_q = T;
-  if (!q || !cache || !block_table || !q_start || !seq_lens || !o) return set_error(RA_ERR_INVALID, "NULL tensor pointer");
-  if ((rc = check_rows("q", q, q_token_stride, q_head_stride))) return rc;
-  if ((rc = check_rope(p, rope, rope_rows))) return rc;
-  if (!aligned(cache, 128)) return set_error(RA_ERR_INVALID, "cache must be 128-byte aligned");
-  if (!aligned(o, 16)) return set_error(RA_ERR_INVALID, "o must be 16-byte aligned");
-  size_t ml;
-  const int G = p->Hq / p->Hkv;
-  const size_t need = ra::cache_attn_partial_bytes(p->D, p->Hkv, G, max_q, &ml);
-  if (!workspace) return set_error(RA_ERR_WORKSPACE, "workspace is NULL");
-  if (!aligned(workspace, 256)) return set_error(RA_ERR_WORKSPACE, "workspace must be 256-byte aligned");
-  if (workspace_bytes < need) {
-    char msg[96];
-    std::snprintf(msg, sizeof msg, "workspace too small: need %zu bytes", need);
-    return set_error(RA_ERR_WORKSPACE, msg);
-  }
   ra::CacheAttnArgs a;
-  a.g = geom(p, const_cast<void*>(cache));
-  a.q = static_cast<const uint16_t*>(q);
-  a.q_ts = q_token_stride;
-  a.q_hs = q_head_stride;
-  a.block_table = block_table;
-  a.q_start = q_start;
-  a.seq_lens = seq_lens;
-  a.rope = rope;
-  a.rope_rows = rope_rows;
-  a.o = o;
-  a.lse = lse;
-  a.part_o = static_cast<float*>(workspace);
-  a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ml);
-  const double scale = p->sm_scale == 0.0f ? 1.0 / std::sqrt(static_cast<double>(p->D)) : p->sm_scale;
-  const double norm = p->rotation == RA_ROT_HADAMARD ? 1.0 / std::sqrt(static_cast<double>(p->D)) : 1.0;
-  a.c = static_cast<float>(scale * norm * 1.4426950408889634);   // base 2
-  a.R = R;
-  a.T = T;
-  a.max_q = max_q;
-  a.Hq = p->Hq;
-  a.G = G;
-  a.max_blocks = p->max_blocks;
-  a.causal = p->causal;
-  a.window = p->window;
-  a.is_fp16 = p->in_dtype == RA_FP16;
-  a.out_dtype = p->out_dtype;
-  a.had = p->rotation == RA_ROT_HADAMARD;
-  a.vhad = p->v_rotation == RA_VROT_HADAMARD;
-  a.target = a.target_rows = 0;
+  const int rc = attn_args(p, R, T, max_q, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope,
+                           rope_rows, o, lse, workspace, workspace_bytes, &a);
+  if (rc || a.T == 0) return rc;
   return hip_status(ra::launch_cache_attn(a, p->D, static_cast<hipStream_t>(stream)), "cache_attn");
+}
+
+int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_t R, int32_t T, int32_t max_q,
+                                 const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* cache,
+                                 const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
+                                 const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
+                                 size_t workspace_bytes, void* stream) {
+  if (p && !p->causal) return set_error(RA_ERR_UNSUPPORTED, "sinks need causal attention");
+  if (sinks < 0) return set_error(RA_ERR_INVALID, "sinks must be >= 0");
+  if (sinks > (1 << 30)) return set_error(RA_ERR_UNSUPPORTED, "sinks must not exceed 2^30");
+  ra::CacheAttnArgs a;
+  const int rc = attn_args(p, R, T, max_q, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope,
+                           rope_rows, o, lse, workspace, workspace_bytes, &a);
+  if (rc || a.T == 0) return rc;
+  a.sinks = sinks;
+  return hip_status(ra::launch_cache_attn_sinks(a, p->D, static_cast<hipStream_t>(stream)), "cache_attn_sinks");
+}
+
+int rotate_attn_cache_shared_workspace_size(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T, size_t* bytes) {
+  const int rc = check_shared(p, R, groups, T);
+  if (rc) return rc;
+  if (!bytes) return set_error(RA_ERR_INVALID, "bytes is NULL");
+  *bytes = ra::cache_shared_bytes(p->D, p->Hkv, p->Hq / p->Hkv, R, groups, T);
+  return RA_OK;
+}
+
+int rotate_attn_cache_attn_shared(const ra_cache_params* p, int32_t R, int32_t T, int32_t groups, const void* q,
+                                  int64_t q_token_stride, int64_t q_head_stride, const void* cache,
+                                  const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
+                                  const int32_t* positions, const int32_t* group_start, const int32_t* prefix_lens,
+                                  const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+  int rc = check_shared(p, R, groups, T);
+  if (rc) return rc;
+  if (R == 0 || T == 0) return RA_OK;
+  if (!positions || (groups && (!group_start || !prefix_lens))) return set_error(RA_ERR_INVALID, "NULL tensor pointer");
+  ra::CacheAttnArgs a;
+  rc = attn_tensors(p, R, T, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope, rope_rows, o,
+                    lse, &a);
+  if (rc) return rc;
+  rc = check_workspace(workspace, workspace_bytes, ra::cache_shared_bytes(p->D, p->Hkv, a.G, R, groups, T));
+  if (rc) return rc;
+  a.max_q = T;
+  a.groups = groups;
+  a.group_start = group_start;
+  a.prefix_lens = prefix_lens;
+  a.positions = positions;
+  return hip_status(ra::launch_cache_attn_shared(a, p->D, workspace, static_cast<hipStream_t>(stream)),
+                    "cache_attn_shared");
 }
 
 int rotate_attn_cache_pages_workspace_size(const ra_cache_params* p, int32_t R, size_t* bytes) {

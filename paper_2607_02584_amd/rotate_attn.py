@@ -104,6 +104,9 @@ def lib():
             "rotate_attn_cache_plan": [CP, I, I] + [P] * 13,
             "rotate_attn_cache_append": [CP, I, P, S, S, P, S, S, P, P, P, I, P, P],
             "rotate_attn_cache_read": [CP, I, P, P, P, P, P],
+            "rotate_attn_cache_attn_sinks": [CP, I, I, I, I, P, S, S, P, P, P, P, P, I, P, P, P, ctypes.c_size_t, P],
+            "rotate_attn_cache_shared_workspace_size": [CP, I, I, I, ctypes.POINTER(ctypes.c_size_t)],
+            "rotate_attn_cache_attn_shared": [CP, I, I, I, P, S, S, P, P, P, P, P, P, P, P, I, P, P, P, ctypes.c_size_t, P],
             "rotate_attn_cache_pages_workspace_size": [CP, I, ctypes.POINTER(ctypes.c_size_t)],
             "rotate_attn_cache_fork": [CP, I, I, P, P, P, TP, TP, P, P, ctypes.c_size_t, P, P],
             "rotate_attn_cache_trim": [CP, I, P, I, TP, TP, P, P, ctypes.c_size_t, P, P],
@@ -514,6 +517,56 @@ def cache_attn(p, q, cache, block_table, q_start, seq_lens, max_q, o, ws, lse=No
         table, rows, _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
         None if lse is None else _cache_tensor(lse, "lse", dt[FP32], shape[:2], dev),
         _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
+
+
+def cache_attn_sinks(p, sinks, q, cache, block_table, q_start, seq_lens, max_q, o, ws, lse=None, rope=None, stream=None):
+    """cache_attn under the params' window, beside which each request's first
+    `sinks` tokens stay visible (workspace as cache_attn's)."""
+    dt = _cache_dtypes()
+    pages, dev, R, T = _cache_pages(p, cache, dt["u8"]), cache.device, seq_lens.numel(), q.shape[0]
+    shape, i32 = (T, p.Hq, p.D), dt["i32"]
+    table, rows = _cache_rope(p, rope, dev)
+    nws = _nbytes(ws)
+    _cache_call(
+        lib().rotate_attn_cache_attn_sinks, "rotate_attn_cache_attn_sinks", dev, stream, ctypes.byref(p), sinks, R, T, max_q,
+        _cache_tensor(q, "q", dt[p.in_dtype], shape, dev, True), *_cache_rows(q), pages,
+        _cache_tensor(block_table, "block_table", i32, (R, p.max_blocks), dev),
+        _cache_tensor(q_start, "q_start", i32, (R + 1,), dev), _cache_tensor(seq_lens, "seq_lens", i32, (R,), dev),
+        table, rows, _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
+        None if lse is None else _cache_tensor(lse, "lse", dt[FP32], shape[:2], dev),
+        _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
+
+
+def cache_attn_shared(p, q, cache, block_table, q_start, seq_lens, positions, group_start, prefix_lens, o, ws, lse=None,
+                      rope=None, stream=None):
+    """cache_attn of requests in groups that hold the same first tokens: requests
+    group_start[g] .. group_start[g + 1] - 1 share prefix_lens[g] of them, which are
+    read once for all (positions as cache_plan leaves them)."""
+    dt = _cache_dtypes()
+    pages, dev, R, T = _cache_pages(p, cache, dt["u8"]), cache.device, seq_lens.numel(), q.shape[0]
+    shape, i32, groups = (T, p.Hq, p.D), dt["i32"], prefix_lens.numel()
+    table, rows = _cache_rope(p, rope, dev)
+    nws = _nbytes(ws)
+    _cache_call(
+        lib().rotate_attn_cache_attn_shared, "rotate_attn_cache_attn_shared", dev, stream, ctypes.byref(p), R, T, groups,
+        _cache_tensor(q, "q", dt[p.in_dtype], shape, dev, True), *_cache_rows(q), pages,
+        _cache_tensor(block_table, "block_table", i32, (R, p.max_blocks), dev),
+        _cache_tensor(q_start, "q_start", i32, (R + 1,), dev), _cache_tensor(seq_lens, "seq_lens", i32, (R,), dev),
+        _cache_tensor(positions, "positions", i32, (T,), dev),
+        _cache_tensor(group_start, "group_start", i32, (groups + 1,), dev),
+        _cache_tensor(prefix_lens, "prefix_lens", i32, (groups,), dev), table, rows,
+        _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
+        None if lse is None else _cache_tensor(lse, "lse", dt[FP32], shape[:2], dev),
+        _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
+
+
+def cache_shared_workspace(p: CacheParams, R: int, groups: int, T: int, device="cuda"):
+    """Workspace of cache_attn_shared."""
+    import torch
+    n = ctypes.c_size_t()
+    _check(lib().rotate_attn_cache_shared_workspace_size(ctypes.byref(p), R, groups, T, ctypes.byref(n)),
+           "rotate_attn_cache_shared_workspace_size")
+    return torch.empty(max(n.value, 256), dtype=torch.uint8, device=device)
 
 
 def _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out, table_out,

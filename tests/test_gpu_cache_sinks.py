@@ -1,0 +1,170 @@
+"""cache_attn_sinks against plain numpy in 64 bits (tests/cache_case.py)."""
+import numpy as np
+import pytest
+
+from cache_case import Case, HALF, i32
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def ra():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2607_02584_amd import rotate_attn as m
+    m.lib()
+    return m
+
+
+def _many(c):
+    return max(c.qs + [0]) * (c.p.Hq // c.p.Hkv) > 32
+
+
+@pytest.mark.parametrize("D,page", [(128, 16), (64, 64), (128, 256)])
+@pytest.mark.parametrize("n", [1, 2, 16, 63, 64, 65, 130, 1000])
+@pytest.mark.parametrize("window,sinks", [(1, 1), (20, 4), (64, 64), (100, 65), (30, 0), (2000, 3), (1, 5000), (0, 7)])
+def test_single_tokens(ra, D, page, n, window, sinks):
+    c = Case(ra, 4, 2, D, page, [n], [1], window=window, sinks=sinks, seed=n + sinks)
+    c.run()
+    c.check(False)
+
+
+@pytest.mark.parametrize("dt,out", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "fp32"), ("fp16", "bf16")])
+@pytest.mark.parametrize("Hq,Hkv", [(12, 12), (5, 1), (40, 8), (20, 1), (48, 1)])
+def test_decode_types_and_heads(ra, dt, out, Hq, Hkv):
+    c = Case(ra, Hq, Hkv, 128, 32, [300, 1, 0, 777, 1025, 64], [1, 1, 0, 1, 1, 0], dt, out, rope=True, had=True,
+             vhad=out == "fp32", window=90, sinks=5, pad=3, seed=Hq, strided=True)
+    c.run()
+    c.check(_many(c))
+
+
+@pytest.mark.parametrize("D,Hq,Hkv,page,dt,out", [(128, 4, 2, 16, "bf16", "bf16"), (64, 6, 2, 64, "fp16", "fp16"),
+                                                  (128, 8, 1, 128, "fp16", "fp32"), (64, 3, 3, 32, "bf16", "fp32")])
+@pytest.mark.parametrize("lens,qs", [([40, 7, 130], [40, 7, 130]), ([600, 1313], [5, 257]), ([1, 1000, 90], [1, 33, 0])])
+@pytest.mark.parametrize("window,sinks", [(50, 3), (1, 1), (64, 128), (130, 70), (300, 64)])
+def test_prompts(ra, D, Hq, Hkv, page, dt, out, lens, qs, window, sinks):
+    c = Case(ra, Hq, Hkv, D, page, lens, qs, dt, out, rope=True, had=window != 1, vhad=window == 50, window=window, sinks=sinks,
+             pad=2, seed=len(lens) + window)
+    c.run()
+    c.check(_many(c))
+
+
+@pytest.mark.parametrize("R", [70, 300])
+def test_many_requests(ra, R):
+    rng = np.random.default_rng(R)
+    lens = rng.integers(0, 400, R).tolist()
+    qs = [min(n, int(q)) for n, q in zip(lens, rng.choice([0, 1, 1, 1, 5, 60], R))]
+    c = Case(ra, 4, 1, 64, 32, lens, qs, rope=True, vhad=True, window=70, sinks=9, pad=1, seed=R)
+    c.run()
+    c.check(True)
+
+
+@pytest.mark.parametrize("q_len", [1, 9, 150])
+def test_long_windows_are_split(ra, q_len):
+    c = Case(ra, 2, 1, 128, 64, [9000, 3000], [q_len, 1], rope=True, window=5000, sinks=200, seed=q_len)
+    c.run()
+    c.check(_many(c))
+
+
+def test_more_queries_than_tokens(ra):
+    c = Case(ra, 4, 2, 128, 16, [3, 0, 20], [7, 2, 50], window=4, sinks=2, seed=3)
+    c.run()
+    c.check(True)
+
+
+@pytest.mark.parametrize("window,sinks", [(0, 0), (0, 50), (300, 0), (5000, 7), (30, 5000)])
+def test_equals_cache_attn_where_the_gap_is_empty(ra, window, sinks):
+    """Sinks that add nothing: the same bits as cache_attn (with as many sinks as tokens, as without a window)."""
+    for qs in ([1, 1], [4, 1], [120, 3]):
+        a = Case(ra, 8, 2, 128, 32, [1000, 300], qs, rope=True, window=window, sinks=sinks, seed=1)
+        x, lse = (t.clone() for t in a.run())
+        a.sinks = None
+        if sinks >= 1000:
+            a.p.window = 0
+        y, lse2 = a.run()
+        if sinks and window and sinks < 1000:      # blocks counted for sinks may cut the keys elsewhere
+            assert (x.float() - y.float()).abs().max() < 8 * HALF["bf16"] * y.float().abs().max()
+        elif sinks < 1000:
+            assert torch.equal(x, y) and torch.equal(lse, lse2)
+        else:
+            assert (x.float() - y.float()).abs().max() < 8 * HALF["bf16"] * y.float().abs().max()
+
+
+def test_pages_of_the_gap_are_not_read(ra):
+    """Entries between the first tokens and the window are -1, their pages hold NaN; the same bits as with them there."""
+    for qs in ([1, 1, 1], [6, 1, 90]):
+        window, sinks, page = 100, 20, 16
+        c = Case(ra, 4, 2, 128, page, [1000, 300, 700], qs, rope=True, window=window, sinks=sinks, seed=5)
+        x, lse = (t.clone() for t in c.run())
+        for r, (n, m) in enumerate(zip(c.lens, c.qs)):
+            for j in range(-(-n // page)):
+                if j * page >= sinks and (j + 1) * page <= n - m - window + 1:
+                    c.scales()[c.table[r, j]] = np.nan
+                    c.table[r, j] = -1 if j % 2 else c.p.num_pages + j
+        y, lse2 = c.run()
+        assert torch.equal(x, y) and torch.equal(lse, lse2)
+        c.check(_many(c))
+
+
+def test_what_a_row_does_not_see_cannot_reach_it(ra):
+    """NaN scales in the gap and behind a row: every row that does not see them has the same bits, the others are NaN."""
+    for q_len in (6, 40):
+        n, window, sinks = 300, 30, 10
+        c = Case(ra, 4, 2, 128, 16, [n], [q_len], window=window, sinks=sinks, seed=q_len, pad=2)
+        c.q[q_len:] = float("nan")
+        x, lse = (t.clone() for t in c.run())
+        gone = list(range(sinks, n - q_len - window + 1)) + [n - 2, n - 1]
+        for t in gone:
+            c.scales()[c.table[0, t // 16], :, :, t % 16] = np.nan
+        y, lse2 = c.run()
+        assert torch.equal(x[:q_len - 2], y[:q_len - 2]) and torch.equal(lse[:q_len - 2], lse2[:q_len - 2])
+        assert torch.isnan(y[q_len - 2:q_len]).all() and (y[q_len:] == 5.0).all()
+        # a first token with a V that is not finite reaches every row, their lse stays
+        c.scales()[c.table[0, 0], :, 1, 3] = np.inf
+        z, lse3 = c.run()
+        assert torch.isnan(z[:q_len]).all() and torch.equal(lse3[:q_len - 2], lse2[:q_len - 2])
+
+
+def test_repeats_and_streams(ra):
+    c = Case(ra, 8, 2, 128, 32, [5000, 300, 4000], [1, 40, 2], rope=True, had=True, window=1000, sinks=40, seed=30)
+    x, lse = (t.clone() for t in c.run())
+    side = torch.cuda.Stream()
+    y, lse2 = c.run(stream=side.cuda_stream)
+    assert torch.equal(x, y) and torch.equal(lse, lse2)
+
+
+def test_a_stream_of_tokens_in_bounded_memory(ra):
+    """A request goes on far past its pages: each step plans, appends, attends with sinks and loses the pages behind
+    the window.  Outputs equal those of a request that keeps everything, bit for bit, and the pages held stay few."""
+    rng = np.random.default_rng(3)
+    page, window, sinks, R = 16, 40, 5, 2
+    i = dict(dtype=torch.int32, device="cuda")
+    runs = []
+    for evict in (True, False):
+        p = ra.make_cache_params(4, 2, 64, page_size=page, num_pages=12 if evict else 80, max_blocks=40, window=window)
+        st = ra.alloc_cache(p, R)
+        tables = [st[k] for k in ("seq_lens", "block_table", "page_refs", "free_pages", "free_count")]
+        T = 60
+        q_start, positions, slots, status, new = (torch.zeros(n, **i) for n in (R + 1, T, T, 4, R))
+        runs.append((p, st, tables, q_start, positions, slots, status, new, ra.cache_workspace(p, R, T, 30),
+                     ra.cache_pages_workspace(p, R)))
+    for step in range(40):
+        counts = [20, 25] if step == 0 else [int(rng.integers(1, 12)), 1]
+        x = torch.tensor(rng.standard_normal((60, 8, 64))).to(torch.bfloat16).cuda()
+        got = []
+        for k, (p, st, tables, q_start, positions, slots, status, new, ws, pws) in enumerate(runs):
+            new.copy_(i32(counts))
+            ra.cache_plan(p, st["seq_lens"], new, st["block_table"], st["free_pages"], st["free_count"], q_start, positions,
+                          slots, status)
+            assert status[0].item() == 0
+            ra.cache_append(p, x[:, 4:6], x[:, 6:], slots, st["cache"])
+            o, lse = torch.zeros(60, 4, 64, dtype=torch.bfloat16, device="cuda"), torch.zeros(60, 4, device="cuda")
+            ra.cache_attn_sinks(p, sinks, x[:, :4], st["cache"], st["block_table"], q_start, st["seq_lens"], 30, o, ws, lse=lse)
+            if k == 0:
+                ra.cache_trim(p, *tables, st["cache"], pws, status, sinks=sinks)
+                assert status[0].item() == 0
+                # a page of first tokens, those that a window of 40 touches, and the one that is being filled
+                assert st["free_count"].item() >= 12 - 2 * 5
+            got.append((o, lse))
+        assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]), step
