@@ -94,7 +94,14 @@ struct CacheAttnArgs {
   const int* group_start;           // [groups + 1]
   const int* prefix_lens;           // [groups]
   const int* positions;             // [T]
-  int2* info;                       // [groups + R] where the parts of a prefix or request are (set by the launch)
+  // set by the launch
+  int4* requests;                   // [groups + R][2] prefixes and requests
+  int2* info;                       // [groups + R] where their parts are: first row, parts (negative: from the back)
+  int4* pieces[2];                  // of few and of many rows
+  int* counts;                      // [2]
+  int bound[2];                     // of the pieces
+  uint16_t* turned;                 // [T][Hq][2][D] Q as the matrix products take it
+  float* back;                      // [T][Hq] what the scores are multiplied by
   int64_t part_rows;                // rows of part_o for each KV head
 };
 

@@ -42,18 +42,16 @@ constexpr int kBlock = 64;        // keys
 // Which keys a call's rows see:
 //   kAll     the request's, cut by causality and a window
 //   kSinks   those, and its first `sinks` tokens whatever the window
-//   kShared  those of a prefix that a group of requests holds together, and the request's behind it.
-//            Piece by piece either is a request of its own here: numbers below `groups` are
-//            the groups' prefixes (rows: the queries of all the group's requests), the
-//            others the requests' own keys.
+//   kShared  those of a prefix that a group of requests holds together, and the request's behind it:
+//            either is a request of its own here, numbers below `groups` being the groups' prefixes
+//            (rows: the queries of all the group's requests).  Its pieces are
+//            listed by a launch before (ra_cache_shared.hip).
 enum Keys { kAll, kSinks, kShared };
 
 // The two kernels share a call's requests by their number of rows: up to
 // kFewRows a request is bound by its keys (k_few), above by the matrix cores
 // (k_rows).
 constexpr int kFewRows = 32;
-// with shared prefixes: rows of one 16-row product
-constexpr int kFewShared = 16;
 // blocks of the least part: a step of 32 keys for each of the four waves of
 // k_few, twice; for k_rows enough to pay for a partial output of M rows
 template <int M>
@@ -66,54 +64,11 @@ struct Request {
   int lo, table;    // kShared: the first key, and the request whose table names the pages
 };
 
-// The request's group, -1 for none: the last one that begins at r or before, if it holds r.
-__device__ __forceinline__ int group_of(const CacheAttnArgs& a, int r) {
-  int x = -1, y = a.groups;   // group_start[x] <= r < group_start[y]
-  while (y - x > 1) {
-    const int m = (x + y) >> 1;
-    if (a.group_start[m] <= r) x = m; else y = m;
-  }
-  return x >= 0 && r < a.group_start[x + 1] ? x : -1;
-}
-// Tokens that group g shares: no more than its first request, whose table is read, holds.
-__device__ __forceinline__ int prefix_of(const CacheAttnArgs& a, int g) {
-  const int r0 = a.group_start[g];
-  if (r0 < 0 || r0 >= a.R) return 0;
-  int n = a.prefix_lens[g];
-  const int most = a.max_blocks << a.g.page_log, held = a.seq_lens[r0];
-  n = n < held ? n : held;
-  return n < 0 ? 0 : n > most ? most : n;
-}
-
 template <int M, Keys K>
 __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int r) {
   Request x;
   x.lo = 0;
   x.table = r;
-  if constexpr (K == kShared) {
-    const int g = r < a.groups ? r : group_of(a, r - a.groups);
-    const int prefix = g < 0 ? 0 : prefix_of(a, g);
-    int r0 = r - a.groups, r1 = r0 + 1;
-    if (r < a.groups) {
-      r0 = a.group_start[g];
-      r1 = a.group_start[g + 1];
-      r0 = r0 < 0 ? 0 : r0 > a.R ? a.R : r0;
-      r1 = r1 < r0 ? r0 : r1 > a.R ? a.R : r1;
-    }
-    x.table = r0 < a.R ? r0 : 0;
-    const int q0 = a.q_start[r0], q1 = a.q_start[r1], most = a.max_blocks << a.g.page_log;
-    x.q0 = q0 < 0 ? 0 : q0 > a.T ? a.T : q0;
-    x.ql = (q1 < x.q0 ? x.q0 : q1 > a.T ? a.T : q1) - x.q0;
-    const int n = r < a.groups ? prefix : a.seq_lens[r0];
-    x.n = n < 0 ? 0 : n > most ? most : n;
-    x.first = x.n - x.ql;   // (of a prefix not used: positions are given)
-    x.lo = r < a.groups ? 0 : prefix < x.n ? prefix : x.n;
-    const int rows = r < a.groups && x.n == 0 ? 0 : x.ql * a.G;
-    x.tiles = (rows <= kFewShared) == (M <= kFewShared) ? (rows + M - 1) / M : 0;
-    x.blocks = (x.n + kBlock - 1) / kBlock - x.lo / kBlock;
-    if (x.n <= x.lo) x.blocks = 0;
-    return x;
-  }
   int q0 = a.q_start[r], q1 = a.q_start[r + 1];
   const int most = a.max_blocks << a.g.page_log;
   int n = a.seq_lens[r];
@@ -142,16 +97,24 @@ __device__ __forceinline__ Request request_of(const CacheAttnArgs& a, int r) {
   return x;
 }
 
+// Blocks of a part, W blocks in all: at least W / target, the sum's roundings
+// (the same in every workgroup) included.
+template <int M>
+__device__ __forceinline__ unsigned part_blocks(float W, int target) {
+  const float c = W * (1.0f + 0x1p-10f) / static_cast<float>(target) + 1.0f;
+  const unsigned C = c < 0x1p26f ? static_cast<unsigned>(c) : 1u << 26;   // a request has 2^24 at most
+  return C < static_cast<unsigned>(least_blocks<M>()) ? least_blocks<M>() : C;
+}
+
 struct Piece {
   Request q;
   int r, tile, part, parts, slot;   // slot: place in the workspace of part 0 of this tile (kShared: of the request, in rows)
 };
 
-template <Keys K>
 struct SchedShared {
   float w[4];
   int s[4][2];
-  int hit[K == kShared ? 12 : 10];
+  int hit[10];
 };
 
 // Inclusive sum over a wave by register moves (row shifts, then the rows' last
@@ -180,23 +143,13 @@ __device__ __forceinline__ float wave_total(float v) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
 
-// Blocks of a part, W blocks in all: at least W / target, the sum's roundings
-// (the same in every workgroup) included.
-template <int M>
-__device__ __forceinline__ unsigned part_blocks(float W, int target) {
-  const float c = W * (1.0f + 0x1p-10f) / static_cast<float>(target) + 1.0f;
-  const unsigned C = c < 0x1p26f ? static_cast<unsigned>(c) : 1u << 26;   // a request has 2^24 at most
-  return C < static_cast<unsigned>(least_blocks<M>()) ? least_blocks<M>() : C;
-}
-
 // Piece number x (or, for the merge, tile number x of those with several
 // parts); false past the end.  All 256 threads of the workgroup call it.  Up to
 // 64 requests every wave finds it alone, from one load of the lengths; above,
 // 256 requests at a time through LDS.
 template <int M, Keys K>
-__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared<K>& sh, int x, bool merge, int target,
+__device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& sh, int x, bool merge, int target,
                                            Piece* out) {
-  const int N = K == kShared ? a.R + a.groups : a.R;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   auto parts_of = [&](const Request& q, unsigned C) {
     return q.tiles ? (q.blocks ? static_cast<int>((q.blocks + C - 1) / C) : 1) : 0;
@@ -207,36 +160,27 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared<K
     out->parts = n;
     out->tile = merge ? at : at / n;
     out->part = merge ? 0 : at - out->tile * n;
-    out->slot = K == kShared ? slot : slot + out->tile * n;
-    if (K != kShared) {
-      out->q.lo = 0;
-      out->q.table = r;
-    }
+    out->slot = slot + out->tile * n;
+    out->q.lo = 0;
+    out->q.table = r;
   };
-  // what a request takes of the workspace: with shared prefixes every row of every part, else tiles that are split
-  auto space_of = [&](const Request& q, int n) {
-    if (K == kShared) return q.tiles ? q.ql * a.G * n : 0;
-    return n > 1 ? q.tiles * n : 0;
-  };
-  if (N <= 64) {
+  if (a.R <= 64) {
     Request q = {};
-    if (lane < N) q = request_of<M, K>(a, lane);
+    if (lane < a.R) q = request_of<M, K>(a, lane);
     const float W = wave_total(static_cast<float>(q.tiles) * static_cast<float>(q.blocks));
     const int n = parts_of(q, part_blocks<M>(W, target));
-    const int split = space_of(q, n), mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
+    const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
     const int from = wave_sums(mine) - mine, slot = wave_sums(split) - split;
     const unsigned long long hit = __ballot(x >= from && x < from + mine);
     if (!hit) return false;
     const int r = __builtin_ctzll(hit);
     auto take = [&](int v) { return __builtin_amdgcn_readlane(v, r); };
-    finish(r, x - take(from), take(n), take(slot),
-           {take(q.q0), take(q.ql), take(q.n), take(q.first), take(q.tiles), take(q.blocks), K == kShared ? take(q.lo) : 0,
-            K == kShared ? take(q.table) : 0});
+    finish(r, x - take(from), take(n), take(slot), {take(q.q0), take(q.ql), take(q.n), take(q.first), take(q.tiles), take(q.blocks)});
     return true;
   }
   float W = 0.0f;
   Request q0 = {};
-  for (int r = tid; r < N; r += 256) {
+  for (int r = tid; r < a.R; r += 256) {
     const Request q = request_of<M, K>(a, r);
     if (r == tid) q0 = q;
     W += static_cast<float>(q.tiles) * static_cast<float>(q.blocks);
@@ -247,12 +191,12 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared<K
   __syncthreads();
   const unsigned C = part_blocks<M>((sh.w[0] + sh.w[1]) + (sh.w[2] + sh.w[3]), target);
   int base = 0, slot = 0;
-  for (int r0 = 0; r0 < N; r0 += 256) {
+  for (int r0 = 0; r0 < a.R; r0 += 256) {
     const int r = r0 + tid;
     Request q = {};
-    if (r < N) q = r0 == 0 ? q0 : request_of<M, K>(a, r);
+    if (r < a.R) q = r0 == 0 ? q0 : request_of<M, K>(a, r);
     const int n = parts_of(q, C);
-    const int split = space_of(q, n), mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
+    const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
     const int s0 = wave_sums(mine), s1 = wave_sums(split);
     if (lane == 63) {
       sh.s[w][0] = s0;
@@ -271,9 +215,9 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared<K
     }
     const int from = base + p0 + s0 - mine;
     if (x >= from && x < from + mine) {
-      const int found[12] = {r, x - from, n, slot + p1 + s1 - split, q.q0, q.ql, q.n, q.first, q.tiles, q.blocks, q.lo, q.table};
+      const int found[10] = {r, x - from, n, slot + p1 + s1 - split, q.q0, q.ql, q.n, q.first, q.tiles, q.blocks};
 #pragma unroll
-      for (int i = 0; i < (K == kShared ? 12 : 10); ++i) sh.hit[i] = found[i];
+      for (int i = 0; i < 10; ++i) sh.hit[i] = found[i];
     }
     base += t0;
     slot += t1;
@@ -283,8 +227,7 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared<K
   // the same in every lane, and known to be: loops and addresses stay scalar
   auto take = [&](int i) { return __builtin_amdgcn_readfirstlane(sh.hit[i]); };
   if (take(0) < 0) return false;
-  finish(take(0), take(1), take(2), take(3), {take(4), take(5), take(6), take(7), take(8), take(9), K == kShared ? take(10) : 0,
-                                              K == kShared ? take(11) : 0});
+  finish(take(0), take(1), take(2), take(3), {take(4), take(5), take(6), take(7), take(8), take(9)});
   return true;
 }
 
@@ -371,10 +314,44 @@ __device__ __forceinline__ int row_position(const CacheAttnArgs& a, const Piece&
   if (p.r >= a.groups) return p.q.first + row / a.G;
   return row < p.q.ql * a.G ? a.positions[p.q.q0 + row / a.G] : 0x3fffffff;
 }
-// The first piece of a request notes where its parts are, for the rows' joining.
-template <bool MANY>
-__device__ __forceinline__ void note_parts(const CacheAttnArgs& a, const Piece& p, int h) {
-  if (h == 0 && p.tile == 0 && p.part == 0 && threadIdx.x == 0) a.info[p.r] = make_int2(p.slot, MANY ? -p.parts : p.parts);
+// Piece x of the list for few (0) or many (1) rows: {request, tile, part, parts}; of a request {q0, ql, n, first}, {lo, table, slot}.
+template <int MANY>
+__device__ __forceinline__ bool listed_piece(const CacheAttnArgs& a, int x, Piece* out) {
+  if (x >= __builtin_amdgcn_readfirstlane(a.counts[MANY])) return false;
+  auto all = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+  const int4 c = a.pieces[MANY][x];
+  out->r = all(c.x);
+  out->tile = all(c.y);
+  out->part = all(c.z);
+  out->parts = all(c.w);
+  const int4 u = a.requests[2 * out->r], v = a.requests[2 * out->r + 1];
+  out->q.q0 = all(u.x);
+  out->q.ql = all(u.y);
+  out->q.n = all(u.z);
+  out->q.first = all(u.w);
+  out->q.lo = all(v.x);
+  out->q.table = all(v.y);
+  out->slot = all(v.z);
+  out->q.tiles = out->q.blocks = 0;
+  return true;
+}
+template <int M, Keys K>
+__device__ __forceinline__ bool take_piece(const CacheAttnArgs& a, SchedShared& sh, int x, int target, Piece* out) {
+  if constexpr (K == kShared) return listed_piece<(M > kFewRows)>(a, x, out);
+  else return find_piece<M, K>(a, sh, x, false, target, out);
+}
+// 16 bytes of a row's Q, turned and in two values by the launch before: hi of its D channels, then lo.
+template <int D>
+__device__ __forceinline__ uint4 turned(const CacheAttnArgs& a, const Piece& p, int h, int row, int z, int channel) {
+  if (row >= p.q.ql * a.G) return uint4{};
+  const int i = row / a.G;
+  const int64_t at = static_cast<int64_t>(p.q.q0 + i) * a.Hq + h * a.G + row - i * a.G;
+  return *reinterpret_cast<const uint4*>(a.turned + at * 2 * D + z * D + channel);
+}
+__device__ __forceinline__ float turned_back(const CacheAttnArgs& a, const Piece& p, int h, int row) {
+  if (row >= p.q.ql * a.G) return 1.0f;
+  const int i = row / a.G;
+  return a.back[static_cast<int64_t>(p.q.q0 + i) * a.Hq + h * a.G + row - i * a.G];
 }
 
 // ------------------------------------------------------ few rows per request --
@@ -505,7 +482,7 @@ __device__ __forceinline__ v4f score16(uint4 k, uint4 q, v4f c) {
 // The rows' Q as the second operand of K Q^T: lane = 16 * part + row, its
 // D / 4 channels from part * D / 4 on, after RoPE and rotation.  Returns what
 // the row's scores are to be multiplied by.
-template <int D, bool FINE, Keys K>
+template <int D, bool FINE>
 __device__ __forceinline__ float load_q(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
                                         uint4 (&hi)[D / 32], uint4 (&lo)[D / 32]) {
   constexpr int N = D / 4;
@@ -526,7 +503,7 @@ __device__ __forceinline__ float load_q(const CacheAttnArgs& a, const Piece& p, 
     }
   }
   if (a.rope) {
-    int pos = K == kShared ? row_position(a, p, row) : p.q.first + i;
+    int pos = p.q.first + i;
     pos = pos < 0 ? 0 : pos >= a.rope_rows ? a.rope_rows - 1 : pos;
     const float2* cs = reinterpret_cast<const float2*>(a.rope + static_cast<int64_t>(pos) * D) + part * (N / 2);
 #pragma unroll
@@ -718,15 +695,14 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
   constexpr int kStride = D + 4;                       // floats, against bank conflicts
   __shared__ __align__(16) float so[4][16][kStride];
   __shared__ float sm[4][M], sl[4][M];
-  __shared__ SchedShared<K> sched;
+  __shared__ SchedShared sched;
   __shared__ __align__(16) uint4 sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
   __shared__ float sback[FINE ? M : 1];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
   // heads fastest: the heads of a page, neighbours in memory, are read together
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M, K>(a, sched, x0, false, a.target, &p)) return;
-  if constexpr (K == kShared) note_parts<false>(a, p, h);
+  if (!take_piece<M, K>(a, sched, x0, a.target, &p)) return;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;   // of this tile
@@ -788,9 +764,15 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int row = p.tile * M + nt * 16 + (lane & 15);
-    if (w == nt) {   // one wave for all four
+    if constexpr (K == kShared) {
+      if (w < D / 32) {   // 8 channels of each part of D / 4 for each of the waves
+#pragma unroll
+        for (int z = 0; z < 2; ++z) sq_all[(w * 2 + z) * 64 + lane] = turned<D>(a, p, h, row, z, g * (D / 4) + w * 8);
+      }
+      if (FINE && w == 0 && lane < 16) sback[lane] = turned_back(a, p, h, row);
+    } else if (w == nt) {   // one wave for all four
       uint4 qh[D / 32], ql[D / 32];
-      const float back = load_q<D, FINE, K>(a, p, h, row, lane, qh, ql);
+      const float back = load_q<D, FINE>(a, p, h, row, lane, qh, ql);
       if (FINE && lane < 16) sback[nt * 16 + lane] = back;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
@@ -940,7 +922,7 @@ __device__ __forceinline__ v16f score32(uint4 k, uint4 q, v16f c) {
 }
 
 // As load_q, D / 2 channels per lane.
-template <int D, bool F16, bool FINE, Keys K>
+template <int D, bool F16, bool FINE>
 __device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
                                           uint4 (&hi)[D / 16], uint4 (&lo)[D / 16]) {
   constexpr int N = D / 2;
@@ -961,7 +943,7 @@ __device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p
     }
   }
   if (a.rope) {
-    int pos = K == kShared ? row_position(a, p, row) : p.q.first + i;
+    int pos = p.q.first + i;
     pos = pos < 0 ? 0 : pos >= a.rope_rows ? a.rope_rows - 1 : pos;
     const float2* cs = reinterpret_cast<const float2*>(a.rope + static_cast<int64_t>(pos) * D) + hh * (N / 2);
 #pragma unroll
@@ -1029,16 +1011,15 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
     Scales sc[2];
   };
   __shared__ __align__(16) Buf buf;
-  __shared__ SchedShared<K> sched;
+  __shared__ SchedShared sched;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
   // heads fastest: workgroups go round the 8 XCDs, so a head's keys stay in few L2s
   const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!find_piece<M, K>(a, sched, x0, false, a.target_rows, &p)) return;
-  if constexpr (K == kShared) note_parts<true>(a, p, h);
+  if (!take_piece<M, K>(a, sched, x0, a.target_rows, &p)) return;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
-  if (a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
+  if (K != kShared && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
   const int first = p.q.first;
@@ -1186,7 +1167,17 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
     ask(b0, b0);
   }
   uint4 q[KC], q_lo[KC];
-  const float back = load_q32<D, F16, FINE, K>(a, p, h, row, lane, q, q_lo);
+  float back = 1.0f;
+  if constexpr (K == kShared) {
+#pragma unroll
+    for (int c = 0; c < KC; ++c) {
+      q[c] = turned<D>(a, p, h, row, 0, hh * (D / 2) + c * 8);
+      q_lo[c] = turned<D>(a, p, h, row, 1, hh * (D / 2) + c * 8);
+    }
+    if constexpr (FINE) back = turned_back(a, p, h, row);
+  } else {
+    back = load_q32<D, F16, FINE>(a, p, h, row, lane, q, q_lo);
+  }
   v16f o[MT], s[2];
 #pragma unroll
   for (int i = 0; i < MT; ++i)
@@ -1377,48 +1368,89 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
 #pragma unroll
   for (int i = 0; i < MT; ++i) settle(o[i]);
 
-  // out through LDS, 8 rows of each wave at a time
+  // Out of the registers: of its row a lane holds half of the chunks of E
+  // channels, register r of tile i being channel e = 2 i + r / 8 of chunk 8 (r / 4 % 2) + 4 hh + r % 4.
+  // (Through LDS, a row at a time in whole lines, it took 9 of a piece's 66 us with two pieces per
+  // compute unit; the L2 joins the lines that are written in parts here.)
   l += lane_xor<32>(l);
-  constexpr int kStride = D + 4;
-  static_assert(sizeof(buf) >= NW * 8 * kStride * sizeof(float), "the output rows pass through the tiles' LDS");
-  float* so = reinterpret_cast<float*>(&buf) + w * 8 * kStride;
+  float y[E][8];   // [channel of a chunk][chunk 8 (c / 4) + 4 hh + c % 4]
 #pragma unroll
-  for (int round = 0; round < 4; ++round) {
-    __syncthreads();
-    if ((j >> 3) == round) {
-      // register r of tile i: position 32 i + 8 (r / 4) + 4 hh + r % 4 = e * 16 + chunk
+  for (int e = 0; e < E; ++e)
 #pragma unroll
-      for (int i = 0; i < MT; ++i)
+    for (int c = 0; c < 8; ++c) y[e][c] = o[e >> 1][8 * (e & 1) + c];
+  const int rr = w * 32 + j;
+  if (K == kShared || p.parts != 1) {
+    int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + rr;
+    if constexpr (K == kShared) at = shared_at<true>(a, p.slot, p.parts, p.part, p.q.ql * a.G, p.tile * M + rr, h);
+    if (rr >= rows || at < 0) return;
+    float* dst = a.part_o + at * D + 4 * hh * E;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int e = 2 * i + (r >> 3), chunk = 8 * ((r >> 2) & 1) + 4 * hh + (r & 3);
-          so[(j & 7) * kStride + chunk * E + e] = o[i][r];
-        }
-    }
-    __syncthreads();
-#pragma unroll 1
-    for (int k = 0; k < 8; ++k) {
-      const int rr = w * 32 + round * 8 + k;
-      if (rr >= rows) break;
-      const float mm = __shfl(m, round * 8 + k), ll = __shfl(l, round * 8 + k);
-      float y[D / 64];
+    for (int c = 0; c < 8; ++c)
 #pragma unroll
-      for (int z = 0; z < D / 64; ++z) y[z] = so[k * kStride + lane * (D / 64) + z];
-      if (K != kShared && p.parts == 1) {
-        const int i = (p.tile * M + rr) / a.G;
-        finish_row<D>(a, p.q.q0 + i, h * a.G + p.tile * M + rr - i * a.G, y, mm, ll, lane);
-      } else {
-        int64_t at = (static_cast<int64_t>(p.slot + p.part) * a.g.Hkv + h) * M + rr;
-        if constexpr (K == kShared) {
-          at = shared_at<true>(a, p.slot, p.parts, p.part, p.q.ql * a.G, p.tile * M + rr, h);
-          if (at < 0) continue;
-        }
+      for (int e = 0; e < E; e += 4)
+        *reinterpret_cast<float4*>(dst + (8 * (c >> 2) + (c & 3)) * E + e) = make_float4(y[e][c], y[e + 1][c], y[e + 2][c], y[e + 3][c]);
+    if (hh == 0) a.part_ml[at] = make_float2(m, l);
+    return;
+  }
+  // as finish_row
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
 #pragma unroll
-        for (int z = 0; z < D / 64; ++z) a.part_o[at * D + lane * (D / 64) + z] = y[z];
-        if (lane == 0) a.part_ml[at] = make_float2(mm, ll);
-      }
+  for (int e = 0; e < E; ++e)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) y[e][c] *= inv;
+  if (a.vhad) {
+    auto stage = [&](float& u, float& v) {
+      const float t = u;
+      u = t + v;
+      v = t - v;
+    };
+#pragma unroll
+    for (int d = 1; d < E; d *= 2)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (!(e & d)) stage(y[e][c], y[e + d][c]);
+#pragma unroll
+    for (int d = 1; d < 4; d *= 2)
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (!(c & d)) stage(y[e][c], y[e][c + d]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) butterfly_lanes<32>(y[e], lane);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) stage(y[e][c], y[e][c + 4]);
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) y[e][c] *= D == 128 ? 0.0883883476483184405501055452631f : 0.125f;
+  }
+  if (rr >= rows) return;
+  const int i = row / a.G;
+  const int64_t out = static_cast<int64_t>(p.q.q0 + i) * a.Hq + h * a.G + row - i * a.G;
+  const int64_t to = out * D + 4 * hh * E;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const int at = (8 * (c >> 2) + (c & 3)) * E;
+    if (a.out_dtype == RA_FP32) {
+#pragma unroll
+      for (int e = 0; e < E; e += 4)
+        *reinterpret_cast<float4*>(static_cast<float*>(a.o) + to + at + e) = make_float4(y[e][c], y[e + 1][c], y[e + 2][c], y[e + 3][c]);
+    } else {
+      const bool f = a.out_dtype == RA_FP16;
+      uint32_t u[E / 2];
+#pragma unroll
+      for (int e = 0; e < E; e += 2) u[e / 2] = pack16(y[e][c], y[e + 1][c], f);
+      uint16_t* dst = static_cast<uint16_t*>(a.o) + to + at;
+      if constexpr (E == 8) *reinterpret_cast<uint4*>(dst) = make_uint4(u[0], u[1], u[2], u[3]);
+      else *reinterpret_cast<uint2*>(dst) = make_uint2(u[0], u[1]);
     }
   }
+  if (a.lse && hh == 0) a.lse[out] = l == 0.0f ? kNegInf : (m + log2f(l)) * kLn2;
 }
 
 // Joins the parts of split tiles, a workgroup for per_group rows: up to eight
@@ -1429,7 +1461,7 @@ constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 template <int D, int M, Keys K = kAll>
 __device__ __forceinline__ void join_tiles(const CacheAttnArgs& a, int target, int per_group) {
   constexpr int W = D / 4, NG = 256 / W;
-  __shared__ SchedShared<K> sched;
+  __shared__ SchedShared sched;
   __shared__ float f[kMostParts];
   __shared__ float red[8];
   __shared__ __align__(16) float4 sum[NG][W];

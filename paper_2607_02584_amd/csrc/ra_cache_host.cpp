@@ -195,8 +195,8 @@ int attn_args(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, con
   return RA_OK;
 }
 
-// Sizes of cache_attn_shared: as check_pieces, with every row once in a prefix and once in its request, whose places in
-// the workspace are 32-bit numbers.
+// Sizes of cache_attn_shared: as check_pieces, with every row once in a prefix and once in its request; a launch per
+// token, with 256 work-items, and one per query head's row, with 16.
 int check_shared(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T) {
   int rc = validate(p);
   if (rc) return rc;
@@ -204,10 +204,10 @@ int check_shared(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T)
   if (groups < 0 || groups > R) return set_error(RA_ERR_INVALID, "groups must be in [0, R]");
   if (!p->causal) return set_error(RA_ERR_UNSUPPORTED, "shared prefixes need causal attention");
   if (p->window) return set_error(RA_ERR_UNSUPPORTED, "shared prefixes cannot be under a window");
-  const int64_t rows = 2 * static_cast<int64_t>(T) * (p->Hq / p->Hkv);
-  const int64_t pieces = (2 * (static_cast<int64_t>(R) + groups) + rows / 128) * p->Hkv;
-  if (pieces >= (1 << 24) - 4096 || rows >= (1 << 30))
-    return set_error(RA_ERR_UNSUPPORTED, "2 * (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096, T * Hq / Hkv below 2^29");
+  const int64_t pieces = (static_cast<int64_t>(R) + groups) * p->Hkv + static_cast<int64_t>(T) * p->Hq / 64;
+  if (pieces >= (1 << 24) - 4096) return set_error(RA_ERR_UNSUPPORTED, "(R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096");
+  if (T > (1 << 22) || static_cast<int64_t>(T) * p->Hq > (1 << 26))
+    return set_error(RA_ERR_UNSUPPORTED, "T must not exceed 2^22, and T * Hq not 2^26, with shared prefixes");
   return RA_OK;
 }
 

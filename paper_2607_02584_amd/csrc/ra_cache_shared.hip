@@ -8,9 +8,12 @@
 // The prefix of a group is a request of its own here, whose rows are the
 // queries of all the group's requests (they follow each other in the batch), so
 // that its keys are read once for all, by the matrix cores as soon as there are
-// more than 16 rows.  Prefixes and requests are cut into pieces together (see
-// the schedule in ra_cache_attn.h); every piece leaves its partial rows in the
-// workspace, and a wave per row joins them.
+// more than 16 rows.
+//
+// Four launches: k_shared_plan cuts prefixes and requests into pieces and turns
+// Q, once for all the pieces that take a row (in each of them it was 5 of a
+// piece's 66 us); the kernels for few and for many rows go through their
+// lists and leave partial rows in the workspace; a wave per row joins them.
 //
 // Bound by HBM while a group's rows are few, by the matrix cores and the softmax
 // beside them from some 64 rows on.
@@ -18,6 +21,367 @@
 
 namespace ra {
 namespace {
+
+constexpr int kFewShared = 16;   // rows of one 16-row product: up to those, k_few
+
+// The lengths of a call, in memory or in LDS.
+struct Lengths {
+  const int* group_start;
+  const int* prefix_lens;
+  const int* q_start;
+  const int* seq_lens;
+};
+
+// The request's group, -1 for none: the last one that begins at r or before, if it holds r.
+__device__ __forceinline__ int group_of(const CacheAttnArgs& a, const Lengths& x, int r) {
+  int g = -1, y = a.groups;   // group_start[g] <= r < group_start[y]
+  while (y - g > 1) {
+    const int m = (g + y) >> 1;
+    if (x.group_start[m] <= r) g = m; else y = m;
+  }
+  return g >= 0 && r < x.group_start[g + 1] ? g : -1;
+}
+// Tokens that group g shares: no more than its first request, whose table is read, holds.
+__device__ __forceinline__ int prefix_of(const CacheAttnArgs& a, const Lengths& x, int g) {
+  const int r0 = x.group_start[g];
+  if (r0 < 0 || r0 >= a.R) return 0;
+  int n = x.prefix_lens[g];
+  const int most = a.max_blocks << a.g.page_log, held = x.seq_lens[r0];
+  n = n < held ? n : held;
+  return n < 0 ? 0 : n > most ? most : n;
+}
+
+// Prefix or request v.  Whatever the device holds, nothing outside the tensors is touched.
+__device__ __forceinline__ Request shared_request(const CacheAttnArgs& a, const Lengths& l, int v) {
+  Request x;
+  const int g = v < a.groups ? v : group_of(a, l, v - a.groups);
+  const int prefix = g < 0 ? 0 : prefix_of(a, l, g);
+  int r0 = v - a.groups, r1 = r0 + 1;
+  if (v < a.groups) {
+    r0 = l.group_start[v];
+    r1 = l.group_start[v + 1];
+    r0 = r0 < 0 ? 0 : r0 > a.R ? a.R : r0;
+    r1 = r1 < r0 ? r0 : r1 > a.R ? a.R : r1;
+  }
+  const int q0 = l.q_start[r0], q1 = l.q_start[r1], most = a.max_blocks << a.g.page_log;
+  x.table = r0 < a.R ? r0 : 0;
+  x.q0 = q0 < 0 ? 0 : q0 > a.T ? a.T : q0;
+  x.ql = (q1 < x.q0 ? x.q0 : q1 > a.T ? a.T : q1) - x.q0;
+  const int n = v < a.groups ? prefix : l.seq_lens[r0];
+  x.n = n < 0 ? 0 : n > most ? most : n;
+  x.first = x.n - x.ql;   // (of a prefix not used: its rows have positions of their own)
+  x.lo = v < a.groups ? 0 : prefix < x.n ? prefix : x.n;
+  if (v < a.groups && x.n == 0) x.ql = 0;
+  const int rows = x.ql * a.G, M = rows <= kFewShared ? kFewShared : kRowTile;
+  x.tiles = (rows + M - 1) / M;
+  x.blocks = x.n > x.lo ? (x.n + kBlock - 1) / kBlock - x.lo / kBlock : 0;
+  return x;
+}
+
+// ------------------------------------------------------------------- plan --
+//
+// A tile of `blocks` blocks is cut into ceil(blocks / C) parts, the same C for all tiles of
+// either kernel.  A piece costs its blocks and `kFixed` more (its page numbers, its first loads,
+// its rows to the workspace).  `places` pieces run at once (a workgroup each, for every KV
+// head), so what is cut so that it fits k rounds takes k (C + kFixed):
+//   sum of weights <= k places,   weight = 1 per part longer than C / 2, else (blocks + kFixed) / (C + kFixed),
+// as small pieces fill what others leave.  The least such C is looked for with k = 1 and k = 2
+// (eight values at a time, three times over), and the cheaper one taken.
+// Cut into W / places blocks instead, without a look at what is left for the second round, 190
+// requests on five prefixes took 950 us in the kernel for many rows, now 600.
+constexpr int kPlan = 512;
+constexpr int kKnown = 4096;      // prefixes and requests whose tiles and blocks are kept in LDS
+constexpr int kRounds = 2;
+constexpr int kLeast[2] = {4, 16};    // blocks of a part at least: few, many rows
+constexpr int kFixed[2] = {10, 6};
+// workgroups of four waves that run at once: by registers three on a compute unit, and two
+constexpr int kPlaces[2] = {768, 512};
+__host__ __device__ constexpr int places_of(int many, int Hkv) { return kPlaces[many] > Hkv ? kPlaces[many] / Hkv : 1; }
+
+// The largest over a wave of values that are not negative (register moves, as wave_sums).
+__device__ __forceinline__ int wave_most(int v) {
+  auto take = [&](int o) { v = o > v ? o : v; };
+  take(__builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));   // row_shr:1
+  take(__builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+  take(__builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+  take(__builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+  take(__builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));   // row_bcast:15
+  take(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));   // row_bcast:31
+  return __builtin_amdgcn_readlane(v, 63);
+}
+
+struct PlanShared {
+  int blocks[kKnown];
+  int tiles[kKnown];             // of few rows as they are, of many negative
+  int lengths[4 * kPlan + 2];    // where they are no more than kPlan each
+  int from[2][kPlan];            // first piece of each, of few and of many rows
+  int parts[kPlan];
+  float w[kPlan / 64][2];
+  int n[kPlan / 64][4];
+  unsigned lo[2][kRounds], hi[2][kRounds];
+  int fits[2][4 * (kPlan / 64)];
+};
+
+__device__ void plan_pieces(const CacheAttnArgs& a) {
+  __shared__ PlanShared sh;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, N = a.groups + a.R;
+  constexpr int NW = kPlan / 64;
+  // the lengths with one load each, as finding a request's group and prefix takes one after the other
+  Lengths l = {a.group_start, a.prefix_lens, a.q_start, a.seq_lens};
+  if (a.R <= kPlan && a.groups <= kPlan) {
+    int* x = sh.lengths;
+    if (tid <= a.groups && a.groups) x[tid] = a.group_start[tid];
+    if (tid < a.groups) x[kPlan + 1 + tid] = a.prefix_lens[tid];
+    if (tid <= a.R) x[2 * kPlan + 1 + tid] = a.q_start[tid];
+    if (tid < a.R) x[3 * kPlan + 2 + tid] = a.seq_lens[tid];
+    if (tid == 0) {   // the last of kPlan + 1
+      if (a.groups == kPlan) x[kPlan] = a.group_start[kPlan];
+      if (a.R == kPlan) x[3 * kPlan + 1] = a.q_start[kPlan];
+    }
+    __syncthreads();
+    l = {x, x + kPlan + 1, x + 2 * kPlan + 1, x + 3 * kPlan + 2};
+  }
+  // what there is: blocks of all tiles, the longest, tiles
+  float W[2] = {0.0f, 0.0f};
+  int count[2] = {0, 0}, longest[2] = {0, 0};
+  Request mine = {};
+#pragma unroll 1
+  for (int v = tid; v < N; v += kPlan) {
+    const Request q = shared_request(a, l, v);
+    if (v == tid) mine = q;
+    const int many = q.ql * a.G > kFewShared;
+    if (v < kKnown) {
+      sh.blocks[v] = q.blocks;
+      sh.tiles[v] = many ? -q.tiles : q.tiles;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const bool on = many == k;
+      W[k] += on ? static_cast<float>(q.tiles) * static_cast<float>(q.blocks) : 0.0f;
+      count[k] += on ? q.tiles : 0;
+      longest[k] = on && q.blocks > longest[k] ? q.blocks : longest[k];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    W[k] = wave_total(W[k]);
+    count[k] = __builtin_amdgcn_readlane(wave_sums(count[k]), 63);
+    longest[k] = wave_most(longest[k]);
+  }
+  if (lane == 0)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      sh.w[w][k] = W[k];
+      sh.n[w][k] = count[k];
+      sh.n[w][2 + k] = longest[k];
+    }
+  __syncthreads();
+  W[0] = W[1] = 0.0f;
+  count[0] = count[1] = longest[0] = longest[1] = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      W[k] += sh.w[i][k];
+      count[k] += sh.n[i][k];
+      longest[k] = sh.n[i][2 + k] > longest[k] ? sh.n[i][2 + k] : longest[k];
+    }
+  // Blocks of a part.
+  auto most = [](float x) { return x < 0x1p26f ? static_cast<unsigned>(x) : 1u << 26; };   // a request has 2^24 at most
+  unsigned C[2];
+  const bool search = N <= kKnown;
+  if (search) {
+    // (at `hi` every tile is a small piece)
+    if (tid < 2 * kRounds) {
+      const int k = tid / kRounds, r = tid % kRounds;
+      const float places = static_cast<float>((r + 1) * places_of(k, a.g.Hkv));
+      const unsigned lo = most((k ? W[1] : W[0]) / places), one = 2 * (k ? longest[1] : longest[0]) + 2;
+      const unsigned all = most(((k ? W[1] : W[0]) + static_cast<float>(kFixed[k]) * static_cast<float>(k ? count[1] : count[0])) / places) + 2;
+      sh.lo[k][r] = lo < static_cast<unsigned>(kLeast[k]) ? kLeast[k] : lo;
+      sh.hi[k][r] = (one > all ? one : all) + kLeast[k];
+    }
+    __syncthreads();
+    // kernel, rounds, and which four of eight values
+    const int k = w / (NW / 2), r = w / (NW / 2 / kRounds) % kRounds, x = w % (NW / 2 / kRounds);
+    constexpr int NZ = 4, NX = NZ * (NW / 2 / kRounds);
+    const float places = static_cast<float>((r + 1) * places_of(k, a.g.Hkv)), fixed = static_cast<float>(kFixed[k]);
+    unsigned lo = sh.lo[k][r], hi = sh.hi[k][r];
+#pragma unroll 1   // (code that runs once costs more to fetch than to run)
+    for (int step = 0; step < 3; ++step) {
+      float fc[NZ], inv[NZ], per[NZ], sum[NZ] = {};
+#pragma unroll
+      for (int z = 0; z < NZ; ++z) {
+        fc[z] = static_cast<float>(lo + static_cast<unsigned>(static_cast<uint64_t>(hi - lo) * (NZ * x + z) / NX));
+        inv[z] = 1.0f / fc[z];
+        per[z] = 1.0f / (fc[z] + fixed);
+      }
+#pragma unroll 1
+      for (int v = lane; v < N; v += 64) {
+        const int t = k ? -sh.tiles[v] : sh.tiles[v];
+        const float b = static_cast<float>(sh.blocks[v]);
+        if (t <= 0) continue;
+        // (binary32: at the edge a part more or less is of no matter)
+#pragma unroll
+        for (int z = 0; z < NZ; ++z) sum[z] += static_cast<float>(t) * (b > 0.5f * fc[z] ? ceilf(b * inv[z]) : (b + fixed) * per[z]);
+      }
+#pragma unroll
+      for (int z = 0; z < NZ; ++z) {
+        sum[z] = wave_total(sum[z]);
+        if (lane == 0) sh.fits[step & 1][NZ * w + z] = sum[z] <= places;
+      }
+      __syncthreads();   // (two sets of answers: the next step writes the other one)
+      // the least value that fits ends the range; the one before it begins it
+      int good = NX;
+#pragma unroll
+      for (int i = NX - 1; i >= 0; --i)
+        if (sh.fits[step & 1][NZ * (w - x) + i]) good = i;
+      const uint64_t d = hi - lo;
+      const unsigned from = lo;
+      if (good < NX) hi = from + static_cast<unsigned>(d * good / NX);
+      if (good > 0) lo = from + static_cast<unsigned>(d * (good - 1) / NX);
+    }
+    if (lane == 0 && x == 0) sh.hi[k][r] = hi;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      C[i] = sh.hi[i][0];
+      unsigned long long cost = C[i] + static_cast<unsigned>(kFixed[i]);
+#pragma unroll
+      for (int j = 1; j < kRounds; ++j) {
+        const unsigned long long other = static_cast<unsigned long long>(j + 1) * (sh.hi[i][j] + static_cast<unsigned>(kFixed[i]));
+        if (other < cost) {
+          cost = other;
+          C[i] = sh.hi[i][j];
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const unsigned c = most(W[i] / static_cast<float>(kRounds * places_of(i, a.g.Hkv))) + 1;
+      C[i] = c < static_cast<unsigned>(kLeast[i]) ? kLeast[i] : c;
+    }
+  }
+  // pieces and places in the workspace, in order
+  int carry[4] = {0, 0, 0, 0};   // pieces and rows of parts, of few and many rows
+  for (int v0 = 0; v0 < N; v0 += kPlan) {
+    const int v = v0 + tid;
+    Request q = {};
+    if (v < N) q = v0 == 0 ? mine : shared_request(a, l, v);
+    const int many = q.ql * a.G > kFewShared;
+    const unsigned c = many ? C[1] : C[0];
+    const int parts = q.tiles ? (q.blocks ? static_cast<int>((q.blocks + c - 1) / c) : 1) : 0;
+    const int val[4] = {many ? 0 : q.tiles * parts, many ? q.tiles * parts : 0, many ? 0 : q.ql * a.G * parts,
+                        many ? q.ql * a.G * parts : 0};
+    int from[4];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      from[i] = wave_sums(val[i]);
+      if (lane == 63) sh.n[w][i] = from[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      int all = 0, before = 0;
+#pragma unroll
+      for (int j = 0; j < NW; ++j) {
+        if (j < w) before += sh.n[j][i];
+        all += sh.n[j][i];
+      }
+      from[i] += carry[i] + before - val[i];
+      carry[i] += all;
+    }
+    sh.from[0][tid] = from[0];
+    sh.from[1][tid] = from[1];
+    sh.parts[tid] = many ? -parts : parts;
+    __syncthreads();
+    // a thread per piece finds its request: the last one whose pieces begin there or before
+    const int here = N - v0 < kPlan ? N - v0 : kPlan;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int p0 = sh.from[k][0], p1 = carry[k] < a.bound[k] ? carry[k] : a.bound[k];   // (past the bound: lengths that do not fit the call)
+      if (p0 < 0) continue;
+      for (int at = p0 + tid; at < p1; at += kPlan) {
+        int x = 0, y = here;
+        while (y - x > 1) {
+          const int m = (x + y) >> 1;
+          if (sh.from[k][m] <= at) x = m; else y = m;
+        }
+        const int n = k ? -sh.parts[x] : sh.parts[x], i = at - sh.from[k][x];
+        if (n > 0) a.pieces[k][at] = make_int4(v0 + x, i / n, i % n, n);
+      }
+    }
+    if (v >= N) continue;
+    const int base = many ? from[3] : from[2];
+    a.requests[2 * v] = make_int4(q.q0, q.ql, q.n, q.first);
+    a.requests[2 * v + 1] = make_int4(q.lo, q.table, base, 0);
+    a.info[v] = make_int2(base, many ? -parts : parts);
+  }
+  if (tid < 2) a.counts[tid] = (tid ? carry[1] : carry[0]) < a.bound[tid] ? (tid ? carry[1] : carry[0]) : a.bound[tid];
+}
+
+// Q of a row after RoPE, rotation and scale as two 16-bit values (see load_q): D / 8 lanes hold it.
+template <int D>
+__device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row, bool fine) {
+  const int b = row_block(threadIdx.x & (D / 8 - 1));
+  const bool ok = row < static_cast<int64_t>(a.T) * a.Hq;   // lanes without a row keep running: the moves between lanes need whole rows
+  const int t = ok ? static_cast<int>(row / a.Hq) : 0, head = ok ? static_cast<int>(row - static_cast<int64_t>(t) * a.Hq) : 0;
+  const uint4 x = *reinterpret_cast<const uint4*>(a.q + static_cast<int64_t>(t) * a.q_ts + head * a.q_hs + b * 8);
+  const uint32_t u[4] = {x.x, x.y, x.z, x.w};
+  float y[8];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    y[2 * e] = cache_h2f(static_cast<uint16_t>(u[e] & 0xffff), a.is_fp16);
+    y[2 * e + 1] = cache_h2f(static_cast<uint16_t>(u[e] >> 16), a.is_fp16);
+  }
+  if (a.rope) {
+    int pos = a.positions[t];
+    pos = pos < 0 ? 0 : pos >= a.rope_rows ? a.rope_rows - 1 : pos;
+    const float4* p = reinterpret_cast<const float4*>(a.rope + static_cast<int64_t>(pos) * D + b * 8);
+    const float4 c[2] = {p[0], p[1]};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float cs = e & 1 ? c[e >> 1].z : c[e >> 1].x, sn = e & 1 ? c[e >> 1].w : c[e >> 1].y;
+      const float m = y[2 * e], n = y[2 * e + 1];
+      y[2 * e] = m * cs - n * sn;
+      y[2 * e + 1] = m * sn + n * cs;
+    }
+  }
+  float scale = a.c;   // scores come out in base 2
+  if (a.had) {
+    hadamard_row<D>(y, b);
+    scale *= row_sign(b);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] *= scale;
+  if (fine) {
+    float m = 0.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
+    m = fmaxf(m, lane_xor<1>(m));
+    m = fmaxf(m, lane_xor<2>(m));
+    m = fmaxf(m, lane_xor<7>(m));
+    if constexpr (D == 128) m = fmaxf(m, lane_xor<8>(m));
+    const float power = row_power(m);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] *= power;
+    if (ok && b == 0) a.back[row] = inverse_power(power);
+  }
+  uint4 hi, lo;
+  split8(y, fine, hi, lo);
+  if (ok) {
+    uint16_t* dst = a.turned + row * 2 * D + b * 8;
+    *reinterpret_cast<uint4*>(dst) = hi;
+    *reinterpret_cast<uint4*>(dst + D) = lo;
+  }
+}
+
+template <int D>
+__global__ __launch_bounds__(kPlan) void k_shared_plan(CacheAttnArgs a) {
+  if (blockIdx.x == 0) return plan_pieces(a);
+  turn_q<D>(a, static_cast<int64_t>(blockIdx.x - 1) * (kPlan * 8 / D) + threadIdx.x / (D / 8), a.out_dtype == RA_FP32);
+}
 
 // A row's parts, 64 at a time: the request's own, then its prefix's.
 template <int D>
@@ -48,8 +412,9 @@ __global__ __launch_bounds__(256) void k_join(CacheAttnArgs a) {
   };
   parts_of(a.groups + r, from, q1, 0);
   s[1].parts = 0;
-  const int g = group_of(a, r);
-  if (g >= 0 && prefix_of(a, g) > 0) {
+  const Lengths l = {a.group_start, a.prefix_lens, a.q_start, a.seq_lens};
+  const int g = group_of(a, l, r);
+  if (g >= 0 && prefix_of(a, l, g) > 0) {
     const int r1 = a.group_start[g + 1] > a.R ? a.R : a.group_start[g + 1];
     const int first = a.q_start[a.group_start[g]];
     parts_of(g, first < 0 ? 0 : first, a.q_start[r1], 1);
@@ -73,10 +438,10 @@ __global__ __launch_bounds__(256) void k_join(CacheAttnArgs a) {
     for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
     mm = fmaxf(M, mm);
     const float x = rescale(ml.x, mm), old = rescale(M, mm);
-    float l = x * ml.y;
+    float sum = x * ml.y;
 #pragma unroll
-    for (int d = 32; d; d >>= 1) l += __shfl_xor(l, d);
-    L = L * old + l;
+    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
+    L = L * old + sum;
     M = mm;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) out[e] *= old;
@@ -105,16 +470,17 @@ __global__ __launch_bounds__(256) void k_join(CacheAttnArgs a) {
 
 template <int D>
 hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
-  const int64_t rows = static_cast<int64_t>(a.T) * a.G, all = static_cast<int64_t>(a.R) + a.groups;
-  const dim3 few_grid(static_cast<unsigned>((all + a.target) * a.g.Hkv));
-  if (a.out_dtype == RA_FP32) k_fine_few<D, 1, 2, kShared><<<few_grid, dim3(256), 0, s>>>(a);
-  else k_few<D, 1, 2, kShared><<<few_grid, dim3(256), 0, s>>>(a);
+  const int64_t rows = static_cast<int64_t>(a.T) * a.Hq;
+  k_shared_plan<D><<<dim3(static_cast<unsigned>(1 + (rows + kPlan * 8 / D - 1) / (kPlan * 8 / D))), dim3(kPlan), 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (rows > kFewShared) {
-    // a prefix or request of many rows has more than kFewShared of them; prefixes and requests take every row once each
-    const int64_t most = 2 * rows / kFewShared < all ? 2 * rows / kFewShared : all;
-    const dim3 grid(static_cast<unsigned>((most + 2 * rows / kRowTile + a.target_rows) * a.g.Hkv));
+  const dim3 few_grid(static_cast<unsigned>(a.bound[0]) * a.g.Hkv);
+  if (a.out_dtype == RA_FP32) k_fine_few<D, 1, 2, kShared><<<few_grid, dim3(256), 0, s>>>(a);
+  else k_few<D, 1, 2, kShared><<<few_grid, dim3(256), 0, s>>>(a);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.bound[1]) {
+    const dim3 grid(static_cast<unsigned>(a.bound[1]) * a.g.Hkv);
     if (a.out_dtype == RA_FP32) {
       if (a.is_fp16) k_fine_rows<D, true, kShared><<<grid, dim3(256), 0, s>>>(a);
       else k_fine_rows<D, false, kShared><<<grid, dim3(256), 0, s>>>(a);
@@ -133,19 +499,37 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
 }
 
 struct SharedSpace {
-  int64_t rows;             // of every KV head
-  size_t ml, info, bytes;   // offsets
+  int64_t rows;        // of parts, for every KV head
+  int64_t bound[2];    // pieces of few and of many rows
+  size_t ml, requests, pieces[2], info, counts, back, turned, bytes;   // offsets
 };
-// Rows of all parts: every row once for its prefix and once for its own keys,
-// and those of the pieces that cutting adds (at most the targets, a tile each).
+// Every row once for its prefix and once for its own keys; cutting adds at most the pieces of all rounds, a tile each
+// (sum over tiles of parts - 1 <= W / C).  Prefixes and requests of many rows have more than 16 of them.
 SharedSpace space_of(int D, int Hkv, int G, int R, int groups, int T) {
   SharedSpace x;
-  x.rows = 2 * static_cast<int64_t>(T) * G + static_cast<int64_t>(kFewShared) * target_of(kPieces, Hkv) +
-           static_cast<int64_t>(kRowTile) * target_of(kRowPieces, Hkv);
-  const size_t n = static_cast<size_t>(x.rows) * Hkv;
-  x.ml = n * D * sizeof(float);
-  x.info = x.ml + n * sizeof(float2);
-  x.bytes = x.info + (static_cast<size_t>(R) + groups) * sizeof(int2);
+  const int64_t rows = 2 * static_cast<int64_t>(T) * G, all = static_cast<int64_t>(R) + groups;
+  const int64_t few = kRounds * places_of(0, Hkv), many = kRounds * places_of(1, Hkv);
+  x.rows = rows + kFewShared * few + kRowTile * many;
+  x.bound[0] = (all < rows ? all : rows) + few;
+  const int64_t more = rows / kFewShared;
+  x.bound[1] = rows / 2 > kFewShared ? (all < more ? all : more) + rows / kRowTile + many : 0;
+  const size_t n = static_cast<size_t>(x.rows) * Hkv, q = static_cast<size_t>(T) * G * Hkv;
+  size_t at = n * D * sizeof(float);
+  auto take = [&](size_t bytes) {
+    at = (at + 15) / 16 * 16;
+    const size_t here = at;
+    at += bytes;
+    return here;
+  };
+  x.ml = take(n * sizeof(float2));
+  x.requests = take(2 * static_cast<size_t>(all) * sizeof(int4));
+  x.pieces[0] = take(static_cast<size_t>(x.bound[0]) * sizeof(int4));
+  x.pieces[1] = take(static_cast<size_t>(x.bound[1]) * sizeof(int4));
+  x.info = take(static_cast<size_t>(all) * sizeof(int2));
+  x.counts = take(2 * sizeof(int));
+  x.back = take(q * sizeof(float));
+  x.turned = take(q * 4 * D);
+  x.bytes = at;
   return x;
 }
 
@@ -161,10 +545,16 @@ hipError_t launch_cache_attn_shared(const CacheAttnArgs& a, int D, void* workspa
   char* ws = static_cast<char*>(workspace);
   b.part_o = reinterpret_cast<float*>(ws);
   b.part_ml = reinterpret_cast<float2*>(ws + x.ml);
+  b.requests = reinterpret_cast<int4*>(ws + x.requests);
+  for (int i = 0; i < 2; ++i) {
+    b.pieces[i] = reinterpret_cast<int4*>(ws + x.pieces[i]);
+    b.bound[i] = static_cast<int>(x.bound[i]);
+  }
   b.info = reinterpret_cast<int2*>(ws + x.info);
+  b.counts = reinterpret_cast<int*>(ws + x.counts);
+  b.back = reinterpret_cast<float*>(ws + x.back);
+  b.turned = reinterpret_cast<uint16_t*>(ws + x.turned);
   b.part_rows = x.rows;
-  b.target = target_of(kPieces, a.g.Hkv);
-  b.target_rows = target_of(kRowPieces, a.g.Hkv);
   return D == 128 ? shared_d<128>(b, s) : shared_d<64>(b, s);
 }
 
