@@ -97,6 +97,7 @@ struct CacheAttnArgs {
   // set by the launch
   int4* requests;                   // [groups + R][2] prefixes and requests
   int2* info;                       // [groups + R] where their parts are: first row, parts (negative: from the back)
+  int2* owner;                      // [T] request and group of a token
   int4* pieces[2];                  // of few and of many rows
   int* counts;                      // [2]
   int bound[2];                     // of the pieces

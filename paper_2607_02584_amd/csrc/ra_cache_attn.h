@@ -689,20 +689,28 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const 
   }
 }
 
-template <int D, int NT, int KT, bool FINE, Keys K = kAll>
-__device__ __forceinline__ void few_rows(const CacheAttnArgs& a) {
+template <int D, int NT, bool FINE>
+struct FewLds {
+  static constexpr int M = 16 * NT, kStride = D + 4;   // floats, against bank conflicts
+  __align__(16) float so[4][16][kStride];
+  float sm[4][M], sl[4][M];
+  SchedShared sched;
+  __align__(16) uint4 sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
+  float sback[FINE ? M : 1];
+};
+
+// Piece x0 of KV head h.
+template <int D, int NT, int KT, bool FINE, Keys K>
+__device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, FINE>& lds, int x0, int h) {
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
-  constexpr int kStride = D + 4;                       // floats, against bank conflicts
-  __shared__ __align__(16) float so[4][16][kStride];
-  __shared__ float sm[4][M], sl[4][M];
-  __shared__ SchedShared sched;
-  __shared__ __align__(16) uint4 sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
-  __shared__ float sback[FINE ? M : 1];
+  auto& so = lds.so;
+  auto& sm = lds.sm;
+  auto& sl = lds.sl;
+  auto& sq_all = lds.sq_all;
+  auto& sback = lds.sback;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), g = lane >> 4;
-  // heads fastest: the heads of a page, neighbours in memory, are read together
-  const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!take_piece<M, K>(a, sched, x0, a.target, &p)) return;
+  if (!take_piece<M, K>(a, lds.sched, x0, a.target, &p)) return;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
 
   const int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;   // of this tile
@@ -996,28 +1004,29 @@ __device__ __forceinline__ void each(F&& f) {
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
 // TERMS: bf16 values that hold P * (V's scale); three come with binary16 pairs of Q.
-template <int D, bool F16, int TERMS, Keys K = kAll>
-__device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
-  constexpr bool FINE = TERMS == 3;
-  typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
-  constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
+template <int D>
+struct RowsLds {
   struct Scales {
     float ks[64], vs[64];
     unsigned long long there, plain;   // keys that are on a page; those of them with a finite V
   };
-  struct Buf {
-    uint4 k[2][D / 8][64];
-    uint4 v[2][8][D];
-    Scales sc[2];
-  };
-  __shared__ __align__(16) Buf buf;
-  __shared__ SchedShared sched;
+  __align__(16) uint4 k[2][D / 8][64];
+  __align__(16) uint4 v[2][8][D];
+  Scales sc[2];
+  SchedShared sched;
+};
+
+// Piece x0 of KV head h.
+template <int D, bool F16, int TERMS, Keys K>
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& buf, int x0, int h) {
+  constexpr bool FINE = TERMS == 3;
+  typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
+  constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
+  typedef typename RowsLds<D>::Scales Scales;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
-  // heads fastest: workgroups go round the 8 XCDs, so a head's keys stay in few L2s
-  const int x0 = blockIdx.x / a.g.Hkv, h = blockIdx.x - x0 * a.g.Hkv;
   Piece p;
-  if (!take_piece<M, K>(a, sched, x0, a.target_rows, &p)) return;
+  if (!take_piece<M, K>(a, buf.sched, x0, a.target_rows, &p)) return;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
   if (K != kShared && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
 
@@ -1458,7 +1467,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a) {
 // then the sum of their outputs, eight at a time (D / 4 threads each).
 constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 
-template <int D, int M, Keys K = kAll>
+template <int D, int M, Keys K>
 __device__ __forceinline__ void join_tiles(const CacheAttnArgs& a, int target, int per_group) {
   constexpr int W = D / 4, NG = 256 / W;
   __shared__ SchedShared sched;
@@ -1567,23 +1576,34 @@ Grid grid_of(const CacheAttnArgs& a, int M, int target) {
 int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }
 
 // ---------------------------------------------------------------- kernels --
+//
+// Heads are fastest: the heads of a page, neighbours in memory, are read together,
+// and as workgroups go round the 8 XCDs a head's keys stay in few L2s.
 
 template <int D, int NT, int KT, Keys K>
 __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
-  few_rows<D, NT, KT, false, K>(a);
+  __shared__ FewLds<D, NT, false> lds;
+  const int x0 = blockIdx.x / a.g.Hkv;
+  few_rows<D, NT, KT, false, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, int NT, int KT, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
-  few_rows<D, NT, KT, true, K>(a);
+  __shared__ FewLds<D, NT, true> lds;
+  const int x0 = blockIdx.x / a.g.Hkv;
+  few_rows<D, NT, KT, true, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 
 template <int D, bool F16, bool LO, Keys K>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
-  many_rows<D, F16, LO ? 2 : 1, K>(a);
+  __shared__ RowsLds<D> lds;
+  const int x0 = blockIdx.x / a.g.Hkv;
+  many_rows<D, F16, LO ? 2 : 1, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, bool F16, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
-  many_rows<D, F16, 3, K>(a);
+  __shared__ RowsLds<D> lds;
+  const int x0 = blockIdx.x / a.g.Hkv;
+  many_rows<D, F16, 3, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 
 template <int D, int M, Keys K>

@@ -13,7 +13,9 @@
 // Four launches: k_shared_plan cuts prefixes and requests into pieces and turns
 // Q, once for all the pieces that take a row (in each of them it was 5 of a
 // piece's 66 us); the kernels for few and for many rows go through their
-// lists and leave partial rows in the workspace; a wave per row joins them.
+// lists and leave partial rows in the workspace; a wave per row joins them.  (Both
+// kinds of pieces mixed in one launch took as long as one after the other: a piece of many rows that
+// waits for one of few ends as much later.)
 //
 // Bound by HBM while a group's rows are few, by the matrix cores and the softmax
 // beside them from some 64 rows on.
@@ -318,7 +320,10 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     a.requests[2 * v + 1] = make_int4(q.lo, q.table, base, 0);
     a.info[v] = make_int2(base, many ? -parts : parts);
   }
-  if (tid < 2) a.counts[tid] = (tid ? carry[1] : carry[0]) < a.bound[tid] ? (tid ? carry[1] : carry[0]) : a.bound[tid];
+  if (tid < 2) {
+    const int n = tid ? carry[1] : carry[0];
+    a.counts[tid] = n < 0 ? 0 : n < a.bound[tid] ? n : a.bound[tid];
+  }
 }
 
 // Q of a row after RoPE, rotation and scale as two 16-bit values (see load_q): D / 8 lanes hold it.
@@ -377,60 +382,71 @@ __device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row, bool
   }
 }
 
+// The request and group that each of a workgroup's tokens belongs to; {-1, ..} for none.
+__device__ __forceinline__ void find_owners(const CacheAttnArgs& a, int64_t row0, int64_t row1) {
+  const int64_t last = (row1 < static_cast<int64_t>(a.T) * a.Hq ? row1 : static_cast<int64_t>(a.T) * a.Hq) - 1;
+  // tokens whose first head is among these rows
+  const int t0 = static_cast<int>((row0 + a.Hq - 1) / a.Hq), t1 = static_cast<int>(last / a.Hq);
+  for (int t = t0 + threadIdx.x; t <= t1; t += kPlan) {
+    int r = 0, y = a.R;   // q_start[r] <= t < q_start[y]
+    while (y - r > 1) {
+      const int m = (r + y) >> 1;
+      if (a.q_start[m] <= t) r = m; else y = m;
+    }
+    int2 x = make_int2(-1, -1);
+    if (a.q_start[r] <= t && t < a.q_start[r + 1]) {
+      const Lengths l = {a.group_start, a.prefix_lens, a.q_start, a.seq_lens};
+      const int g = group_of(a, l, r);
+      x = make_int2(r, g >= 0 && prefix_of(a, l, g) > 0 ? g : -1);
+    }
+    a.owner[t] = x;
+  }
+}
+
 template <int D>
 __global__ __launch_bounds__(kPlan) void k_shared_plan(CacheAttnArgs a) {
   if (blockIdx.x == 0) return plan_pieces(a);
+  constexpr int kRows = kPlan * 8 / D;
+  find_owners(a, static_cast<int64_t>(blockIdx.x - 1) * kRows, static_cast<int64_t>(blockIdx.x) * kRows);
   turn_q<D>(a, static_cast<int64_t>(blockIdx.x - 1) * (kPlan * 8 / D) + threadIdx.x / (D / 8), a.out_dtype == RA_FP32);
 }
 
-// A row's parts, 64 at a time: the request's own, then its prefix's.
+// ---------------------------------------------------------------- kernels --
+
+// The parts of a row, 64 at a time: the request's own, then its prefix's.
 template <int D>
 __global__ __launch_bounds__(256) void k_join(CacheAttnArgs a) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int t = blockIdx.x, head = blockIdx.y * 4 + w;
   if (head >= a.Hq) return;
-  int r = 0, y = a.R;   // q_start[r] <= t < q_start[y]
-  while (y - r > 1) {
-    const int m = (r + y) >> 1;
-    if (a.q_start[m] <= t) r = m; else y = m;
-  }
-  const int q0 = a.q_start[r], q1 = a.q_start[r + 1];
-  if (t < q0 || t >= q1) return;
+  const int2 of = a.owner[t];   // the token's request and group
+  const int r = __builtin_amdgcn_readfirstlane(of.x), g = __builtin_amdgcn_readfirstlane(of.y);
+  if (r < 0) return;
   const int h = head / a.G, z = head - h * a.G;
-  struct {
-    int base, parts, rows, row;
-    bool many;
-  } s[2];
-  const int from = q0 < 0 ? 0 : q0;
-  auto parts_of = [&](int v, int first, int end, int which) {
+  int first[2], parts[2], rows[2], row[2];
+  bool many[2];
+  auto take = [&](int i, int v) {
     const int2 x = a.info[v];
-    s[which].many = x.y < 0;
-    s[which].parts = x.y < 0 ? -x.y : x.y;
-    s[which].base = x.x;
-    s[which].rows = ((end > a.T ? a.T : end) - first) * a.G;
-    s[which].row = (t - first) * a.G + z;
+    const int4 q = a.requests[2 * v];   // q0, ql
+    first[i] = x.x;
+    many[i] = x.y < 0;
+    parts[i] = x.y < 0 ? -x.y : x.y;
+    rows[i] = q.y * a.G;
+    row[i] = (t - q.x) * a.G + z;
   };
-  parts_of(a.groups + r, from, q1, 0);
-  s[1].parts = 0;
-  const Lengths l = {a.group_start, a.prefix_lens, a.q_start, a.seq_lens};
-  const int g = group_of(a, l, r);
-  if (g >= 0 && prefix_of(a, l, g) > 0) {
-    const int r1 = a.group_start[g + 1] > a.R ? a.R : a.group_start[g + 1];
-    const int first = a.q_start[a.group_start[g]];
-    parts_of(g, first < 0 ? 0 : first, a.q_start[r1], 1);
-  }
-  // (more parts than the cutting makes: lengths changed under the call)
-  const int n0 = s[0].parts < 65536 ? s[0].parts : 0, n = n0 + (s[1].parts < 65536 ? s[1].parts : 0);
+  take(0, a.groups + r);
+  parts[1] = 0;
+  if (g >= 0) take(1, g);
+  else first[1] = rows[1] = row[1] = 0, many[1] = false;
+  const int n0 = parts[0], n = n0 + parts[1];
   float M = kNegInf, L = 0.0f, out[D / 64] = {};
   for (int i0 = 0; i0 < n; i0 += 64) {
     const int i = i0 + lane;
     int64_t at = -1;
     if (i < n) {
-      const bool own = i < n0;
-      const int base = own ? s[0].base : s[1].base, part = own ? i : i - n0, rows = own ? s[0].rows : s[1].rows;
-      const int row = own ? s[0].row : s[1].row, parts = own ? n0 : n - n0;
-      at = (own ? s[0].many : s[1].many) ? shared_at<true>(a, base, parts, part, rows, row, h)
-                                         : shared_at<false>(a, base, parts, part, rows, row, h);
+      const int k = i < n0 ? 0 : 1, part = k ? i - n0 : i;
+      at = (k ? many[1] : many[0]) ? shared_at<true>(a, k ? first[1] : first[0], k ? parts[1] : n0, part, k ? rows[1] : rows[0], k ? row[1] : row[0], h)
+                                   : shared_at<false>(a, k ? first[1] : first[0], k ? parts[1] : n0, part, k ? rows[1] : rows[0], k ? row[1] : row[0], h);
     }
     const float2 ml = at >= 0 ? a.part_ml[at] : make_float2(kNegInf, 0.0f);
     float mm = ml.x;
@@ -438,29 +454,26 @@ __global__ __launch_bounds__(256) void k_join(CacheAttnArgs a) {
     for (int d = 32; d; d >>= 1) mm = fmaxf(mm, __shfl_xor(mm, d));
     mm = fmaxf(M, mm);
     const float x = rescale(ml.x, mm), old = rescale(M, mm);
-    float sum = x * ml.y;
-#pragma unroll
-    for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-    L = L * old + sum;
+    L = L * old + wave_total(x * ml.y);
     M = mm;
 #pragma unroll
     for (int e = 0; e < D / 64; ++e) out[e] *= old;
-    const int many = n - i0 < 64 ? n - i0 : 64;
+    const int count = n - i0 < 64 ? n - i0 : 64;
     const int lo = static_cast<int>(at), hi = static_cast<int>(at >> 32);
-    // eight at a time, so that their loads are under way together (places that are none: row 0, left out)
-    for (int k0 = 0; k0 < many; k0 += 8) {
-      float v[8][D / 64], f[8];
+    // sixteen at a time, so that their loads are under way together (places that are none: 0)
+#pragma unroll 1
+    for (int k0 = 0; k0 < count; k0 += 16) {
+      float v[16][D / 64], f[16];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
+      for (int k = 0; k < 16; ++k) {
         f[k] = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), k0 + k));
         const int64_t p = static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(__builtin_amdgcn_readlane(hi, k0 + k))) << 32 |
                                                static_cast<uint32_t>(__builtin_amdgcn_readlane(lo, k0 + k)));
-        const bool there = p >= 0;
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) v[k][e] = there ? a.part_o[p * D + lane * (D / 64) + e] : 0.0f;
+        for (int e = 0; e < D / 64; ++e) v[k][e] = p >= 0 ? a.part_o[p * D + lane * (D / 64) + e] : 0.0f;
       }
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
+      for (int k = 0; k < 16; ++k)
 #pragma unroll
         for (int e = 0; e < D / 64; ++e) out[e] += f[k] * v[k][e];
     }
@@ -481,19 +494,18 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   if (a.bound[1]) {
     const dim3 grid(static_cast<unsigned>(a.bound[1]) * a.g.Hkv);
-    if (a.out_dtype == RA_FP32) {
-      if (a.is_fp16) k_fine_rows<D, true, kShared><<<grid, dim3(256), 0, s>>>(a);
-      else k_fine_rows<D, false, kShared><<<grid, dim3(256), 0, s>>>(a);
-    } else if (a.out_dtype == RA_FP16) {
-      if (a.is_fp16) k_rows<D, true, true, kShared><<<grid, dim3(256), 0, s>>>(a);
-      else k_rows<D, false, true, kShared><<<grid, dim3(256), 0, s>>>(a);
-    } else {
-      if (a.is_fp16) k_rows<D, true, false, kShared><<<grid, dim3(256), 0, s>>>(a);
-      else k_rows<D, false, false, kShared><<<grid, dim3(256), 0, s>>>(a);
-    }
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    // P in as many bf16 values as the output shows
+    auto go = [&](auto f16) {
+      constexpr bool F16 = decltype(f16)::value;
+      if (a.out_dtype == RA_FP32) k_fine_rows<D, F16, kShared><<<grid, dim3(256), 0, s>>>(a);
+      else if (a.out_dtype == RA_FP16) k_rows<D, F16, true, kShared><<<grid, dim3(256), 0, s>>>(a);
+      else k_rows<D, F16, false, kShared><<<grid, dim3(256), 0, s>>>(a);
+    };
+    if (a.is_fp16) go(std::integral_constant<bool, true>{});
+    else go(std::integral_constant<bool, false>{});
   }
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
   k_join<D><<<dim3(a.T, (a.Hq + 3) / 4), dim3(256), 0, s>>>(a);
   return hipGetLastError();
 }
@@ -501,7 +513,7 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
 struct SharedSpace {
   int64_t rows;        // of parts, for every KV head
   int64_t bound[2];    // pieces of few and of many rows
-  size_t ml, requests, pieces[2], info, counts, back, turned, bytes;   // offsets
+  size_t ml, requests, pieces[2], info, owner, counts, back, turned, bytes;   // offsets
 };
 // Every row once for its prefix and once for its own keys; cutting adds at most the pieces of all rounds, a tile each
 // (sum over tiles of parts - 1 <= W / C).  Prefixes and requests of many rows have more than 16 of them.
@@ -526,6 +538,7 @@ SharedSpace space_of(int D, int Hkv, int G, int R, int groups, int T) {
   x.pieces[0] = take(static_cast<size_t>(x.bound[0]) * sizeof(int4));
   x.pieces[1] = take(static_cast<size_t>(x.bound[1]) * sizeof(int4));
   x.info = take(static_cast<size_t>(all) * sizeof(int2));
+  x.owner = take(static_cast<size_t>(T) * sizeof(int2));
   x.counts = take(2 * sizeof(int));
   x.back = take(q * sizeof(float));
   x.turned = take(q * 4 * D);
@@ -551,6 +564,7 @@ hipError_t launch_cache_attn_shared(const CacheAttnArgs& a, int D, void* workspa
     b.bound[i] = static_cast<int>(x.bound[i]);
   }
   b.info = reinterpret_cast<int2*>(ws + x.info);
+  b.owner = reinterpret_cast<int2*>(ws + x.owner);
   b.counts = reinterpret_cast<int*>(ws + x.counts);
   b.back = reinterpret_cast<float*>(ws + x.back);
   b.turned = reinterpret_cast<uint16_t*>(ws + x.turned);
