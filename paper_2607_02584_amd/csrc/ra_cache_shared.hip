@@ -96,9 +96,10 @@ constexpr int kKnown = 4096;      // prefixes and requests whose tiles and block
 constexpr int kRounds = 2;
 constexpr int kLeast[2] = {4, 16};    // blocks of a part at least: few, many rows
 constexpr int kFixed[2] = {10, 6};
-// workgroups of four waves that run at once: by registers three on a compute unit, and two
-constexpr int kPlaces[2] = {768, 512};
-__host__ __device__ constexpr int places_of(int many, int Hkv) { return kPlaces[many] > Hkv ? kPlaces[many] / Hkv : 1; }
+constexpr float kFewCost = 0.3f;      // of a block of keys for few rows, in blocks for many
+// workgroups of four waves that run at once: two on a compute unit, by registers and LDS
+constexpr int kPlaces = 512;
+__host__ __device__ constexpr int places_of(int Hkv) { return kPlaces > Hkv ? kPlaces / Hkv : 1; }
 
 // The largest over a wave of values that are not negative (register moves, as wave_sums).
 __device__ __forceinline__ int wave_most(int v) {
@@ -119,9 +120,9 @@ struct PlanShared {
   int from[2][kPlan];            // first piece of each, of few and of many rows
   int parts[kPlan];
   float w[kPlan / 64][2];
-  int n[kPlan / 64][4];
+  int n[kPlan / 64][6];
   unsigned lo[2][kRounds], hi[2][kRounds];
-  int fits[2][4 * (kPlan / 64)];
+  int fits[2][4 * (kPlan / 64)], wide[3][2 * kRounds];
 };
 
 __device__ void plan_pieces(const CacheAttnArgs& a) {
@@ -145,7 +146,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   }
   // what there is: blocks of all tiles, the longest, tiles
   float W[2] = {0.0f, 0.0f};
-  int count[2] = {0, 0}, longest[2] = {0, 0};
+  int count[2] = {0, 0}, longest[2] = {0, 0}, finest[2] = {0, 0};   // finest: pieces of kLeast blocks
   Request mine = {};
 #pragma unroll 1
   for (int v = tid; v < N; v += kPlan) {
@@ -162,6 +163,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       W[k] += on ? static_cast<float>(q.tiles) * static_cast<float>(q.blocks) : 0.0f;
       count[k] += on ? q.tiles : 0;
       longest[k] = on && q.blocks > longest[k] ? q.blocks : longest[k];
+      finest[k] += on ? q.tiles * ((q.blocks + kLeast[k] - 1) / kLeast[k]) : 0;
     }
   }
 #pragma unroll
@@ -169,6 +171,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     W[k] = wave_total(W[k]);
     count[k] = __builtin_amdgcn_readlane(wave_sums(count[k]), 63);
     longest[k] = wave_most(longest[k]);
+    finest[k] = __builtin_amdgcn_readlane(wave_sums(finest[k]), 63);
   }
   if (lane == 0)
 #pragma unroll
@@ -176,10 +179,11 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       sh.w[w][k] = W[k];
       sh.n[w][k] = count[k];
       sh.n[w][2 + k] = longest[k];
+      sh.n[w][4 + k] = finest[k];
     }
   __syncthreads();
   W[0] = W[1] = 0.0f;
-  count[0] = count[1] = longest[0] = longest[1] = 0;
+  count[0] = count[1] = longest[0] = longest[1] = finest[0] = finest[1] = 0;
 #pragma unroll
   for (int i = 0; i < NW; ++i)
 #pragma unroll
@@ -187,26 +191,46 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       W[k] += sh.w[i][k];
       count[k] += sh.n[i][k];
       longest[k] = sh.n[i][2 + k] > longest[k] ? sh.n[i][2 + k] : longest[k];
+      finest[k] += sh.n[i][4 + k];
     }
+  // either kind's share of the places
+  int places_for[2];
+  {
+    const int all = places_of(a.g.Hkv);
+    const float few = kFewCost * (W[0] + static_cast<float>(kFixed[0]) * static_cast<float>(count[0]));
+    const float many = W[1] + static_cast<float>(kFixed[1]) * static_cast<float>(count[1]);
+    int n = static_cast<int>(static_cast<float>(all) * many / (few + many + 1e-6f) + 0.5f);
+    n = n < 1 || all < 2 ? 1 : n >= all ? (count[0] ? all - 1 : all) : n;
+    places_for[1] = n;
+    places_for[0] = count[1] && all > n ? all - n : all;
+  }
   // Blocks of a part.
   auto most = [](float x) { return x < 0x1p26f ? static_cast<unsigned>(x) : 1u << 26; };   // a request has 2^24 at most
   unsigned C[2];
-  const bool search = N <= kKnown;
-  if (search) {
-    // (at `hi` every tile is a small piece)
+  if (finest[0] <= places_for[0] && finest[1] <= places_for[1]) {
+    C[0] = kLeast[0];
+    C[1] = kLeast[1];
+  } else if (N <= kKnown) {
+    // (at `hi` every tile is a small piece, or the tiles' last parts fill what is left of the places)
     if (tid < 2 * kRounds) {
       const int k = tid / kRounds, r = tid % kRounds;
-      const float places = static_cast<float>((r + 1) * places_of(k, a.g.Hkv));
+      const float places = static_cast<float>((r + 1) * (k ? places_for[1] : places_for[0]));
       const unsigned lo = most((k ? W[1] : W[0]) / places), one = 2 * (k ? longest[1] : longest[0]) + 2;
       const unsigned all = most(((k ? W[1] : W[0]) + static_cast<float>(kFixed[k]) * static_cast<float>(k ? count[1] : count[0])) / places) + 2;
       sh.lo[k][r] = lo < static_cast<unsigned>(kLeast[k]) ? kLeast[k] : lo;
-      sh.hi[k][r] = (one > all ? one : all) + kLeast[k];
+      unsigned hi = one > all ? one : all;
+      const float left = places - static_cast<float>(k ? count[1] : count[0]);
+      if (left >= 1.0f) {
+        const unsigned even = most((k ? W[1] : W[0]) / left) + 1;
+        hi = even < hi ? even : hi;
+      }
+      sh.hi[k][r] = hi > static_cast<unsigned>(kLeast[k]) ? hi : kLeast[k];
     }
     __syncthreads();
     // kernel, rounds, and which four of eight values
     const int k = w / (NW / 2), r = w / (NW / 2 / kRounds) % kRounds, x = w % (NW / 2 / kRounds);
     constexpr int NZ = 4, NX = NZ * (NW / 2 / kRounds);
-    const float places = static_cast<float>((r + 1) * places_of(k, a.g.Hkv)), fixed = static_cast<float>(kFixed[k]);
+    const float places = static_cast<float>((r + 1) * (k ? places_for[1] : places_for[0])), fixed = static_cast<float>(kFixed[k]);
     unsigned lo = sh.lo[k][r], hi = sh.hi[k][r];
 #pragma unroll 1   // (code that runs once costs more to fetch than to run)
     for (int step = 0; step < 3; ++step) {
@@ -241,6 +265,13 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       const unsigned from = lo;
       if (good < NX) hi = from + static_cast<unsigned>(d * good / NX);
       if (good > 0) lo = from + static_cast<unsigned>(d * (good - 1) / NX);
+      // on while any of the four ranges is wide
+      if (lane == 0 && x == 0) sh.wide[step][k * kRounds + r] = hi > lo + 1 + lo / 32;
+      __syncthreads();
+      int wide = 0;
+#pragma unroll
+      for (int i = 0; i < 2 * kRounds; ++i) wide |= sh.wide[step][i];
+      if (!wide) break;
     }
     if (lane == 0 && x == 0) sh.hi[k][r] = hi;
     __syncthreads();
@@ -260,7 +291,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   } else {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const unsigned c = most(W[i] / static_cast<float>(kRounds * places_of(i, a.g.Hkv))) + 1;
+      const unsigned c = most(W[i] / static_cast<float>(kRounds * places_for[i])) + 1;
       C[i] = c < static_cast<unsigned>(kLeast[i]) ? kLeast[i] : c;
     }
   }
@@ -413,6 +444,20 @@ __global__ __launch_bounds__(kPlan) void k_shared_plan(CacheAttnArgs a) {
 
 // ---------------------------------------------------------------- kernels --
 
+// Both kinds of pieces in one launch: those of many rows begin on their share
+// of the places, those of few rows, which wait for memory for most of their time, follow each other on the rest.
+template <int D, bool F16, int TERMS>
+__global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a) {
+  constexpr bool FINE = TERMS == 3;
+  __shared__ union {
+    FewLds<D, 1, FINE> few;
+    RowsLds<D> rows;
+  } lds;
+  const int x = blockIdx.x / a.g.Hkv, h = blockIdx.x - x * a.g.Hkv, many = __builtin_amdgcn_readfirstlane(a.counts[1]);
+  if (x < many) many_rows<D, F16, TERMS, kShared>(a, lds.rows, x, h);
+  else few_rows<D, 1, 2, FINE, kShared>(a, lds.few, x - many, h);
+}
+
 // The parts of a row, 64 at a time: the request's own, then its prefix's.
 template <int D>
 __global__ __launch_bounds__(256) void k_join(CacheAttnArgs a) {
@@ -487,19 +532,17 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
   k_shared_plan<D><<<dim3(static_cast<unsigned>(1 + (rows + kPlan * 8 / D - 1) / (kPlan * 8 / D))), dim3(kPlan), 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 few_grid(static_cast<unsigned>(a.bound[0]) * a.g.Hkv);
-  if (a.out_dtype == RA_FP32) k_fine_few<D, 1, 2, kShared><<<few_grid, dim3(256), 0, s>>>(a);
-  else k_few<D, 1, 2, kShared><<<few_grid, dim3(256), 0, s>>>(a);
-  e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  if (a.bound[1]) {
-    const dim3 grid(static_cast<unsigned>(a.bound[1]) * a.g.Hkv);
+  const dim3 grid(static_cast<unsigned>(a.bound[0] + a.bound[1]) * a.g.Hkv);
+  if (!a.bound[1]) {
+    if (a.out_dtype == RA_FP32) k_fine_few<D, 1, 2, kShared><<<grid, dim3(256), 0, s>>>(a);
+    else k_few<D, 1, 2, kShared><<<grid, dim3(256), 0, s>>>(a);
+  } else {
     // P in as many bf16 values as the output shows
     auto go = [&](auto f16) {
       constexpr bool F16 = decltype(f16)::value;
-      if (a.out_dtype == RA_FP32) k_fine_rows<D, F16, kShared><<<grid, dim3(256), 0, s>>>(a);
-      else if (a.out_dtype == RA_FP16) k_rows<D, F16, true, kShared><<<grid, dim3(256), 0, s>>>(a);
-      else k_rows<D, F16, false, kShared><<<grid, dim3(256), 0, s>>>(a);
+      if (a.out_dtype == RA_FP32) k_both<D, F16, 3><<<grid, dim3(256), 0, s>>>(a);
+      else if (a.out_dtype == RA_FP16) k_both<D, F16, 2><<<grid, dim3(256), 0, s>>>(a);
+      else k_both<D, F16, 1><<<grid, dim3(256), 0, s>>>(a);
     };
     if (a.is_fp16) go(std::integral_constant<bool, true>{});
     else go(std::integral_constant<bool, false>{});
@@ -520,7 +563,7 @@ struct SharedSpace {
 SharedSpace space_of(int D, int Hkv, int G, int R, int groups, int T) {
   SharedSpace x;
   const int64_t rows = 2 * static_cast<int64_t>(T) * G, all = static_cast<int64_t>(R) + groups;
-  const int64_t few = kRounds * places_of(0, Hkv), many = kRounds * places_of(1, Hkv);
+  const int64_t few = kRounds * places_of(Hkv), many = few;   // cut off tiles at most
   x.rows = rows + kFewShared * few + kRowTile * many;
   x.bound[0] = (all < rows ? all : rows) + few;
   const int64_t more = rows / kFewShared;
