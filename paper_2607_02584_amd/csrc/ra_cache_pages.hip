@@ -329,16 +329,24 @@ __global__ __launch_bounds__(kPlan) void k_trim_plan(TrimArgs a) {
   }
 }
 
-__device__ __forceinline__ void let_go(const PageTables& t, const TrimSpace& s, int id) {
-  if (is_page(id, t) && atomicSub(&t.refs[id], 1) == 0) atomicAdd(&s.chunk[id >> kChunkLog], 1);
+// (A workgroup counts its marked pages in LDS first: one addition in memory for each of them
+// met at a few dozen addresses and made 123 us of what takes 10, 1000 requests that let go of 60 000 entries.)
+constexpr int kNear = 4096;   // chunks that are counted so
+__device__ __forceinline__ void let_go(const PageTables& t, const TrimSpace& s, int* near, int id) {
+  if (!is_page(id, t) || atomicSub(&t.refs[id], 1) != 0) return;
+  const int c = id >> kChunkLog;
+  atomicAdd(c < kNear ? &near[c] : &s.chunk[c], 1);
 }
 
 __global__ __launch_bounds__(256) void k_trim(TrimArgs a) {
   const PageTables& t = a.t;
   if (t.status[0]) return;
+  __shared__ int near[kNear];
   const TrimSpace s = trim_space(t);
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int pieces = pieces_of(t);
+  const int pieces = pieces_of(t), chunks = chunks_of(t.num_pages) < kNear ? chunks_of(t.num_pages) : kNear;
+  for (int i = threadIdx.x; i < chunks; i += 256) near[i] = 0;
+  __syncthreads();
   const int rows = (t.R + 3) / 4;   // units of four requests, a wave each
   const int64_t units = rows + static_cast<int64_t>(s.copies[0]) * pieces;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
@@ -355,7 +363,7 @@ __global__ __launch_bounds__(256) void k_trim(TrimArgs a) {
       }
       auto go = [&](int j0, int j1) {
         for (int j = j0 + lane; j < j1; j += 64) {
-          let_go(t, s, row[j]);
+          let_go(t, s, near, row[j]);
           row[j] = -1;
         }
       };
@@ -369,9 +377,12 @@ __global__ __launch_bounds__(256) void k_trim(TrimArgs a) {
     if (is_page(x.z, t)) copy_piece(t, x.y, x.z, c);
     if (c == 0 && threadIdx.x == 0) {
       t.table[static_cast<int64_t>(x.x) * t.max_blocks + (t.seq[x.x] >> t.page_log)] = is_page(x.z, t) ? x.z : -1;
-      let_go(t, s, x.y);
+      let_go(t, s, near, x.y);
     }
   }
+  __syncthreads();
+  for (int i = threadIdx.x; i < chunks; i += 256)
+    if (near[i]) atomicAdd(&s.chunk[i], near[i]);
 }
 
 __global__ __launch_bounds__(kPlan) void k_give_back(TrimArgs a) {
@@ -418,11 +429,12 @@ __global__ __launch_bounds__(kPlan) void k_give_back(TrimArgs a) {
 // targets are disjoint, so pages are copied in any order.
 //
 // The plan marks the free pages as bits in LDS, kBits pages at a time (all of
-// them, for caches of up to 2^19 pages), and numbers the bits.
+// them, for caches of up to 2^18 pages), and sums the bits of each word: a page's
+// place among the free ones, and among those in use, follows from that.
 //
 // Workspace: the number of moves, source pages and targets [num_pages / 2 + 1 each],
 // for every page from k on its number among the sources or -1.
-constexpr int kBits = 1 << 19;
+constexpr int kBits = 1 << 18;
 
 struct CompactSpace {
   int* moves;
@@ -443,6 +455,7 @@ __device__ __forceinline__ CompactSpace compact_space(const PageTables& t) {
 __global__ __launch_bounds__(kPlan) void k_compact_plan(PageTables t) {
   if (blockIdx.x) return copy_tables(t, blockIdx.x - 1, gridDim.x - 1);
   __shared__ unsigned bits[kBits / 32];
+  __shared__ int sums[kBits / 32];   // free pages before a word, of the round
   __shared__ int wave[kPlan / 64], flag;
   const CompactSpace s = compact_space(t);
   const int tid = threadIdx.x, most = longest_of(t), half = t.num_pages / 2 + 1;
@@ -454,7 +467,7 @@ __global__ __launch_bounds__(kPlan) void k_compact_plan(PageTables t) {
     if (t.seq != t.seq_in) t.seq[r] = L;
   }
   flags = block_or<kPlan>(flags, &flag);
-  int sources = 0, targets = 0;
+  int targets = 0, before = 0;   // free pages before k, and before the round
   if (!(flags & 8)) {
     const int k = t.num_pages - count;
     for (int first = 0; first < t.num_pages; first += kBits) {
@@ -463,46 +476,43 @@ __global__ __launch_bounds__(kPlan) void k_compact_plan(PageTables t) {
       for (int i = tid; i < words; i += kPlan) bits[i] = 0;
       __syncthreads();
       int bad = 0;
-      for (int i = tid; i < count; i += kPlan) {
-        const int id = t.free_in[i];
-        if (!is_page(id, t)) bad = 16;
-        else if (id >= first && id - first < n) bad |= atomicOr(&bits[(id - first) >> 5], 1u << (id & 31)) >> (id & 31) & 1 ? 16 : 0;
+      for (int i0 = tid; i0 < count; i0 += 8 * kPlan) {   // eight loads under way
+        int id[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) id[e] = i0 + e * kPlan < count ? t.free_in[i0 + e * kPlan] : 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (i0 + e * kPlan >= count) continue;
+          if (!is_page(id[e], t)) bad = 16;
+          else if (id[e] >= first && id[e] - first < n)
+            bad |= atomicOr(&bits[(id[e] - first) >> 5], 1u << (id[e] & 31)) >> (id[e] & 31) & 1 ? 16 : 0;
+        }
       }
       flags |= block_or<kPlan>(bad, &flag);
-      // a run of words per thread: free pages before k are targets, pages in use from k on sources
       const int per = (words + kPlan - 1) / kPlan, w0 = tid * per, w1 = w0 + per < words ? w0 + per : words;
-      auto below = [&](int w) {   // bits of word w that are pages before k
-        const int d = k - (first + w * 32);
-        return d <= 0 ? 0u : d >= 32 ? ~0u : (1u << d) - 1;
-      };
-      auto valid = [&](int w) {   // bits that are pages
-        const int d = n - w * 32;
-        return d >= 32 ? ~0u : (1u << d) - 1;
-      };
-      int a = 0, b = 0;
+      int own = 0, all;
+      for (int w = w0; w < w1; ++w) own += __popc(bits[w]);
+      own = block_scan<kPlan>(own, wave, &all);
       for (int w = w0; w < w1; ++w) {
-        a += __popc(bits[w] & below(w));
-        b += __popc(~bits[w] & ~below(w) & valid(w));
+        sums[w] = own;
+        own += __popc(bits[w]);
       }
-      int all_a, all_b;
-      a = targets + block_scan<kPlan>(a, wave, &all_a);
-      b = sources + block_scan<kPlan>(b, wave, &all_b);
-      for (int w = w0; w < w1; ++w) {
-        const int p0 = first + w * 32;
-        for (unsigned m = bits[w] & below(w); m; m &= m - 1) {
-          if (a < half) s.dst[a] = p0 + __ffs(m) - 1;
-          ++a;
-        }
-        for (unsigned m = ~below(w) & valid(w); m; m &= m - 1) {
-          const int e = __ffs(m) - 1;
-          const bool used = !(bits[w] >> e & 1);
-          if (used && b < half) s.src[b] = p0 + e;
-          s.number[p0 + e - k] = used ? b : -1;
-          b += used;
+      __syncthreads();
+      auto free_before = [&](int p) { return before + sums[p >> 5] + __popc(bits[p >> 5] & ((1u << (p & 31)) - 1)); };   // p: of the round
+      if (k >= first + n) targets = before + all;
+      else if (k >= first) targets = free_before(k - first);
+      for (int p = tid; p < n; p += kPlan) {
+        const int page = first + p, f = free_before(p);
+        const bool free = bits[p >> 5] >> (p & 31) & 1;
+        if (page < k) {
+          if (free && f < half) s.dst[f] = page;
+        } else {
+          const int i = (page - f) - (k - targets);   // pages in use between k and this one
+          s.number[page - k] = free ? -1 : i;
+          if (!free && i >= 0 && i < half) s.src[i] = page;
         }
       }
-      targets += all_a;
-      sources += all_b;
+      before += all;
     }
   }
   if (tid == 0) {
