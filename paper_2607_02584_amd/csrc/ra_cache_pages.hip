@@ -14,8 +14,10 @@ namespace ra {
 namespace {
 
 constexpr int kPlan = 1024;           // threads of the workgroup that plans
-constexpr int kCopyBytes = 16384;     // of a page, that one workgroup copies at a time
-constexpr int kCopyGroups = 2048;     // workgroups that go round pieces of pages
+// Of a page, what one workgroup copies at a time: 16 bytes a thread.  (With four or two times as much 125
+// pages of 26 KB took 16 us to move, not 4, and 255 of 1.4 MB 78, not 70.)
+constexpr int kCopyBytes = 4096;
+constexpr int kCopyGroups = 8192;     // workgroups that go round pieces of pages
 constexpr int kChunkLog = 12;         // pages that one workgroup gives back to the stack
 constexpr int kMaxRequests = 65536;
 
@@ -100,23 +102,12 @@ int copy_groups(const PageTables& t) {
 
 // Piece `c` of a page's bytes.
 __device__ __forceinline__ void copy_piece(const PageTables& t, int src, int dst, int c) {
-  const int64_t from = static_cast<int64_t>(c) * kCopyBytes;
-  const uint4* a = reinterpret_cast<const uint4*>(t.cache + static_cast<int64_t>(src) * t.page_bytes + from);
-  uint4* b = reinterpret_cast<uint4*>(t.cache + static_cast<int64_t>(dst) * t.page_bytes + from);
-  const int64_t left = (t.page_bytes - from) / 16;   // pages are whole pieces of 128 bytes
-  const int n = static_cast<int>(left < kCopyBytes / 16 ? left : kCopyBytes / 16);
-  uint4 v[kCopyBytes / 16 / 256];
-#pragma unroll
-  for (int i = 0; i < kCopyBytes / 16 / 256; ++i) {
-    const int at = i * 256 + threadIdx.x;
-    if (at < n) v[i] = a[at];
-  }
-#pragma unroll
-  for (int i = 0; i < kCopyBytes / 16 / 256; ++i) {
-    const int at = i * 256 + threadIdx.x;
-    if (at < n) b[at] = v[i];
-  }
+  const int64_t at = static_cast<int64_t>(c) * kCopyBytes + threadIdx.x * 16;
+  if (at < t.page_bytes)   // whole pieces of 128 bytes
+    *reinterpret_cast<uint4*>(t.cache + static_cast<int64_t>(dst) * t.page_bytes + at) =
+        *reinterpret_cast<const uint4*>(t.cache + static_cast<int64_t>(src) * t.page_bytes + at);
 }
+static_assert(kCopyBytes == 256 * 16, "a workgroup's 16 bytes a thread");
 __host__ __device__ __forceinline__ int pieces_of(const PageTables& t) {
   return static_cast<int>((t.page_bytes + kCopyBytes - 1) / kCopyBytes);
 }
@@ -198,14 +189,18 @@ __global__ __launch_bounds__(kPlan) void k_fork_plan(ForkArgs a) {
 
 __global__ __launch_bounds__(256) void k_fork(ForkArgs a) {
   const PageTables& t = a.t;
-  if (t.status[0]) return;
   const int* len = t.ws;
   const int2* copy = reinterpret_cast<const int2*>(t.ws + ((a.n + 1) & ~1));
   const int pieces = pieces_of(t), per = pieces + 1;
   const int64_t units = static_cast<int64_t>(a.n) * per;
+  // (loads that do not depend on each other are asked for together: each takes a microsecond here.
+  // There are n entries whatever the status, and a workgroup has a unit.)
+  int2 x = copy[blockIdx.x / per];
+  const int refused = t.status[0];
+  if (refused) return;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int i = static_cast<int>(u / per), c = static_cast<int>(u - static_cast<int64_t>(i) * per);
-    const int2 x = copy[i];
+    if (u != blockIdx.x) x = copy[i];
     if (c < pieces) {
       if (is_page(x.x, t) && is_page(x.y, t)) copy_piece(t, x.x, x.y, c);
       continue;
@@ -340,15 +335,16 @@ __device__ __forceinline__ void let_go(const PageTables& t, const TrimSpace& s, 
 
 __global__ __launch_bounds__(256) void k_trim(TrimArgs a) {
   const PageTables& t = a.t;
-  if (t.status[0]) return;
   __shared__ int near[kNear];
   const TrimSpace s = trim_space(t);
+  const int refused = t.status[0], copies = s.copies[0];
+  if (refused) return;
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int pieces = pieces_of(t), chunks = chunks_of(t.num_pages) < kNear ? chunks_of(t.num_pages) : kNear;
   for (int i = threadIdx.x; i < chunks; i += 256) near[i] = 0;
   __syncthreads();
   const int rows = (t.R + 3) / 4;   // units of four requests, a wave each
-  const int64_t units = rows + static_cast<int64_t>(s.copies[0]) * pieces;
+  const int64_t units = rows + static_cast<int64_t>(copies) * pieces;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     if (u < rows) {
       const int r = static_cast<int>(u) * 4 + w;

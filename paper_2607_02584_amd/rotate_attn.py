@@ -388,6 +388,12 @@ def _cache_dtypes():
 def _cache_tensor(t, name, dtype, shape, device=None, strided=False):
     """A device tensor of this type and shape, contiguous; `strided`: channels
     adjacent, the other strides multiples of 8 elements."""
+    if device is not None:   # all is well, as a rule
+        try:
+            if t.dtype is dtype and t.shape == shape and t.get_device() == device.index and t.is_contiguous():
+                return t.data_ptr()
+        except AttributeError:
+            pass
     import torch
     if not isinstance(t, torch.Tensor):
         raise ValueError(f"{name} must be a tensor")
@@ -573,17 +579,23 @@ def _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, ca
                  refs_out, free_out, count_out):
     """R, the device, and (tables, out, cache, workspace, its bytes, status) as the library takes them."""
     dt = _cache_dtypes()
-    i32, R = dt["i32"], seq_lens.numel()
-    pages, dev = _cache_pages(p, cache, dt["u8"]), cache.device
-    one = (("seq_lens", seq_lens, seq_out, (R,)), ("block_table", block_table, table_out, (R, p.max_blocks)),
-           ("page_refs", page_refs, refs_out, (p.num_pages,)), ("free_pages", free_pages, free_out, (p.num_pages,)),
-           ("free_count", free_count, count_out, (1,)))
-    before = [_cache_tensor(t, name, i32, shape, dev) for name, t, _, shape in one]
-    after = [at if o is None else _cache_tensor(o, name + "'s new state", i32, shape, dev)
-             for at, (name, _, o, shape) in zip(before, one)]
+    i32, u8, R = dt["i32"], dt["u8"], seq_lens.numel()
+    pages, dev = _cache_pages(p, cache, u8), cache.device
+    per_request, per_page, rows = (R,), (p.num_pages,), (R, p.max_blocks)
+    check = _cache_tensor
+    seq = check(seq_lens, "seq_lens", i32, per_request, dev)
+    table = check(block_table, "block_table", i32, rows, dev)
+    refs = check(page_refs, "page_refs", i32, per_page, dev)
+    free = check(free_pages, "free_pages", i32, per_page, dev)
+    count = check(free_count, "free_count", i32, (1,), dev)
+    out = CacheTables(seq if seq_out is None else check(seq_out, "seq_out", i32, per_request, dev),
+                      table if table_out is None else check(table_out, "table_out", i32, rows, dev),
+                      refs if refs_out is None else check(refs_out, "refs_out", i32, per_page, dev),
+                      free if free_out is None else check(free_out, "free_out", i32, per_page, dev),
+                      count if count_out is None else check(count_out, "count_out", i32, (1,), dev))
     nws = _nbytes(ws)
-    return R, dev, (CacheTables(*before), CacheTables(*after), pages, _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev),
-                    nws, _cache_tensor(status, "status", i32, (4,), dev))
+    return R, dev, (CacheTables(seq, table, refs, free, count), out, pages, check(ws, "workspace", u8, (nws,), dev), nws,
+                    check(status, "status", i32, (4,), dev))
 
 
 def cache_fork(p, parents, children, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status,
