@@ -454,7 +454,7 @@ int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_
  * seq_lens).  Causal attention without a window.  R, T and groups (at most R) fix the
  * grid; lengths, groups and prefixes are device data.  Values there that do not
  * fit touch nothing outside the tensors and the workspace.
- * Limits: (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096, T must not exceed
+ * Limits: 2 * (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096, T must not exceed
  * 2^22, nor T * Hq 2^26.  Precision as cache_attn's, rows of a prefix being those of all its queries: with bf16
  * outputs weights times V's scales are one bf16 value (2^-8) where a prefix, or a
  * request's own keys, have more than 16 rows (queries times Hq / Hkv).

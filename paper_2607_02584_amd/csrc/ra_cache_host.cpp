@@ -204,8 +204,8 @@ int check_shared(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T)
   if (groups < 0 || groups > R) return set_error(RA_ERR_INVALID, "groups must be in [0, R]");
   if (!p->causal) return set_error(RA_ERR_UNSUPPORTED, "shared prefixes need causal attention");
   if (p->window) return set_error(RA_ERR_UNSUPPORTED, "shared prefixes cannot be under a window");
-  const int64_t pieces = (static_cast<int64_t>(R) + groups) * p->Hkv + static_cast<int64_t>(T) * p->Hq / 64;
-  if (pieces >= (1 << 24) - 4096) return set_error(RA_ERR_UNSUPPORTED, "(R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096");
+  const int64_t pieces = 2 * (static_cast<int64_t>(R) + groups) * p->Hkv + static_cast<int64_t>(T) * p->Hq / 64;
+  if (pieces >= (1 << 24) - 4096) return set_error(RA_ERR_UNSUPPORTED, "2 * (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096");
   if (T > (1 << 22) || static_cast<int64_t>(T) * p->Hq > (1 << 26))
     return set_error(RA_ERR_UNSUPPORTED, "T must not exceed 2^22, and T * Hq not 2^26, with shared prefixes");
   return RA_OK;

@@ -101,18 +101,6 @@ constexpr float kFewCost = 0.3f;      // of a block of keys for few rows, in blo
 constexpr int kPlaces = 512;
 __host__ __device__ constexpr int places_of(int Hkv) { return kPlaces > Hkv ? kPlaces / Hkv : 1; }
 
-// The largest over a wave of values that are not negative (register moves, as wave_sums).
-__device__ __forceinline__ int wave_most(int v) {
-  auto take = [&](int o) { v = o > v ? o : v; };
-  take(__builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));   // row_shr:1
-  take(__builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
-  take(__builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
-  take(__builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
-  take(__builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));   // row_bcast:15
-  take(__builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false));   // row_bcast:31
-  return __builtin_amdgcn_readlane(v, 63);
-}
-
 struct PlanShared {
   int blocks[kKnown];
   int tiles[kKnown];             // of few rows as they are, of many negative
