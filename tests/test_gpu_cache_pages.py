@@ -403,3 +403,53 @@ def test_another_stream(ra):
     c.call("cache_fork", _i32([3, 1]), _i32([0, 2]), stream=side.cuda_stream)
     want, status = ref.fork(c.state, 64, 4, [3, 1], [0, 2])
     c.check(c.t, want, status)
+
+
+def test_nothing_to_do(ra):
+    """No requests, no pairs, no pages free."""
+    rng = random.Random(1)
+    c = Cache(ra, rng, 3, 16, 2, 6, lens=[32, 32, 32])
+    assert c.state["count"] == 0
+    for apart in (False, True):
+        for name, args in (("cache_fork", (_i32([]), _i32([]))), ("cache_trim", ()), ("cache_compact", ())):
+            out = c.call(name, *args, apart=apart)
+            c.check(out, c.state, [0, 0, {"cache_compact": 6}.get(name, 0), 0 if name == "cache_compact" else 32])
+    p = ra.make_cache_params(1, 1, 64, page_size=16, num_pages=4, max_blocks=2)
+    t = [torch.zeros(n, dtype=torch.int32, device="cuda") for n in ((0,), (0, 2), (4,), (4,), (1,))]
+    t[3].copy_(_i32([3, 1, 0, 2]))
+    t[4].fill_(4)
+    cache, ws, status = torch.zeros(4, 16 * 72, dtype=torch.uint8, device="cuda"), ra.cache_pages_workspace(p, 0), _i32([9] * 4)
+    ra.cache_fork(p, _i32([]), _i32([]), *t, cache, ws, status)
+    assert status.tolist() == [0, 0, 0, 0]
+    ra.cache_trim(p, *t, cache, ws, status)
+    assert status.tolist() == [0, 0, 0, 0] and t[3].tolist() == [3, 1, 0, 2] and t[4].item() == 4
+    ra.cache_compact(p, *t, cache, ws, status)
+    assert status.tolist() == [0, 0, 0, 0] and t[3].tolist() == [3, 2, 1, 0]
+
+
+def test_pages_past_32_bits(ra):
+    """A cache of more than 4 GiB: its last pages are copied from and to where they are."""
+    Hkv, D, page = 8, 128, 256
+    pages = (5 << 30) // (Hkv * page * (D + 8))
+    p = ra.make_cache_params(Hkv, Hkv, D, page_size=page, num_pages=pages, max_blocks=2)
+    size = ra.cache_layout(p)["page_bytes"]
+    cache = torch.zeros(pages, size, dtype=torch.uint8, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    last = torch.randint(0, 256, (2, size), generator=g, dtype=torch.uint8, device="cuda")
+    cache[pages - 2:] = last
+    stack = [pages - 3] + [0] * (pages - 1)
+    t = dict(seq=_i32([300, 0]), table=_i32([[pages - 1, pages - 2], [-1, -1]]), refs=_i32(np.zeros(pages)),
+             free=_i32(stack), count=_i32([1]))
+    ws, status = ra.cache_pages_workspace(p, 2), _i32([0] * 4)
+    ra.cache_fork(p, _i32([0]), _i32([1]), *t.values(), cache, ws, status)
+    assert status.tolist() == [0, 1, 1, 300] and torch.equal(cache[pages - 3], last[0])
+    ra.cache_trim(p, *t.values(), cache, ws, status, keep=_i32([0, -1]))
+    assert status.tolist() == [0, 0, 1, 300]
+    # the stack names every page but two that lie at the end: they move to the front
+    free = np.arange(pages)
+    free = free[(free != pages - 1) & (free != pages - 3)]
+    t["free"].copy_(_i32(np.concatenate([free, [0, 0]])))
+    t["count"].fill_(pages - 2)
+    ra.cache_compact(p, *t.values(), cache, ws, status)
+    assert status.tolist() == [0, 2, 2, 0] and t["table"].tolist() == [[-1, -1], [1, 0]]
+    assert torch.equal(cache[0], last[0]) and torch.equal(cache[1], last[1])

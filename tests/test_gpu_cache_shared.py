@@ -265,3 +265,94 @@ def test_fork_then_attend_captured(ra):
                 ra.cache_fork(p, i32([0, 0, 0, 0]), i32([1, 2, 3, 4]), st["seq_lens"], st["block_table"], st["page_refs"],
                               st["free_pages"], st["free_count"], st["cache"], s[6], s[1]["status"])
                 assert s[1]["status"].tolist()[:3] == [0, 4, 24]
+
+
+def _regroup(c, starts, prefix, got=None):
+    """The case's call with these groups."""
+    ra, R = c.ra, len(c.lens)
+    c.fresh()
+    ws = ra.cache_shared_workspace(c.p, R, len(prefix), c.T)
+    ra.cache_attn_shared(c.p, c.q, torch.from_numpy(c.cache).cuda(), i32(c.table), i32(c.start), i32(c.lens), c.positions,
+                         i32(starts), i32(prefix), c.o, ws, lse=c.lse, rope=c.rope())
+    torch.cuda.synchronize()
+
+
+def test_no_groups_and_empty_ones(ra):
+    c = _case(ra, [(5, 70), (4, 33)], own=60, queries=(1, 3, 20), rope=True, seed=21, pad=2)
+    for starts, prefix in (([0], []), ([0, 0, 5, 5, 9], [7, 70, 50, 33]), ([0, 5, 9, 9, 9], [70, 33, 1, 2]), ([2, 5], [70]),
+                           ([0, 0, 0], [5, 5]), ([9, 9], [3])):
+        _regroup(c, starts, prefix)
+        c.check(True)
+
+
+def test_rows_before_the_first_request(ra):
+    """q_start need not begin at 0: rows before it are left as they were."""
+    c = _case(ra, [(6, 100), (3, 40)], own=50, queries=(1, 2), rope=True, seed=22)
+    want = c.want()
+    shift, T = 7, c.T
+    c.start = c.start + shift
+    c.q = torch.cat((torch.full_like(c.q[:shift], float("nan")), c.q))
+    c.positions = torch.cat((c.positions.new_full((shift,), -1), c.positions))
+    c.T = T + shift
+    c.run()
+    assert (c.o[:shift] == 5.0).all() and (c.lse[:shift] == 5.0).all()
+    c.check(True, got=(c.o[shift:], c.lse[shift:]), want=want)
+
+
+@pytest.mark.parametrize("R,groups", [(700, 600), (5000, 300), (3000, 2900)])
+def test_thousands_of_requests_and_groups(ra, R, groups):
+    """More prefixes and requests than their lengths, or their tiles, are kept of in one place."""
+    rng = np.random.default_rng(R)
+    page, n = 16, 24                                   # all hold the same two pages' worth of tokens, 20 shared
+    qs = [int(x) for x in rng.choice([0, 1, 1, 2], R)]
+    lens = [n] * R
+    cuts = np.sort(rng.choice(np.arange(1, R), groups - 1, replace=False)).tolist()
+    c = Case(ra, 2, 1, 64, page, [n] * 8, [q for q in [1] * 8], seed=R)
+    c.lens, c.qs = lens, qs
+    c.table = np.repeat(c.table[:1], R, 0)
+    c.start = np.concatenate([[0], np.cumsum(qs)]).astype(np.int32)
+    c.T = int(c.start[-1])
+    c.q = torch.tensor(rng.standard_normal((c.T, 2, 64))).to(torch.bfloat16).cuda()
+    c.positions = i32([n - m + i for m in qs for i in range(m)])
+    _regroup(c, [0] + cuts + [R], rng.integers(0, 21, groups).tolist())
+    # every request has the same keys
+    r = [i for i in range(R) if qs[i] == 1][:40] + [i for i in range(R) if qs[i] == 2][-40:]
+    o, lse = c.o, c.lse
+    pick = np.concatenate([np.arange(c.start[i], c.start[i + 1]) for i in r])
+    d = Case(ra, 2, 1, 64, page, [n] * 8, [1] * 8, seed=R)
+    d.lens, d.qs = [n] * len(r), [qs[i] for i in r]
+    d.table = c.table[:len(r)]
+    d.start = np.concatenate([[0], np.cumsum(d.qs)]).astype(np.int32)
+    d.T, d.q = len(pick), c.q[torch.from_numpy(pick).cuda()]
+    where = torch.from_numpy(pick).cuda()
+    d.check(True, got=(o[where], lse[where]))
+    assert torch.isfinite(o).all() and torch.isfinite(lse).all()
+
+
+def test_more_heads_than_places(ra):
+    c = _case(ra, [(3, 100), (20, 70)], own=30, queries=(1, 2), Hq=600, Hkv=600, D=64, seed=23)
+    c.run()
+    c.check(True)
+
+
+def test_two_calls_on_two_streams(ra):
+    """Calls with workspaces of their own do not meet."""
+    a = _case(ra, [(12, 900), (3, 700)], own=300, queries=(1, 2, 30), rope=True, seed=7)
+    b = _case(ra, [(30, 500)], own=100, queries=(1,), rope=True, seed=8)
+    want = [[t.clone() for t in c.run()] for c in (a, b)]
+    args = []
+    for c in (a, b):
+        starts = [g[0] for g in c.groups] + [c.groups[-1][1]]
+        ws = ra.cache_shared_workspace(c.p, len(c.lens), len(c.groups), c.T)
+        args.append((c.p, c.q, torch.from_numpy(c.cache).cuda(), i32(c.table), i32(c.start), i32(c.lens), c.positions, i32(starts),
+                     i32([g[2] for g in c.groups]), c.o, ws, c.lse, c.rope()))
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, x, s in zip((a, b), args, streams):
+            with torch.cuda.stream(s):
+                c.o.zero_()
+                ra.cache_attn_shared(*x[:-2], lse=x[-2], rope=x[-1])
+    torch.cuda.synchronize()
+    for c, w in zip((a, b), want):
+        assert torch.equal(c.o, w[0]) and torch.equal(c.lse, w[1])
