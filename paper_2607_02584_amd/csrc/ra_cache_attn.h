@@ -592,7 +592,7 @@ template <int D, int NT>
 struct Rows {
   v4f o[NT][D / 16];
   float m[NT], l[NT];
-  float back[NT];       // FINE: what scores are multiplied by
+  float back[NT];       // fine Q: what scores are multiplied by
   int hi[NT], lo[NT];   // keys that the lane's row sees: [lo, hi)
 };
 
@@ -603,10 +603,17 @@ struct Rows {
 // first use of its result: the compiler then leaves out the wait states that
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
+// Q is two binary16 values for binary32 outputs, and for all of cache_attn_sinks and cache_attn_shared: their lse is as
+// exact as binary32 arithmetic whatever the outputs' type.  (Two bf16 values left 2e-6 of an lse over few keys.  For many
+// rows it costs 5 %, sinks_prompt 520 -> 545 us, of which the multiplication by the rows' powers of two is a tenth.)
+template <bool FINE, Keys K>
+constexpr bool fine_q() { return FINE || K != kAll; }
+
 template <int D, int NT, int N, int KT, bool FINE, Keys K>
 __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const Tile16<D> (&t)[KT], unsigned there, bool whole, int key0,
                                           int g, int sinks) {
   constexpr int KC = D / 32;
+  constexpr bool QF = fine_q<FINE, K>();
   v4f s[N][KT];
 #pragma unroll
   for (int i = 0; i < KT; ++i) {
@@ -614,11 +621,11 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const 
     for (int nt = 0; nt < N; ++nt) s[nt][i] = v4f{0, 0, 0, 0};
 #pragma unroll
     for (int c = 0; c < KC; ++c) {
-      const uint4 k = codes8<FINE>(dword_of<D>(t[i].k, c));
+      const uint4 k = codes8<QF>(dword_of<D>(t[i].k, c));
 #pragma unroll
       for (int nt = 0; nt < N; ++nt) {
-        s[nt][i] = score16<FINE>(k, sq[(nt * KC + c) * 128], s[nt][i]);
-        s[nt][i] = score16<FINE>(k, sq[(nt * KC + c) * 128 + 64], s[nt][i]);
+        s[nt][i] = score16<QF>(k, sq[(nt * KC + c) * 128], s[nt][i]);
+        s[nt][i] = score16<QF>(k, sq[(nt * KC + c) * 128 + 64], s[nt][i]);
       }
     }
     const float ks[4] = {t[i].ks.x, t[i].ks.y, t[i].ks.z, t[i].ks.w};
@@ -626,7 +633,7 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const 
     for (int nt = 0; nt < N; ++nt) {
       const float base = x.m[nt] == kNegInf ? 0.0f : x.m[nt];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[nt][i][e] = __fmaf_rn(s[nt][i][e], FINE ? ks[e] * x.back[nt] : ks[e], -base);
+      for (int e = 0; e < 4; ++e) s[nt][i][e] = __fmaf_rn(s[nt][i][e], QF ? ks[e] * x.back[nt] : ks[e], -base);
     }
   }
   constexpr int PN = FINE ? 3 : 2;
@@ -728,19 +735,20 @@ __device__ __forceinline__ void few_step(Rows<D, NT>& x, const uint4* sq, const 
   }
 }
 
-template <int D, int NT, bool FINE>
+template <int D, int NT, bool QF>
 struct FewLds {
   static constexpr int M = 16 * NT, kStride = D + 4;   // floats, against bank conflicts
   __align__(16) float so[4][16][kStride];
   float sm[4][M], sl[4][M];
   SchedShared sched;
   __align__(16) uint4 sq_all[NT * (D / 32) * 128];   // [nt][channel step][hi, lo][lane]
-  float sback[FINE ? M : 1];
+  float sback[QF ? M : 1];
 };
 
 // Piece x0 of KV head h.
 template <int D, int NT, int KT, bool FINE, Keys K>
-__device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, FINE>& lds, int x0, int h) {
+__device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, fine_q<FINE, K>()>& lds, int x0, int h) {
+  constexpr bool QF = fine_q<FINE, K>();
   constexpr int M = 16 * NT, E = D / 16, kStep = 16 * KT, S = kBlock / kStep;
   auto& so = lds.so;
   auto& sm = lds.sm;
@@ -816,11 +824,11 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, F
 #pragma unroll
         for (int z = 0; z < 2; ++z) sq_all[(w * 2 + z) * 64 + lane] = turned<D>(a, p, h, row, z, g * (D / 4) + w * 8);
       }
-      if (FINE && w == 0 && lane < 16) sback[lane] = turned_back(a, p, h, row);
+      if (w == 0 && lane < 16) sback[lane] = turned_back(a, p, h, row);
     } else if (w == nt) {   // one wave for all four
       uint4 qh[D / 32], ql[D / 32];
-      const float back = load_q<D, FINE>(a, p, h, row, lane, qh, ql);
-      if (FINE && lane < 16) sback[nt * 16 + lane] = back;
+      const float back = load_q<D, QF>(a, p, h, row, lane, qh, ql);
+      if (QF && lane < 16) sback[nt * 16 + lane] = back;
 #pragma unroll
       for (int c = 0; c < D / 32; ++c) {
         sq_all[(nt * (D / 32) + c) * 128 + lane] = qh[c];
@@ -838,7 +846,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, F
   }
   __syncthreads();
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) x.back[nt] = FINE ? sback[nt * 16 + (lane & 15)] : 1.0f;
+  for (int nt = 0; nt < NT; ++nt) x.back[nt] = QF ? sback[nt * 16 + (lane & 15)] : 1.0f;
   if constexpr (K == kShared) {
     static_assert(NT == 1, "one product's rows");
     if (prefix) {
@@ -1058,7 +1066,7 @@ struct RowsLds {
 // Piece x0 of KV head h.
 template <int D, bool F16, int TERMS, Keys K>
 __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& buf, int x0, int h) {
-  constexpr bool FINE = TERMS == 3;
+  constexpr bool QF = fine_q<TERMS == 3, K>();
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
   typedef typename RowsLds<D>::Scales Scales;
@@ -1161,7 +1169,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
     if constexpr (c < D / 32) {
       const uint32_t x = dword_of<D>(sk, c);
       buf.k[b & 1][(lane >> 4) * (D / 32) + c][mine + (lane & 15)] =
-          codes8<FINE>(x);
+          codes8<QF>(x);
     }
   };
   auto put_v = [&](int b, auto part) {   // channels E / 4 * part .. of the lane's chunk
@@ -1222,9 +1230,9 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
       q[c] = turned<D>(a, p, h, row, 0, hh * (D / 2) + c * 8);
       q_lo[c] = turned<D>(a, p, h, row, 1, hh * (D / 2) + c * 8);
     }
-    if constexpr (FINE) back = turned_back(a, p, h, row);
+    back = turned_back(a, p, h, row);
   } else {
-    back = load_q32<D, F16, FINE>(a, p, h, row, lane, q, q_lo);
+    back = load_q32<D, F16, QF>(a, p, h, row, lane, q, q_lo);
   }
   v16f o[MT], s[2];
 #pragma unroll
@@ -1249,8 +1257,8 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
 #pragma unroll
     for (int kc = 0; kc < KC; ++kc) {
       const uint4 k = k_op(b0, c, kc);
-      s[c] = score32<FINE>(k, q[kc], s[c]);
-      s[c] = score32<FINE>(k, q_lo[kc], s[c]);
+      s[c] = score32<QF>(k, q[kc], s[c]);
+      s[c] = score32<QF>(k, q_lo[kc], s[c]);
     }
     settle(s[c]);
   }
@@ -1269,7 +1277,7 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
 #pragma unroll
       for (int r = 0; r < 16; r += 4) {
         float4 k4 = *reinterpret_cast<const float4*>(&t.ks[c * 32 + 2 * r + 4 * hh]);
-        if constexpr (FINE) k4.x *= back, k4.y *= back, k4.z *= back, k4.w *= back;
+        if constexpr (QF) k4.x *= back, k4.y *= back, k4.z *= back, k4.w *= back;
         x[c][r] = __fmaf_rn(s[c][r], k4.x, -base);
         x[c][r + 1] = __fmaf_rn(s[c][r + 1], k4.y, -base);
         x[c][r + 2] = __fmaf_rn(s[c][r + 2], k4.z, -base);
@@ -1381,8 +1389,8 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
           if constexpr (i == 1)
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
-          s[c] = score32<FINE>(op, q[i / 2], s[c]);
-          s[c] = score32<FINE>(op, q_lo[i / 2], s[c]);
+          s[c] = score32<QF>(op, q[i / 2], s[c]);
+          s[c] = score32<QF>(op, q_lo[i / 2], s[c]);
         }
         constexpr int n = c * NP + i + kAhead;
         if constexpr (n < 2 * NP) op = operand(n / NP, n % NP);
@@ -1621,13 +1629,13 @@ int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }
 
 template <int D, int NT, int KT, Keys K>
 __global__ __launch_bounds__(256, 2) void k_few(CacheAttnArgs a) {
-  __shared__ FewLds<D, NT, false> lds;
+  __shared__ FewLds<D, NT, fine_q<false, K>()> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   few_rows<D, NT, KT, false, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, int NT, int KT, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
-  __shared__ FewLds<D, NT, true> lds;
+  __shared__ FewLds<D, NT, fine_q<true, K>()> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   few_rows<D, NT, KT, true, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }

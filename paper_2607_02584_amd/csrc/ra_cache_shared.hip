@@ -345,9 +345,9 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   }
 }
 
-// Q of a row after RoPE, rotation and scale as two 16-bit values (see load_q): D / 8 lanes hold it.
+// Q of a row after RoPE, rotation and scale as two binary16 values and a power of two (see load_q): D / 8 lanes hold it.
 template <int D>
-__device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row, bool fine) {
+__device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row) {
   const int b = row_block(threadIdx.x & (D / 8 - 1));
   const bool ok = row < static_cast<int64_t>(a.T) * a.Hq;   // lanes without a row keep running: the moves between lanes need whole rows
   const int t = ok ? static_cast<int>(row / a.Hq) : 0, head = ok ? static_cast<int>(row - static_cast<int64_t>(t) * a.Hq) : 0;
@@ -379,21 +379,19 @@ __device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row, bool
   }
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= scale;
-  if (fine) {
-    float m = 0.0f;
+  float m = 0.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
-    m = fmaxf(m, lane_xor<1>(m));
-    m = fmaxf(m, lane_xor<2>(m));
-    m = fmaxf(m, lane_xor<7>(m));
-    if constexpr (D == 128) m = fmaxf(m, lane_xor<8>(m));
-    const float power = row_power(m);
+  for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(y[e]));
+  m = fmaxf(m, lane_xor<1>(m));
+  m = fmaxf(m, lane_xor<2>(m));
+  m = fmaxf(m, lane_xor<7>(m));
+  if constexpr (D == 128) m = fmaxf(m, lane_xor<8>(m));
+  const float power = row_power(m);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] *= power;
-    if (ok && b == 0) a.back[row] = inverse_power(power);
-  }
+  for (int e = 0; e < 8; ++e) y[e] *= power;
+  if (ok && b == 0) a.back[row] = inverse_power(power);
   uint4 hi, lo;
-  split8(y, fine, hi, lo);
+  split8(y, true, hi, lo);
   if (ok) {
     uint16_t* dst = a.turned + row * 2 * D + b * 8;
     *reinterpret_cast<uint4*>(dst) = hi;
@@ -427,7 +425,7 @@ __global__ __launch_bounds__(kPlan) void k_shared_plan(CacheAttnArgs a) {
   if (blockIdx.x == 0) return plan_pieces(a);
   constexpr int kRows = kPlan * 8 / D;
   find_owners(a, static_cast<int64_t>(blockIdx.x - 1) * kRows, static_cast<int64_t>(blockIdx.x) * kRows);
-  turn_q<D>(a, static_cast<int64_t>(blockIdx.x - 1) * (kPlan * 8 / D) + threadIdx.x / (D / 8), a.out_dtype == RA_FP32);
+  turn_q<D>(a, static_cast<int64_t>(blockIdx.x - 1) * (kPlan * 8 / D) + threadIdx.x / (D / 8));
 }
 
 // ---------------------------------------------------------------- kernels --
@@ -438,7 +436,7 @@ template <int D, bool F16, int TERMS>
 __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a) {
   constexpr bool FINE = TERMS == 3;
   __shared__ union {
-    FewLds<D, 1, FINE> few;
+    FewLds<D, 1, true> few;
     RowsLds<D> rows;
   } lds;
   const int x = blockIdx.x / a.g.Hkv, h = blockIdx.x - x * a.g.Hkv, many = __builtin_amdgcn_readfirstlane(a.counts[1]);

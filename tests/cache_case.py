@@ -130,17 +130,7 @@ class Case:
             if m == 0:
                 continue
             sl = slice(self.start[r], self.start[r + 1])
-            pos, key = n - m + np.arange(m)[:, None], np.arange(n)[None, :]
-            seen = key <= pos
-            if p.window:
-                seen = seen & ((key > pos - p.window) | (key < (self.sinks or 0)))
-            ids = self.table[r, np.arange(n) // p.page_size] if n else np.zeros(0, np.int32)
-            there = (ids >= 0) & (ids < p.num_pages)
-            seen = seen & there[None, :]
-            slots = np.where(there, ids, 0) * p.page_size + np.arange(n) % p.page_size
-            kc, ks, vc, vs = ref.rows(self.cache, slots, p.page_size, p.Hkv, D)
-            any_sees = seen.any(0)[:, None, None]
-            k, v = (np.where(any_sees, ref.value(c) * s[..., None].astype(np.float64), 0.0) for c, s in ((kc, ks), (vc, vs)))
+            pos, seen, k, v = self._seen(r)
             x = f64(self.q[sl])
             if self.cs is not None:
                 x = ref.turn(x, self.cs[np.maximum(pos[:, 0], 0)])
@@ -160,6 +150,55 @@ class Case:
                 size_v[sl, h] = np.abs(av).sum(1, keepdims=True) / np.sqrt(D) if p.v_rotation else av
                 size_s[sl, h] = np.where(seen, D ** -0.5 * (np.abs(x[:, h]) @ np.abs(kh).T), 0.0).max(1, initial=0.0)
         return o, lse, size_v, size_s
+
+    def _seen(self, r):
+        """Positions and mask of request r, and its keys and values in 64 bits (0 where nobody sees them)."""
+        p, n, m = self.p, self.lens[r], self.qs[r]
+        pos, key = n - m + np.arange(m)[:, None], np.arange(n)[None, :]
+        seen = key <= pos
+        if p.window:
+            seen = seen & ((key > pos - p.window) | (key < (self.sinks or 0)))
+        ids = self.table[r, np.arange(n) // p.page_size] if n else np.zeros(0, np.int32)
+        there = (ids >= 0) & (ids < p.num_pages)
+        seen = seen & there[None, :]
+        slots = np.where(there, ids, 0) * p.page_size + np.arange(n) % p.page_size
+        kc, ks, vc, vs = ref.rows(self.cache, slots, p.page_size, p.Hkv, p.D)
+        any_sees = seen.any(0)[:, None, None]
+        return pos, seen, *(np.where(any_sees, ref.value(c) * s[..., None].astype(np.float64), 0.0) for c, s in ((kc, ks), (vc, vs)))
+
+    def lse32(self):
+        """lse in elementary binary32 operations (torch, on the host)."""
+        p = self.p
+        G, f = p.Hq // p.Hkv, torch.float32
+        H = torch.tensor(ref.hadamard(p.D) / np.sqrt(p.D)).to(f)
+        lse = np.full((self.T, p.Hq), 5.0)
+        for r in range(len(self.lens)):
+            if self.qs[r] == 0:
+                continue
+            pos, seen, k, _ = self._seen(r)
+            sl = slice(self.start[r], self.start[r + 1])
+            k, seen = torch.tensor(k).to(f), torch.tensor(seen)
+            x = self.q[sl].cpu().to(f)
+            if self.cs is not None:
+                cs = torch.tensor(self.cs[np.maximum(pos[:, 0], 0)])[:, None]
+                a, b = x[..., 0::2], x[..., 1::2]
+                x = torch.stack((a * cs[..., 0] - b * cs[..., 1], a * cs[..., 1] + b * cs[..., 0]), -1).flatten(-2)
+            for h in range(p.Hq):
+                y = x[:, h] @ H if p.rotation else x[:, h]
+                s = (y @ k[:, h // G].T.contiguous()) * np.float32(p.D ** -0.5)
+                s = torch.where(seen, s, -torch.inf)
+                top = s.max(1, keepdim=True).values
+                lse[sl, h] = (top + torch.log(torch.exp(s - top).sum(1, keepdim=True)))[:, 0].double().numpy()
+        return lse
+
+    def check_lse(self):
+        """Error of lse against 64 bits at most twice that of binary32 operations throughout (as many roundings, in other
+        places), and four roundings of a score as large as these."""
+        _, want, _, size_s = self.want()
+        n = self.start[-1]
+        want, size_s, got, plain = want[:n], size_s[:n], f64(self.lse)[:n], self.lse32()[:n]
+        unit = 2.0 ** -24 * (1 + np.abs(want).max() + size_s.max())
+        assert np.abs(got - want).max() <= 2 * np.abs(plain - want).max() + 4 * unit
 
     def check(self, one, n=None, got=None, want=None):
         """Bounds by arithmetic.  one: weights times V's scales may be one bf16 value (half a step, 2^-8).  Scores: Q as

@@ -2,7 +2,7 @@
 import numpy as np
 import pytest
 
-from cache_case import Case, HALF, i32
+from cache_case import Case, i32
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -123,6 +123,16 @@ def test_large_scores_and_one_side_that_vanishes(ra):
     c = _case(ra, [(20, 300), (3, 200)], own=60, queries=(1, 9), dt="fp16", out="fp32", gain=60.0, seed=5)
     c.run()
     c.check(True)
+
+
+@pytest.mark.parametrize("dt,out", [("bf16", "bf16"), ("fp16", "fp16"), ("bf16", "fp16"), ("bf16", "fp32")])
+@pytest.mark.parametrize("D,had", [(128, True), (64, False)])
+@pytest.mark.parametrize("members,prefix,own,queries", [(3, 4, 3, (1,)), (30, 5, 3, (1, 2)), (12, 700, 200, (1, 20))])
+def test_lse_is_as_exact_as_binary32_arithmetic(ra, dt, out, D, had, members, prefix, own, queries):
+    """Over few keys too, whatever the outputs' type and the kernel."""
+    c = _case(ra, [(members, prefix)], own=own, queries=queries, D=D, dt=dt, out=out, rope=True, had=had, seed=members, gain=4.0)
+    c.run()
+    c.check_lse()
 
 
 def test_what_a_row_does_not_see_cannot_reach_it(ra):
