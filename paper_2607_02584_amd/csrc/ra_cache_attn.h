@@ -1681,13 +1681,25 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   return e != hipSuccess ? e : merge<D, M, K>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
 }
 
+// How many bf16 values hold P times V's scale for many rows: as many as the output shows.  For bf16 outputs one leaves
+// as much error as their own rounding does, sqrt(2) of it in all.  The errors of a scale group are one error, so over
+// few rows with few keys the mean can be a good deal more than that; there the new operators take two, which costs a
+// tenth (8 queries of 32 heads over 600 keys 33.2 us with one and 36.8 with two; 8 requests over a prefix of 30 000
+// 49.2 and 54.9 us).  At 512 rows 2048 group errors are averaged, and one value's error is sqrt(2) within 2 percent.
+constexpr int64_t kTwoTerms = 512;   // rows of all heads up to which
+template <Keys K>
+int terms_of(const CacheAttnArgs& a) {
+  if (a.out_dtype == RA_FP32) return 3;
+  return a.out_dtype == RA_FP16 || (K != kAll && static_cast<int64_t>(a.T) * a.Hq <= kTwoTerms) ? 2 : 1;
+}
+
 template <int D, bool F16, Keys K>
 hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
   const Grid g = grid_of(a, kRowTile, a.target_rows);
   const dim3 grid(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv));
-  // P in as many bf16 values as the output shows
-  if (a.out_dtype == RA_FP32) k_fine_rows<D, F16, K><<<grid, dim3(256), 0, s>>>(a);
-  else if (a.out_dtype == RA_FP16) k_rows<D, F16, true, K><<<grid, dim3(256), 0, s>>>(a);
+  const int terms = terms_of<K>(a);
+  if (terms == 3) k_fine_rows<D, F16, K><<<grid, dim3(256), 0, s>>>(a);
+  else if (terms == 2) k_rows<D, F16, true, K><<<grid, dim3(256), 0, s>>>(a);
   else k_rows<D, F16, false, K><<<grid, dim3(256), 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   return e != hipSuccess ? e : merge<D, kRowTile, K>(a, g, a.target_rows, static_cast<int64_t>(a.max_q) * a.G, s);

@@ -10,12 +10,15 @@
 // that its keys are read once for all, by the matrix cores as soon as there are
 // more than 16 rows.
 //
-// Four launches: k_shared_plan cuts prefixes and requests into pieces and turns
+// Three launches: k_shared_plan cuts prefixes and requests into pieces and turns
 // Q, once for all the pieces that take a row (in each of them it was 5 of a
-// piece's 66 us); the kernels for few and for many rows go through their
-// lists and leave partial rows in the workspace; a wave per row joins them.  (Both
-// kinds of pieces mixed in one launch took as long as one after the other: a piece of many rows that
-// waits for one of few ends as much later.)
+// piece's 66 us); k_both goes through the pieces of many rows and those of few
+// and leaves partial rows in the workspace (k_few alone where no prefix can have
+// more than 16 rows); k_join joins a row's parts, a wave per row.  Pieces of many
+// rows come first in the grid and are cut for their share of the places that the
+// card has, so that those of few run beside them from the start: 64 requests on 4
+// prefixes took 117 us with one launch after the other, 101 with the two kinds
+// alternating (whoever waits for a place ends as much later), 96 so.
 //
 // Bound by HBM while a group's rows are few, by the matrix cores and the softmax
 // beside them from some 64 rows on.
@@ -90,7 +93,7 @@ __device__ __forceinline__ Request shared_request(const CacheAttnArgs& a, const 
 // as small pieces fill what others leave.  The least such C is looked for with k = 1 and k = 2
 // (eight values at a time, three times over), and the cheaper one taken.
 // Cut into W / places blocks instead, without a look at what is left for the second round, 190
-// requests on five prefixes took 950 us in the kernel for many rows, now 600.
+// requests on five prefixes took 1000 us, with this 760 (the whole call, two launches still).
 constexpr int kPlan = 512;
 constexpr int kKnown = 4096;      // prefixes and requests whose tiles and blocks are kept in LDS
 constexpr int kRounds = 2;
@@ -523,11 +526,11 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
     if (a.out_dtype == RA_FP32) k_fine_few<D, 1, 2, kShared><<<grid, dim3(256), 0, s>>>(a);
     else k_few<D, 1, 2, kShared><<<grid, dim3(256), 0, s>>>(a);
   } else {
-    // P in as many bf16 values as the output shows
+    const int terms = terms_of<kShared>(a);
     auto go = [&](auto f16) {
       constexpr bool F16 = decltype(f16)::value;
-      if (a.out_dtype == RA_FP32) k_both<D, F16, 3><<<grid, dim3(256), 0, s>>>(a);
-      else if (a.out_dtype == RA_FP16) k_both<D, F16, 2><<<grid, dim3(256), 0, s>>>(a);
+      if (terms == 3) k_both<D, F16, 3><<<grid, dim3(256), 0, s>>>(a);
+      else if (terms == 2) k_both<D, F16, 2><<<grid, dim3(256), 0, s>>>(a);
       else k_both<D, F16, 1><<<grid, dim3(256), 0, s>>>(a);
     };
     if (a.is_fp16) go(std::integral_constant<bool, true>{});
