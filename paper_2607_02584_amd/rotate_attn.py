@@ -437,12 +437,33 @@ def _cache_rope(p, rope, device):
     return ptr, rows
 
 
+def _cache_ints(device, *what):
+    """Addresses of int32 tensors, given as (tensor, name, shape)."""
+    i32, index = _cache_dtypes()["i32"], device.index
+    try:   # all is well, as a rule
+        at = [t.data_ptr() for t, _, shape in what
+              if t.dtype is i32 and t.shape == shape and t.get_device() == index and t.is_contiguous()]
+        if len(at) == len(what):
+            return at
+    except AttributeError:
+        pass
+    return [_cache_tensor(t, name, i32, shape, device) for t, name, shape in what]
+
+
+def _current_stream(device):
+    """The device's current stream: its handle alone where torch hands that out
+    (0.1 us of host time instead of 1.9)."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
+
+
 def _cache_call(fn, where, device, stream, *args):
     """fn(*args, stream) with the tensors' device current, on `stream` or that
     device's current stream."""
     import torch
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
+        stream = _current_stream(device)
     if torch.cuda.current_device() == device.index:
         status = fn(*args, stream)
     else:
@@ -530,15 +551,14 @@ def cache_attn_sinks(p, sinks, q, cache, block_table, q_start, seq_lens, max_q, 
     `sinks` tokens stay visible (workspace as cache_attn's)."""
     dt = _cache_dtypes()
     pages, dev, R, T = _cache_pages(p, cache, dt["u8"]), cache.device, seq_lens.numel(), q.shape[0]
-    shape, i32 = (T, p.Hq, p.D), dt["i32"]
+    shape = T, p.Hq, p.D
     table, rows = _cache_rope(p, rope, dev)
     nws = _nbytes(ws)
     _cache_call(
         lib().rotate_attn_cache_attn_sinks, "rotate_attn_cache_attn_sinks", dev, stream, ctypes.byref(p), sinks, R, T, max_q,
         _cache_tensor(q, "q", dt[p.in_dtype], shape, dev, True), *_cache_rows(q), pages,
-        _cache_tensor(block_table, "block_table", i32, (R, p.max_blocks), dev),
-        _cache_tensor(q_start, "q_start", i32, (R + 1,), dev), _cache_tensor(seq_lens, "seq_lens", i32, (R,), dev),
-        table, rows, _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
+        *_cache_ints(dev, (block_table, "block_table", (R, p.max_blocks)), (q_start, "q_start", (R + 1,)),
+                     (seq_lens, "seq_lens", (R,))), table, rows, _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
         None if lse is None else _cache_tensor(lse, "lse", dt[FP32], shape[:2], dev),
         _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
 
@@ -550,17 +570,15 @@ def cache_attn_shared(p, q, cache, block_table, q_start, seq_lens, positions, gr
     read once for all (positions as cache_plan leaves them)."""
     dt = _cache_dtypes()
     pages, dev, R, T = _cache_pages(p, cache, dt["u8"]), cache.device, seq_lens.numel(), q.shape[0]
-    shape, i32, groups = (T, p.Hq, p.D), dt["i32"], prefix_lens.numel()
+    shape, groups = (T, p.Hq, p.D), prefix_lens.numel()
     table, rows = _cache_rope(p, rope, dev)
     nws = _nbytes(ws)
     _cache_call(
         lib().rotate_attn_cache_attn_shared, "rotate_attn_cache_attn_shared", dev, stream, ctypes.byref(p), R, T, groups,
         _cache_tensor(q, "q", dt[p.in_dtype], shape, dev, True), *_cache_rows(q), pages,
-        _cache_tensor(block_table, "block_table", i32, (R, p.max_blocks), dev),
-        _cache_tensor(q_start, "q_start", i32, (R + 1,), dev), _cache_tensor(seq_lens, "seq_lens", i32, (R,), dev),
-        _cache_tensor(positions, "positions", i32, (T,), dev),
-        _cache_tensor(group_start, "group_start", i32, (groups + 1,), dev),
-        _cache_tensor(prefix_lens, "prefix_lens", i32, (groups,), dev), table, rows,
+        *_cache_ints(dev, (block_table, "block_table", (R, p.max_blocks)), (q_start, "q_start", (R + 1,)),
+                     (seq_lens, "seq_lens", (R,)), (positions, "positions", (T,)),
+                     (group_start, "group_start", (groups + 1,)), (prefix_lens, "prefix_lens", (groups,))), table, rows,
         _cache_tensor(o, "o", dt[p.out_dtype], shape, dev),
         None if lse is None else _cache_tensor(lse, "lse", dt[FP32], shape[:2], dev),
         _cache_tensor(ws, "workspace", dt["u8"], (nws,), dev), nws)
@@ -578,24 +596,20 @@ def cache_shared_workspace(p: CacheParams, R: int, groups: int, T: int, device="
 def _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out, table_out,
                  refs_out, free_out, count_out):
     """R, the device, and (tables, out, cache, workspace, its bytes, status) as the library takes them."""
-    dt = _cache_dtypes()
-    i32, u8, R = dt["i32"], dt["u8"], seq_lens.numel()
+    R, u8 = seq_lens.numel(), _cache_dtypes()["u8"]
     pages, dev = _cache_pages(p, cache, u8), cache.device
-    per_request, per_page, rows = (R,), (p.num_pages,), (R, p.max_blocks)
-    check = _cache_tensor
-    seq = check(seq_lens, "seq_lens", i32, per_request, dev)
-    table = check(block_table, "block_table", i32, rows, dev)
-    refs = check(page_refs, "page_refs", i32, per_page, dev)
-    free = check(free_pages, "free_pages", i32, per_page, dev)
-    count = check(free_count, "free_count", i32, (1,), dev)
-    out = CacheTables(seq if seq_out is None else check(seq_out, "seq_out", i32, per_request, dev),
-                      table if table_out is None else check(table_out, "table_out", i32, rows, dev),
-                      refs if refs_out is None else check(refs_out, "refs_out", i32, per_page, dev),
-                      free if free_out is None else check(free_out, "free_out", i32, per_page, dev),
-                      count if count_out is None else check(count_out, "count_out", i32, (1,), dev))
+    per_request, per_page, rows, one = (R,), (p.num_pages,), (R, p.max_blocks), (1,)
+    at = _cache_ints(dev, (seq_lens, "seq_lens", per_request), (block_table, "block_table", rows),
+                     (page_refs, "page_refs", per_page), (free_pages, "free_pages", per_page),
+                     (free_count, "free_count", one),
+                     (seq_lens if seq_out is None else seq_out, "seq_out", per_request),
+                     (block_table if table_out is None else table_out, "table_out", rows),
+                     (page_refs if refs_out is None else refs_out, "refs_out", per_page),
+                     (free_pages if free_out is None else free_out, "free_out", per_page),
+                     (free_count if count_out is None else count_out, "count_out", one), (status, "status", (4,)))
     nws = _nbytes(ws)
-    return R, dev, (CacheTables(seq, table, refs, free, count), out, pages, check(ws, "workspace", u8, (nws,), dev), nws,
-                    check(status, "status", i32, (4,), dev))
+    return R, dev, (CacheTables(*at[:5]), CacheTables(*at[5:10]), pages, _cache_tensor(ws, "workspace", u8, (nws,), dev), nws,
+                    at[10])
 
 
 def cache_fork(p, parents, children, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status,
@@ -606,10 +620,10 @@ def cache_fork(p, parents, children, seq_lens, block_table, page_refs, free_page
     updated in place unless arrays for their new state are given."""
     R, dev, rest = _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out,
                                 table_out, refs_out, free_out, count_out)
-    i32, n = _cache_dtypes()["i32"], parents.numel()
-    _cache_call(lib().rotate_attn_cache_fork, "rotate_attn_cache_fork", dev, stream, ctypes.byref(p), R, n,
-                _cache_tensor(parents, "parents", i32, (n,), dev), _cache_tensor(children, "children", i32, (n,), dev),
-                None if lens is None else _cache_tensor(lens, "lens", i32, (n,), dev), *rest)
+    n = (parents.numel(),)
+    what = (parents, "parents", n), (children, "children", n), (lens, "lens", n)
+    _cache_call(lib().rotate_attn_cache_fork, "rotate_attn_cache_fork", dev, stream, ctypes.byref(p), R, n[0],
+                *((*_cache_ints(dev, *what[:2]), None) if lens is None else _cache_ints(dev, *what)), *rest)
 
 
 def cache_trim(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, keep=None, sinks=-1,
@@ -620,7 +634,7 @@ def cache_trim(p, seq_lens, block_table, page_refs, free_pages, free_count, cach
     R, dev, rest = _page_tables(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out,
                                 table_out, refs_out, free_out, count_out)
     _cache_call(lib().rotate_attn_cache_trim, "rotate_attn_cache_trim", dev, stream, ctypes.byref(p), R,
-                None if keep is None else _cache_tensor(keep, "keep", _cache_dtypes()["i32"], (R,), dev), sinks, *rest)
+                None if keep is None else _cache_ints(dev, (keep, "keep", (R,)))[0], sinks, *rest)
 
 
 def cache_compact(p, seq_lens, block_table, page_refs, free_pages, free_count, cache, ws, status, seq_out=None,
