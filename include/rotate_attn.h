@@ -438,7 +438,8 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
  * between the two are not read, and their table entries may be -1
  * (cache_trim).  Arguments, workspace and limits are those of cache_attn; so is the
  * precision of o (one bf16 value only from T * Hq > 512 on), and lse is as exact as
- * binary32 arithmetic whatever the type of o. */
+ * binary32 arithmetic whatever the type of o; elements of a query are held to within
+ * 2^-24 of its largest. */
 int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_t R, int32_t T, int32_t max_q,
                                  const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* cache,
                                  const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
@@ -460,10 +461,11 @@ int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_
  * 2^22, nor T * Hq 2^26.
  * Precision: o as cache_attn's (with bf16 outputs and T * Hq > 512 weights times V's
  * scales are one bf16 value, 2^-8, where a prefix, or a request's own keys, have more
- * than 16 rows: queries times Hq / Hkv, a prefix having those of its whole group); lse is as exact as
- * binary32 arithmetic whatever the type of o.
+ * than 16 rows: queries times Hq / Hkv, a prefix having those of its whole group); lse is
+ * as exact as binary32 arithmetic whatever the type of o; elements of a query are held to
+ * within 2^-24 of its largest.
  * Workspace: cache_shared_workspace_size bytes (partial outputs of every row, twice, and
- * Q: about T Hq (12 D + 16), and 147 456 rows of (4 D + 8) for cuts), 256-byte
+ * Q: about T Hq (15.75 D + 16), and 147 456 rows of (4 D + 8) for cuts), 256-byte
  * aligned; its contents do not matter before or after. */
 int rotate_attn_cache_shared_workspace_size(const ra_cache_params* p, int32_t R, int32_t groups, int32_t T, size_t* bytes);
 int rotate_attn_cache_attn_shared(const ra_cache_params* p, int32_t R, int32_t T, int32_t groups, const void* q,

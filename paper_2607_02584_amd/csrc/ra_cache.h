@@ -101,7 +101,8 @@ struct CacheAttnArgs {
   int4* pieces[2];                  // of few and of many rows
   int* counts;                      // [2]
   int bound[2];                     // of the pieces
-  uint16_t* turned;                 // [T][Hq][2][D] Q as the matrix products take it
+  uint16_t* turned;                 // [T][Hq][2][D] Q as the matrix products of few rows take it
+  uint8_t* turned6;                 // [T][Hq][5][D] in 6 bits each, of many rows
   float* back;                      // [T][Hq] what the scores are multiplied by
   int64_t part_rows;                // rows of part_o for each KV head
 };

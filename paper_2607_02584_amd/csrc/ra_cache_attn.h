@@ -379,6 +379,19 @@ __device__ __forceinline__ bool take_piece(const CacheAttnArgs& a, SchedShared& 
   if constexpr (K == kShared) return listed_piece<(M > kFewRows)>(a, x, out);
   else return find_piece<M, K>(a, sh, x, false, target, out);
 }
+// Q of cache_attn_sinks and cache_attn_shared for many rows: a row, scaled by a power of two so that its largest element is in
+// [1, 2), as the sum of kTerms digits to the base 32, multiples of 1/8 up to 2 times 32^-z.  An E2M3 code holds such a
+// digit (its value times 8 and its sign are the code), and the matrix cores take 6-bit codes of Q and the 4-bit ones of K, as
+// they lie in the page, at four times the rate of 16 bits.  Five digits hold every element to within 2^-24 of the row's largest,
+// in 20 products of 32 cycles for a wave's 32 rows and 64 keys; two binary16 values needed 32, codes turned into
+// binary16 and four times the LDS for K.  (sinks_prompt 545 -> 457 us, shared_documents 780 -> 674, shared_decode 98 -> 89;
+// four digits would leave 2e-6 of an lse over few keys.)
+constexpr int kTerms = 5;
+// 1.5 * 2^k with k such that adding it leaves multiples of 32^-z / 8
+__host__ __device__ constexpr float digit_of(int z) { return 1.5f * (1 << 20 >> (5 * z)); }
+template <int D>
+__host__ __device__ constexpr int row_bytes6() { return kTerms * D * 3 / 4; }
+
 // 16 bytes of a row's Q, turned and in two values by the launch before: hi of its D channels, then lo.
 template <int D>
 __device__ __forceinline__ uint4 turned(const CacheAttnArgs& a, const Piece& p, int h, int row, int z, int channel) {
@@ -386,6 +399,31 @@ __device__ __forceinline__ uint4 turned(const CacheAttnArgs& a, const Piece& p, 
   const int i = row / a.G;
   const int64_t at = static_cast<int64_t>(p.q.q0 + i) * a.Hq + h * a.G + row - i * a.G;
   return *reinterpret_cast<const uint4*>(a.turned + at * 2 * D + z * D + channel);
+}
+// The lane's half of a row's Q in terms of 6 bits (many rows), as the launch before left it.
+template <int D>
+__device__ __forceinline__ void turned6(const CacheAttnArgs& a, const Piece& p, int h, int row, int hh, uint32_t (&q)[D / 64][kTerms][6]) {
+  uint32_t w[kTerms][D * 3 / 32] = {};
+  if (row < p.q.ql * a.G) {
+    const int i = row / a.G;
+    const int64_t at = static_cast<int64_t>(p.q.q0 + i) * a.Hq + h * a.G + row - i * a.G;
+    typedef typename std::conditional<D == 128, uint4, uint2>::type V;
+    const V* src = reinterpret_cast<const V*>(a.turned6 + at * row_bytes6<D>() + hh * (D * 3 / 8));
+#pragma unroll
+    for (int z = 0; z < kTerms; ++z)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const V v = src[z * 6 + i];
+        constexpr int N = sizeof(V) / 4;
+        w[z][N * i] = v.x;
+        w[z][N * i + 1] = v.y;
+        if constexpr (D == 128) w[z][N * i + 2] = v.z, w[z][N * i + 3] = v.w;
+      }
+  }
+#pragma unroll
+  for (int z = 0; z < kTerms; ++z)
+#pragma unroll
+    for (int i = 0; i < D * 3 / 32; ++i) q[i / 6][z][i % 6] = w[z][i];
 }
 __device__ __forceinline__ float turned_back(const CacheAttnArgs& a, const Piece& p, int h, int row) {
   if (row >= p.q.ql * a.G) return 1.0f;
@@ -604,8 +642,8 @@ struct Rows {
 // the use needs on the skipping path (seen as wrong first registers when the
 // second 16 rows were skipped inside the step).  N is therefore a constant.
 // Q is two binary16 values for binary32 outputs, and for all of cache_attn_sinks and cache_attn_shared: their lse is as
-// exact as binary32 arithmetic whatever the outputs' type.  (Two bf16 values left 2e-6 of an lse over few keys.  For many
-// rows it costs 5 %, sinks_prompt 520 -> 545 us, of which the multiplication by the rows' powers of two is a tenth.)
+// exact as binary32 arithmetic whatever the outputs' type.  (Two bf16 values left 2e-6 of an lse over few keys.)
+// For many rows these hold Q as digits.
 template <bool FINE, Keys K>
 constexpr bool fine_q() { return FINE || K != kAll; }
 
@@ -941,15 +979,15 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, f
 // --------------------------------------------------------- many rows per request --
 //
 // Bound by the matrix cores and the softmax beside them.  NW waves of 32 rows
-// share tiles of 64 keys in LDS, as bf16 values of the codes (exact), scales
-// apart: each wave loads its share of the next tile's codes while the present
+// share tiles of 64 keys in LDS, as bf16 values of the codes (exact; K of the operators with digits as it
+// lies in the page), scales apart: each wave loads its share of the next tile's codes while the present
 // one is computed, and converts them into the other LDS buffer at its end.
 // S^T = K Q^T and O^T += V^T P^T on the 32x32x16 product: a lane holds one
 // query's scores (key 32 c + 8 (r / 4) + 4 hh + r % 4 in register r of chunk
 // c), which rounded to 16 bits are the second operand of the next product, and
 // the same query's output, so that rescaling it is a factor per lane.
 //
-// Q (after RoPE, rotation and scale, in binary32) is the sum of two bf16
+// Q (after RoPE, rotation and scale, in binary32) is for cache_attn the sum of two bf16
 // values, within 2^-17 of each element.  P * (V's scale) is one, within 2^-8,
 // where the output is bf16, which is then 2.3e-3 off (relative) instead of
 // 1.7e-3, and two (LO) where it is binary16: prompts of 26k tokens take 2.0 ms
@@ -959,7 +997,7 @@ __device__ __forceinline__ void few_rows(const CacheAttnArgs& a, FewLds<D, NT, f
 // 2^127: in units of a tile's largest scale, binary16 loses the rows that do not
 // see that token.
 //
-// LDS: K [chunk of 8 channels][key], V [octet of keys][channel position], 16
+// LDS: K [chunk of 8 channels][key] (as digits meet it: [chunk of 32 channels][key]), V [octet of keys][channel position], 16
 // bytes each, read by 32 neighbouring lanes in a row without bank conflicts.
 // Channel d of V sits at position (d % E) * 16 + d / E, E = D / 16 (its page
 // order), an octet holds keys 16 s + 4 hh + {0..3, 8..11} of step s.
@@ -976,15 +1014,13 @@ __device__ __forceinline__ v16f score32(uint4 k, uint4 q, v16f c) {
   else return mfma32(k, q, c);
 }
 
-// As load_q, D / 2 channels per lane.
-template <int D, bool F16, bool FINE>
-__device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
-                                          uint4 (&hi)[D / 16], uint4 (&lo)[D / 16]) {
+// D / 2 channels of a row after RoPE, rotation and scale.
+template <int D, bool F16>
+__device__ __forceinline__ void values_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane, float (&y)[D / 2]) {
   constexpr int N = D / 2;
   const int hh = lane >> 5;
   const bool ok = row < p.q.ql * a.G;
   const int i = ok ? row / a.G : 0, head = h * a.G + (ok ? row - i * a.G : 0);
-  float y[N];
   const uint16_t* src = a.q + static_cast<int64_t>(p.q.q0 + i) * a.q_ts + head * a.q_hs + hh * N;
 #pragma unroll
   for (int c = 0; c < N / 8; ++c) {
@@ -1015,6 +1051,15 @@ __device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p
   }
 #pragma unroll
   for (int e = 0; e < N; ++e) y[e] *= a.c;   // scores come out in base 2
+}
+
+// As load_q, D / 2 channels per lane.
+template <int D, bool F16, bool FINE>
+__device__ __forceinline__ float load_q32(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
+                                          uint4 (&hi)[D / 16], uint4 (&lo)[D / 16]) {
+  constexpr int N = D / 2;
+  float y[N];
+  values_q32<D, F16>(a, p, h, row, lane, y);
   float power = 1.0f;
   if constexpr (FINE) {
     float m = 0.0f;
@@ -1044,6 +1089,67 @@ __device__ __forceinline__ void each(F&& f) {
   each_(f, std::make_integer_sequence<int, N>());
 }
 
+// 32 values -> 6-bit codes (E2M3) of value / scale, the two sources interleaved.  The
+// instruction writes its result before it has read all of its sources, and reads their first registers a cycle
+// early, which the compiler does not know; nor does it see that a product may follow.
+__device__ __forceinline__ void pack6(const v16f& even, const v16f& odd, float scale, uint32_t (&to)[6]) {
+  typedef uint32_t v6u __attribute__((ext_vector_type(6)));
+  v6u r = {};
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("s_nop 0\n\tv_cvt_scalef32_2xpk16_fp6_f32 %0, %1, %2, %3\n\ts_nop 1" : "=&v"(r) : "v"(even), "v"(odd), "s"(scale));
+#endif
+#pragma unroll
+  for (int i = 0; i < 6; ++i) to[i] = r[i];
+}
+
+// c += K times digit Z of Q: 32 keys, 32 rows, 64 channels.  (The form without scales is a single instruction word.)
+template <int Z>
+__device__ __forceinline__ v16f score6(uint4 k, const uint32_t (&q)[6], v16f c) {
+  typedef int v8i __attribute__((ext_vector_type(8)));
+  const v8i A = {static_cast<int>(k.x), static_cast<int>(k.y), static_cast<int>(k.z), static_cast<int>(k.w), 0, 0, 0, 0};
+  const v8i B = {static_cast<int>(q[0]), static_cast<int>(q[1]), static_cast<int>(q[2]), static_cast<int>(q[3]),
+                 static_cast<int>(q[4]), static_cast<int>(q[5]), 0, 0};
+  if constexpr (Z == 0) return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, 2, 0, 0, 0, 0);
+  // biased exponents 127 - 5, - 10, - 15, - 20, a byte each
+  else return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(A, B, c, 4, 2, 0, 0x7f7f7f7f, Z - 1, 0x6b70757a);
+}
+
+// load_q32 as digits.
+template <int D, bool F16>
+__device__ __forceinline__ float load_q6(const CacheAttnArgs& a, const Piece& p, int h, int row, int lane,
+                                         uint32_t (&q)[D / 64][kTerms][6]) {
+  constexpr int N = D / 2;
+  float y[N];
+  values_q32<D, F16>(a, p, h, row, lane, y);
+  float m = 0.0f, bad = 0.0f;   // bad: NaN where an element is not finite, which no digit is
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    m = fmaxf(m, fabsf(y[e]));
+    bad = __fmaf_rn(y[e], 0.0f, bad);
+  }
+  bad += lane_xor<32>(bad);
+  const float power = row_power(fmaxf(m, lane_xor<32>(m)));
+#pragma unroll
+  for (int e = 0; e < N; ++e) y[e] = y[e] * power * 0x1p-14f;
+  each<N / 32>([&](auto st) {
+    each<kTerms>([&](auto zz) {
+      constexpr int z = decltype(zz)::value, n = 32 * decltype(st)::value;
+      v16f t[2];
+#pragma unroll
+      for (int e = 0; e < 32; ++e) {
+        float d = y[n + e];
+        if constexpr (z + 1 < kTerms) {
+          d = (d + digit_of(z)) - digit_of(z);
+          y[n + e] -= d;
+        }
+        t[e & 1][e >> 1] = d;
+      }
+      pack6(t[0], t[1], 1.0f / (1 << (5 * z)), q[n / 32][z]);
+    });
+  });
+  return inverse_power(power) * 0x1p14f + bad;
+}
+
 // Pipeline over tiles: a tile begins with its scores in registers.  Once a
 // chunk of 32 keys has its probabilities, its score registers take the next
 // tile's scores of that chunk; those products and the chunk's P V run on the
@@ -1051,13 +1157,13 @@ __device__ __forceinline__ void each(F&& f) {
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
 // TERMS: bf16 values that hold P * (V's scale); three come with binary16 pairs of Q.
-template <int D>
+template <int D, Keys K>
 struct RowsLds {
   struct Scales {
     float ks[64], vs[64];
     unsigned long long there, plain;   // keys that are on a page; those of them with a finite V
   };
-  __align__(16) uint4 k[2][D / 8][64];
+  __align__(16) uint4 k[2][K == kAll ? D / 8 : D / 32][64];   // chunks of 8 channels in 16 bits, of 32 in 4
   __align__(16) uint4 v[2][8][D];
   Scales sc[2];
   SchedShared sched;
@@ -1065,11 +1171,12 @@ struct RowsLds {
 
 // Piece x0 of KV head h.
 template <int D, bool F16, int TERMS, Keys K>
-__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& buf, int x0, int h) {
-  constexpr bool QF = fine_q<TERMS == 3, K>();
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>& buf, int x0, int h) {
+  constexpr bool SIX = K != kAll;          // Q as digits, K as it lies in the page
+  constexpr bool QF = TERMS == 3 || SIX;   // scores are multiplied by `back`
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
-  typedef typename RowsLds<D>::Scales Scales;
+  typedef typename RowsLds<D, K>::Scales Scales;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
   Piece p;
@@ -1166,7 +1273,12 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
   // last tile replaces tiles that are done with.
   auto put_k = [&](int b, auto part) {
     constexpr int c = decltype(part)::value;
-    if constexpr (c < D / 32) {
+    if constexpr (SIX) {
+      if constexpr (c == 0) {   // chunks of 16 channels are put together where D is 64
+        if constexpr (D == 128) buf.k[b & 1][lane >> 4][mine + (lane & 15)] = sk;
+        else reinterpret_cast<uint2*>(&buf.k[b & 1][hh][mine + (lane & 15)])[(lane >> 4) & 1] = sk;
+      }
+    } else if constexpr (c < D / 32) {
       const uint32_t x = dword_of<D>(sk, c);
       buf.k[b & 1][(lane >> 4) * (D / 32) + c][mine + (lane & 15)] =
           codes8<QF>(x);
@@ -1222,15 +1334,14 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
     entries(b0, b0);
     ask(b0, b0);
   }
-  uint4 q[KC], q_lo[KC];
+  uint4 q[KC], q_lo[KC];            // 16-bit values
+  uint32_t q6[D / 64][kTerms][6];   // digits
   float back = 1.0f;
   if constexpr (K == kShared) {
-#pragma unroll
-    for (int c = 0; c < KC; ++c) {
-      q[c] = turned<D>(a, p, h, row, 0, hh * (D / 2) + c * 8);
-      q_lo[c] = turned<D>(a, p, h, row, 1, hh * (D / 2) + c * 8);
-    }
-    back = turned_back(a, p, h, row);
+    turned6<D>(a, p, h, row, hh, q6);
+    back = turned_back(a, p, h, row) * 0x1p14f;
+  } else if constexpr (SIX) {
+    back = load_q6<D, F16>(a, p, h, row, lane, q6);
   } else {
     back = load_q32<D, F16, QF>(a, p, h, row, lane, q, q_lo);
   }
@@ -1249,16 +1360,25 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
   }
   __syncthreads();
 
-  auto k_op = [&](int b, int c, int kc) { return buf.k[b & 1][hh * KC + kc][c * 32 + j]; };
+  constexpr int KS = SIX ? D / 64 : KC;   // of a chunk of keys: operands of K, and products
+  constexpr int KP = SIX ? KS * kTerms : KC;
+  auto k_op = [&](int b, int c, int kc) { return buf.k[b & 1][hh * KS + kc][c * 32 + j]; };
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
+    if constexpr (SIX) {
+      each<KS>([&](auto st) {
+        const uint4 k = k_op(b0, c, st);
+        each<kTerms>([&](auto z) { s[c] = score6<kTerms - 1 - z>(k, q6[st][kTerms - 1 - z], s[c]); });
+      });
+    } else {
 #pragma unroll
-    for (int kc = 0; kc < KC; ++kc) {
-      const uint4 k = k_op(b0, c, kc);
-      s[c] = score32<QF>(k, q[kc], s[c]);
-      s[c] = score32<QF>(k, q_lo[kc], s[c]);
+      for (int kc = 0; kc < KC; ++kc) {
+        const uint4 k = k_op(b0, c, kc);
+        s[c] = score32<QF>(k, q[kc], s[c]);
+        s[c] = score32<QF>(k, q_lo[kc], s[c]);
+      }
     }
     settle(s[c]);
   }
@@ -1362,6 +1482,57 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
     // is one chain (behind the last tile they take what lies there and nothing
     // reads them: a second form of this code costs more than they do)
     static_assert(2 * MT == KC, "as many of either");
+    if constexpr (SIX) {
+      // the same with the operands of K in hand for a whole chunk, and KP / (2 MT) products of the scores for one of P V
+      constexpr int NV = 2 * MT, kAhead = TERMS == 3 ? 2 : 4, NB = KS == 1 ? 2 : 1;   // of K: the next chunk's takes the place of what is done with
+      auto operand = [&](int c, int i) { return buf.v[b & 1][(c * 2 + i / MT) * 2 + hh][(i % MT) * 32 + j]; };
+      uint4 ops[kAhead], ks[NB][KS];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) ops[i] = operand(0, i);
+#pragma unroll
+      for (int i = 0; i < KS; ++i) ks[0][i] = k_op(b + 1, 0, i);
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) probs(0, r4);
+      __builtin_amdgcn_sched_barrier(0);
+      each<2>([&](auto cc) {
+        constexpr int c = decltype(cc)::value;
+        each<NV>([&](auto ii) {
+          constexpr int i = decltype(ii)::value, n = c * NV + i + kAhead;
+          uint4& op = ops[(c * NV + i) % kAhead];
+#pragma unroll
+          for (int z = 0; z < TERMS; ++z) {
+            const uint32_t* w = pw[c][z] + 4 * (i / MT);
+            o[i % MT] = mfma32(op, make_uint4(w[0], w[1], w[2], w[3]), o[i % MT]);
+          }
+          if constexpr (n < 2 * NV) op = operand(n / NV, n % NV);
+          if constexpr (c == 0 && NB == 2 && i == 0) ks[NB - 1][0] = k_op(b + 1, 1, 0);
+          if constexpr (i == 0)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[c][r] = 0.0f;
+          constexpr int x0 = i * KP / NV, x1 = (i + 1) * KP / NV;
+          each<x1 - x0>([&](auto xx) {
+            constexpr int x = x0 + decltype(xx)::value, z = kTerms - 1 - x % kTerms;
+            s[c] = score6<z>(ks[c % NB][x / kTerms], q6[x / kTerms][z], s[c]);
+            if constexpr (c == 0 && NB == 1 && z == 0) ks[0][x / kTerms] = k_op(b + 1, 1, x / kTerms);
+          });
+          if constexpr (i % (NV / 4) == NV / 4 - 1) {
+            if constexpr (c == 0) {
+              probs(1, i / (NV / 4));
+            } else {
+              put_k(b + 2, std::integral_constant<int, i / (NV / 4)>{});
+              put_v(b + 1, std::integral_constant<int, i / (NV / 4)>{});
+            }
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        });
+        if constexpr (c == 0) {
+          __builtin_amdgcn_s_setprio(0);
+          pin_staged();
+        }
+      });
+      l += (ls[0] + ls[1]) + (ls[2] + ls[3]);
+      return;
+    }
     constexpr int NP = 2 * MT + KC, kAhead = 4;
     auto operand = [&](int c, int i) {
       const int n = i / 2;
@@ -1642,13 +1813,13 @@ __global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
 
 template <int D, bool F16, bool LO, Keys K>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
-  __shared__ RowsLds<D> lds;
+  __shared__ RowsLds<D, K> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   many_rows<D, F16, LO ? 2 : 1, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, bool F16, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
-  __shared__ RowsLds<D> lds;
+  __shared__ RowsLds<D, K> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   many_rows<D, F16, 3, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }

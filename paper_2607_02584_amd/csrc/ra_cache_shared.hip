@@ -392,13 +392,38 @@ __device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row) {
   const float power = row_power(m);
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= power;
-  if (ok && b == 0) a.back[row] = inverse_power(power);
+  float bad = 0.0f;   // NaN where an element is not finite, which no digit is
+#pragma unroll
+  for (int e = 0; e < 8; ++e) bad = __fmaf_rn(y[e], 0.0f, bad);
+  bad += lane_xor<1>(bad);
+  bad += lane_xor<2>(bad);
+  bad += lane_xor<7>(bad);
+  if constexpr (D == 128) bad += lane_xor<8>(bad);
+  if (ok && b == 0) a.back[row] = inverse_power(power) + bad;
   uint4 hi, lo;
   split8(y, true, hi, lo);
   if (ok) {
     uint16_t* dst = a.turned + row * 2 * D + b * 8;
     *reinterpret_cast<uint4*>(dst) = hi;
     *reinterpret_cast<uint4*>(dst + D) = lo;
+  }
+  // the digits' codes: |n| in eighths, and the sign
+  uint16_t* six = reinterpret_cast<uint16_t*>(a.turned6 + row * row_bytes6<D>() + b * 6);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) y[e] *= 0x1p-14f;
+#pragma unroll
+  for (int z = 0; z < kTerms; ++z) {
+    uint64_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float d = (y[e] + digit_of(z)) - digit_of(z);
+      y[e] -= d;
+      const uint32_t n = static_cast<uint32_t>(fabsf(d) * (8.0f * (1 << (5 * z))));
+      w |= static_cast<uint64_t>((n & 31) | (__float_as_uint(d) >> 31) << 5) << (6 * e);
+    }
+    if (ok)
+#pragma unroll
+      for (int i = 0; i < 3; ++i) six[z * (D * 3 / 8) + i] = static_cast<uint16_t>(w >> (16 * i));
   }
 }
 
@@ -440,7 +465,7 @@ __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a) {
   constexpr bool FINE = TERMS == 3;
   __shared__ union {
     FewLds<D, 1, true> few;
-    RowsLds<D> rows;
+    RowsLds<D, kShared> rows;
   } lds;
   const int x = blockIdx.x / a.g.Hkv, h = blockIdx.x - x * a.g.Hkv, many = __builtin_amdgcn_readfirstlane(a.counts[1]);
   if (x < many) many_rows<D, F16, TERMS, kShared>(a, lds.rows, x, h);
@@ -545,7 +570,7 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
 struct SharedSpace {
   int64_t rows;        // of parts, for every KV head
   int64_t bound[2];    // pieces of few and of many rows
-  size_t ml, requests, pieces[2], info, owner, counts, back, turned, bytes;   // offsets
+  size_t ml, requests, pieces[2], info, owner, counts, back, turned, turned6, bytes;   // offsets
 };
 // Every row once for its prefix and once for its own keys; cutting adds at most the pieces of all rounds, a tile each
 // (sum over tiles of parts - 1 <= W / C).  Prefixes and requests of many rows have more than 16 of them.
@@ -574,6 +599,7 @@ SharedSpace space_of(int D, int Hkv, int G, int R, int groups, int T) {
   x.counts = take(2 * sizeof(int));
   x.back = take(q * sizeof(float));
   x.turned = take(q * 4 * D);
+  x.turned6 = take(q * kTerms * D * 3 / 4);
   x.bytes = at;
   return x;
 }
@@ -600,6 +626,7 @@ hipError_t launch_cache_attn_shared(const CacheAttnArgs& a, int D, void* workspa
   b.counts = reinterpret_cast<int*>(ws + x.counts);
   b.back = reinterpret_cast<float*>(ws + x.back);
   b.turned = reinterpret_cast<uint16_t*>(ws + x.turned);
+  b.turned6 = reinterpret_cast<uint8_t*>(ws + x.turned6);
   b.part_rows = x.rows;
   return D == 128 ? shared_d<128>(b, s) : shared_d<64>(b, s);
 }

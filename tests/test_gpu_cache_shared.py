@@ -156,6 +156,34 @@ def test_what_a_row_does_not_see_cannot_reach_it(ra):
         assert torch.isnan(z[:c.start[-1]]).all() and torch.equal(lse3[rest], lse2[rest])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("members,queries", [(3, (1,)), (40, (1,)), (4, (20,))])
+def test_queries_that_are_not_finite(ra, D, members, queries):
+    """One element of a query: its rows alone are NaN, lse too."""
+    for value in (float("nan"), float("inf"), -float("inf")):
+        c = _case(ra, [(members, 70)], queries=queries, D=D, seed=members)
+        x, lse = (t.clone() for t in c.run())
+        hit = torch.zeros(c.T, 4, dtype=torch.bool)
+        for t, h, d in ((0, 1, D - 1), (c.T // 2, 3, 5), (c.T - 1, 0, 33)):
+            c.q[t, h, d] = value
+            hit[t, h] = True
+        y, lse2 = c.run()
+        assert torch.isnan(y.cpu()[hit]).all() and torch.isnan(lse2.cpu()[hit]).all()
+        assert torch.equal(x.cpu()[~hit], y.cpu()[~hit]) and torch.equal(lse.cpu()[~hit], lse2.cpu()[~hit])
+
+
+@pytest.mark.parametrize("power", [-60, 60])
+def test_queries_far_from_one(ra, power):
+    """Large queries with small keys and the other way round, rows of zeros among them."""
+    for members, queries in ((3, (1,)), (40, (1, 9))):
+        c = _case(ra, [(members, 70)], queries=queries, seed=members)
+        c.q *= 2.0 ** power
+        c.q[0, 1] = 0.0
+        c.scales()[:, :, 0] *= 2.0 ** -power
+        c.run()
+        c.check(True)
+
+
 def test_pages_that_are_none_are_masked(ra):
     for members in (3, 40):
         c = _case(ra, [(members, 100)], own=50, seed=9)

@@ -135,6 +135,34 @@ def test_what_a_row_does_not_see_cannot_reach_it(ra):
         assert torch.isnan(z[:q_len]).all() and torch.equal(lse3[:q_len - 2], lse2[:q_len - 2])
 
 
+@pytest.mark.parametrize("D,qs", [(128, [1, 60]), (64, [3, 33]), (128, [20])])
+def test_queries_that_are_not_finite(ra, D, qs):
+    """One element of a query: its rows alone are NaN, lse too."""
+    for value in (float("nan"), float("inf"), -float("inf")):
+        c = Case(ra, 6, 2, D, 16, [300] * len(qs), qs, window=40, sinks=5, seed=D)
+        x, lse = (t.clone() for t in c.run())
+        hit = torch.zeros(c.T, 6, dtype=torch.bool)
+        for r in range(len(qs)):
+            t, h, d = c.start[r] + qs[r] // 2, 1 + 2 * r, 7 * r + 30
+            c.q[t, h, d] = value
+            hit[t, h] = True
+        y, lse2 = c.run()
+        assert torch.isnan(y.cpu()[hit]).all() and torch.isnan(lse2.cpu()[hit]).all()
+        assert torch.equal(x.cpu()[~hit], y.cpu()[~hit]) and torch.equal(lse.cpu()[~hit], lse2.cpu()[~hit])
+
+
+@pytest.mark.parametrize("power", [-60, 60])
+def test_queries_far_from_one(ra, power):
+    """Large queries with small keys and the other way round, rows of zeros among them."""
+    for qs in ([1, 3], [70]):
+        c = Case(ra, 4, 2, 128, 16, [200] * len(qs), qs, window=50, sinks=9, seed=power + 100)
+        c.q *= 2.0 ** power
+        c.q[0, 1] = 0.0
+        c.scales()[:, :, 0] *= 2.0 ** -power
+        c.run()
+        c.check(_many(c))
+
+
 def test_repeats_and_streams(ra):
     c = Case(ra, 8, 2, 128, 32, [5000, 300, 4000], [1, 40, 2], rope=True, had=True, window=1000, sinks=40, seed=30)
     x, lse = (t.clone() for t in c.run())
