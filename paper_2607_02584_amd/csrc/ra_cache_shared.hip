@@ -111,7 +111,7 @@ struct PlanShared {
   int from[2][kPlan];            // first piece of each, of few and of many rows
   int parts[kPlan];
   float w[kPlan / 64][2];
-  int n[kPlan / 64][6];
+  int n[kPlan / 64][7];
   unsigned lo[2][kRounds], hi[2][kRounds];
   int fits[2][4 * (kPlan / 64)], wide[3][2 * kRounds];
 };
@@ -138,12 +138,14 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   // what there is: blocks of all tiles, the longest, tiles
   float W[2] = {0.0f, 0.0f};
   int count[2] = {0, 0}, longest[2] = {0, 0}, finest[2] = {0, 0};   // finest: pieces of kLeast blocks
+  int queries = 0;   // of prefixes and requests, no more than 2 T where offsets and groups ascend
   Request mine = {};
 #pragma unroll 1
   for (int v = tid; v < N; v += kPlan) {
     const Request q = shared_request(a, l, v);
     if (v == tid) mine = q;
     const int many = q.ql * a.G > kFewShared;
+    queries = queries + q.ql < 1 << 24 ? queries + q.ql : 1 << 24;
     if (v < kKnown) {
       sh.blocks[v] = q.blocks;
       sh.tiles[v] = many ? -q.tiles : q.tiles;
@@ -172,7 +174,14 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       sh.n[w][2 + k] = longest[k];
       sh.n[w][4 + k] = finest[k];
     }
+  queries = __builtin_amdgcn_readlane(wave_sums(queries), 63);
+  if (lane == 0) sh.n[w][6] = queries < 1 << 24 ? queries : 1 << 24;
   __syncthreads();
+  queries = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) queries += sh.n[i][6];
+  // (what does not fit the call has no pieces: their numbers would pass 32 bits)
+  const bool fits = queries <= 2 * a.T;
   W[0] = W[1] = 0.0f;
   count[0] = count[1] = longest[0] = longest[1] = finest[0] = finest[1] = 0;
 #pragma unroll
@@ -294,7 +303,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     if (v < N) q = v0 == 0 ? mine : shared_request(a, l, v);
     const int many = q.ql * a.G > kFewShared;
     const unsigned c = many ? C[1] : C[0];
-    const int parts = q.tiles ? (q.blocks ? static_cast<int>((q.blocks + c - 1) / c) : 1) : 0;
+    const int parts = q.tiles && fits ? (q.blocks ? static_cast<int>((q.blocks + c - 1) / c) : 1) : 0;
     const int val[4] = {many ? 0 : q.tiles * parts, many ? q.tiles * parts : 0, many ? 0 : q.ql * a.G * parts,
                         many ? q.ql * a.G * parts : 0};
     int from[4];

@@ -221,6 +221,23 @@ def test_lengths_that_do_not_fit_touch_nothing_outside(ra):
         assert (ws[:2048] == 0x33).all() and (ws[2048 + size:] == 0x33).all(), k
 
 
+def test_offsets_whose_rows_pass_32_bits(ra):
+    """3000 requests that all have all 30 000 queries, after their offsets: 4.3e9 rows."""
+    R, T = 6000, 30000
+    p = ra.make_cache_params(48, 1, 64, page_size=16, num_pages=8, max_blocks=4)
+    cache = torch.zeros(8, ra.cache_layout(p)["page_bytes"], dtype=torch.uint8, device="cuda")
+    q = torch.zeros(T, 48, 64, dtype=torch.bfloat16, device="cuda")
+    size = ra.cache_shared_workspace(p, R, 1, T, device="meta").numel()
+    o = torch.full((T + 64, 48, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    ws = torch.full((size + 4096,), 0x33, dtype=torch.uint8, device="cuda")
+    start = np.array([0, T] * (R // 2) + [0])
+    ra.cache_attn_shared(p, q, cache, i32(np.zeros((R, 4))), i32(start), i32(np.full(R, 60)), i32(np.zeros(T)), i32([0, R]),
+                         i32([20]), o[32:32 + T], ws[2048:2048 + size])
+    torch.cuda.synchronize()
+    assert (o[:32] == 7.0).all() and (o[32 + T:] == 7.0).all()
+    assert (ws[:2048] == 0x33).all() and (ws[2048 + size:] == 0x33).all()
+
+
 def test_equals_cache_attn_within_roundings(ra):
     c = _case(ra, [(12, 500)], own=100, queries=(1, 2), dt="bf16", out="fp32", rope=True, seed=6)
     x, lse = (t.clone() for t in c.run())
