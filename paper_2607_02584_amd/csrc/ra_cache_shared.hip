@@ -16,9 +16,10 @@
 // and leaves partial rows in the workspace (k_few alone where no prefix can have
 // more than 16 rows); k_join joins a row's parts, a wave per row.  Pieces of many
 // rows come first in the grid and are cut for their share of the places that the
-// card has, so that those of few run beside them from the start: 64 requests on 4
-// prefixes took 117 us with one launch after the other, 101 with the two kinds
-// alternating (whoever waits for a place ends as much later), 96 so.
+// card has, so that those of few run beside them from the start: 64 requests on a
+// prefix of 32 700 tokens took 117 us with one launch after the other, 101 with the
+// two kinds alternating (whoever waits for a place ends as much later), 96 so (now
+// 88, with Q in digits).
 //
 // Bound by HBM while a group's rows are few, by the matrix cores and the softmax
 // beside them from some 64 rows on.
