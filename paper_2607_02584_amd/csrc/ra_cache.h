@@ -148,9 +148,34 @@ __device__ __forceinline__ double lane_xor(double v) {
   return __hiloint2double(lane_xor<M>(__double2hiint(v)), lane_xor<M>(__double2loint(v)));
 }
 
-// One butterfly stage between lanes that differ in bit M.
+// x's value of the lanes with bit M and y's of those without it change places.
+template <int M>
+__device__ __forceinline__ void lane_swap(float& x, float& y) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
+  const auto z = [&] {
+    if constexpr (M == 32) return __builtin_amdgcn_permlane32_swap(u, v, false, false);
+    else return __builtin_amdgcn_permlane16_swap(u, v, false, false);
+  }();
+  x = __uint_as_float(z[0]);
+  y = __uint_as_float(z[1]);
+#endif
+}
+// One butterfly stage between lanes that differ in bit M.  Where halves of a wave or of 32 lanes are exchanged,
+// two values at a time: a lane takes both sides of one of them, and gives back what is the other's.
 template <int M, typename F, int N>
 __device__ __forceinline__ void butterfly_lanes(F (&y)[N], int lane) {
+  if constexpr (sizeof(F) == 4 && M >= 16 && N % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < N; i += 2) {
+      F a = y[i], b = y[i + 1];
+      lane_swap<M>(a, b);
+      y[i] = a + b;
+      y[i + 1] = a - b;
+      lane_swap<M>(y[i], y[i + 1]);
+    }
+    return;
+  }
   const bool up = lane & M;
 #pragma unroll
   for (int i = 0; i < N; ++i) {

@@ -1128,9 +1128,9 @@ __device__ __forceinline__ float load_q6(const CacheAttnArgs& a, const Piece& p,
     bad = __fmaf_rn(y[e], 0.0f, bad);
   }
   bad += lane_xor<32>(bad);
-  const float power = row_power(fmaxf(m, lane_xor<32>(m)));
+  const float power = row_power(fmaxf(m, lane_xor<32>(m))), unit = power * 0x1p-14f;
 #pragma unroll
-  for (int e = 0; e < N; ++e) y[e] = y[e] * power * 0x1p-14f;
+  for (int e = 0; e < N; ++e) y[e] *= unit;
   each<N / 32>([&](auto st) {
     each<kTerms>([&](auto zz) {
       constexpr int z = decltype(zz)::value, n = 32 * decltype(st)::value;
