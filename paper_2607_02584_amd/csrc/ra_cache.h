@@ -87,8 +87,10 @@ struct CacheAttnArgs {
   int rope_rows, R, T, max_q, Hq, G, max_blocks;
   int causal, window, is_fp16, out_dtype, had, vhad;
   int target, target_rows;          // pieces of work per KV head aimed at (set by the launch)
-  // first tokens that stay visible beside a window
+  // first tokens that stay visible beside a window; partial rows of few rows beside those of many
   int sinks;
+  float* few_o;
+  float2* few_ml;
   // prefixes that requests share
   int groups;
   const int* group_start;           // [groups + 1]
@@ -116,6 +118,8 @@ hipError_t launch_cache_attn_shared(const CacheAttnArgs& a, int D, void* workspa
 size_t cache_shared_bytes(int D, int Hkv, int G, int R, int groups, int T);
 // bytes of workspace that launch_cache_attn's part_o and part_ml take
 size_t cache_attn_partial_bytes(int D, int Hkv, int G, int max_q, size_t* ml_offset);
+// of cache_attn_sinks, which is not less, and where the partial rows of requests of few rows lie
+size_t cache_sinks_bytes(int D, int Hkv, int G, int max_q, size_t* ml, size_t* few_o, size_t* few_ml);
 
 // stores a library error message for rotate_attn_last_error() and returns code
 int set_error(int code, const char* msg) noexcept;

@@ -52,8 +52,8 @@ enum Keys { kAll, kSinks, kShared };
 // kFewRows a request is bound by its keys (k_few), above by the matrix cores
 // (k_rows).
 constexpr int kFewRows = 32;
-// blocks of the least part: a step of 32 keys for each of the four waves of
-// k_few, twice; for k_rows enough to pay for a partial output of M rows
+// Blocks of the least part: a step of 32 keys for each of the four waves of k_few, twice; for many rows enough
+// to pay for a partial output of M rows.
 template <int M>
 constexpr int least_blocks() { return M <= kFewRows ? 4 : 16; }
 
@@ -111,10 +111,17 @@ __device__ __forceinline__ int wave_most(int v) {
 
 // Blocks of a part, W blocks in all: at least W / target, the sum's roundings
 // (the same in every workgroup) included.
-template <int M>
+template <int M, Keys K>
 __device__ __forceinline__ unsigned part_blocks(float W, int target) {
   const float c = W * (1.0f + 0x1p-10f) / static_cast<float>(target) + 1.0f;
   const unsigned C = c < 0x1p26f ? static_cast<unsigned>(c) : 1u << 26;   // a request has 2^24 at most
+  // kSinks: parts of many rows as short as those of few while they fill a quarter of the places at most (one request of 64
+  // rows over 600 keys 31 -> 22 us).  Where they would fill all, what waits for a place loses more than they gain
+  // (30 requests of one query beside a prompt of 300 tokens 59 -> 69 us).
+  if (K == kSinks && M > kFewRows && C < static_cast<unsigned>(least_blocks<M>())) {
+    const unsigned quarter = static_cast<unsigned>(4.0f * c);
+    return quarter < 4 ? 4 : quarter < static_cast<unsigned>(least_blocks<M>()) ? quarter : least_blocks<M>();
+  }
   return C < static_cast<unsigned>(least_blocks<M>()) ? least_blocks<M>() : C;
 }
 
@@ -180,7 +187,7 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
     Request q = {};
     if (lane < a.R) q = request_of<M, K>(a, lane);
     const float W = wave_total(static_cast<float>(q.tiles) * static_cast<float>(q.blocks));
-    const int n = parts_of(q, part_blocks<M>(W, target));
+    const int n = parts_of(q, part_blocks<M, K>(W, target));
     const int split = n > 1 ? q.tiles * n : 0, mine = merge ? (n > 1 ? q.tiles : 0) : q.tiles * n;
     const int from = wave_sums(mine) - mine, slot = wave_sums(split) - split;
     const unsigned long long hit = __ballot(x >= from && x < from + mine);
@@ -207,7 +214,7 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
   }
   if (tid == 0) sh.hit[0] = -1;
   __syncthreads();
-  const unsigned C = part_blocks<M>((sh.w[0] + sh.w[1]) + (sh.w[2] + sh.w[3]), target);
+  const unsigned C = part_blocks<M, K>((sh.w[0] + sh.w[1]) + (sh.w[2] + sh.w[3]), target);
   // kSinks: pieces of long requests come first.  Windows make most of them equally long, and more of them than run at
   // once: what begins last should be short.  (256 requests of up to 4064 keys: 155 -> 143 us.)
   bool first = false;   // piece x is one of those
@@ -1686,18 +1693,18 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>&
 constexpr int kMostParts = 2048;   // 2 * target at most, one KV head
 
 template <int D, int M, Keys K>
-__device__ __forceinline__ void join_tiles(const CacheAttnArgs& a, int target, int per_group) {
+__device__ __forceinline__ void join_tiles(const CacheAttnArgs& a, int target, int per_group, int x0, int h, int z) {
   constexpr int W = D / 4, NG = 256 / W;
   __shared__ SchedShared sched;
   __shared__ float f[kMostParts];
   __shared__ float red[8];
   __shared__ __align__(16) float4 sum[NG][W];
   Piece p;
-  if (!find_piece<M, K>(a, sched, blockIdx.x, true, target, &p)) return;
+  if (!find_piece<M, K>(a, sched, x0, true, target, &p)) return;
   if (M > kFewRows && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // as k_rows numbers them
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, h = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
   int rows = p.q.ql * a.G - p.tile * M < M ? p.q.ql * a.G - p.tile * M : M;
-  const int row0 = blockIdx.z * per_group;
+  const int row0 = z * per_group;
   if (row0 + per_group < rows) rows = row0 + per_group;
   const int64_t step = static_cast<int64_t>(a.g.Hkv) * M;
   if (p.parts <= 8) {
@@ -1791,6 +1798,10 @@ Grid grid_of(const CacheAttnArgs& a, int M, int target) {
   return g;
 }
 
+Grid few_grid_of(const CacheAttnArgs& a) {   // a request of few rows is one tile
+  return {a.R, a.R < a.target ? a.R : a.target};
+}
+
 int target_of(int pieces, int Hkv) { return (pieces + Hkv - 1) / Hkv; }
 
 // ---------------------------------------------------------------- kernels --
@@ -1826,14 +1837,18 @@ __global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
 
 template <int D, int M, Keys K>
 __global__ __launch_bounds__(256) void k_merge(CacheAttnArgs a, int target, int per_group) {
-  join_tiles<D, M, K>(a, target, per_group);
+  join_tiles<D, M, K>(a, target, per_group, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
+// Rows of a tile that a workgroup of the merge takes: a workgroup per row while those are few enough to run at once.
+template <int M>
+int merged_rows(const CacheAttnArgs& a, const Grid& g, int64_t rows) {
+  return g.merges * a.g.Hkv * (rows > M ? M : rows) <= 4096 ? 1 : M > kFewRows ? 16 : 8;
+}
 template <int D, int M, Keys K>
 hipError_t merge(const CacheAttnArgs& a, const Grid& g, int target, int64_t rows, hipStream_t s) {
+  const int per_group = merged_rows<M>(a, g, rows);
   if (rows > M) rows = M;
-  // a workgroup per row while those are few enough to run at once
-  const int per_group = g.merges * a.g.Hkv * rows <= 4096 ? 1 : M > kFewRows ? 16 : 8;
   k_merge<D, M, K><<<dim3(static_cast<unsigned>(g.merges), a.g.Hkv, static_cast<unsigned>((rows + per_group - 1) / per_group)),
                   dim3(256), 0, s>>>(a, target, per_group);
   return hipGetLastError();
@@ -1842,9 +1857,7 @@ hipError_t merge(const CacheAttnArgs& a, const Grid& g, int target, int64_t rows
 template <int D, int NT, Keys K>
 hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   constexpr int M = 16 * NT;
-  Grid g;
-  g.tiles = a.R;   // a request of few rows is one tile
-  g.merges = g.tiles < a.target ? g.tiles : a.target;
+  const Grid g = few_grid_of(a);
   const dim3 grid(static_cast<unsigned>((g.tiles + a.target) * a.g.Hkv));
   if (a.out_dtype == RA_FP32) k_fine_few<D, NT, 2, K><<<grid, dim3(256), 0, s>>>(a);
   else k_few<D, NT, 2, K><<<grid, dim3(256), 0, s>>>(a);

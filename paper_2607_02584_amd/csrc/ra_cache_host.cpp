@@ -174,7 +174,7 @@ int attn_tensors(const ra_cache_params* p, int32_t R, int32_t T, const void* q, 
 int attn_args(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, const void* q, int64_t q_token_stride,
               int64_t q_head_stride, const void* cache, const int32_t* block_table, const int32_t* q_start,
               const int32_t* seq_lens, const float* rope, int32_t rope_rows, void* o, float* lse, void* workspace,
-              size_t workspace_bytes, ra::CacheAttnArgs* x) {
+              size_t workspace_bytes, bool sinks, ra::CacheAttnArgs* x) {
   int rc = validate(p);
   if (rc) return rc;
   if ((rc = check_counts(R, T))) return rc;
@@ -186,11 +186,15 @@ int attn_args(const ra_cache_params* p, int32_t R, int32_t T, int32_t max_q, con
   if ((rc = attn_tensors(p, R, T, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope, rope_rows,
                          o, lse, x)))
     return rc;
-  size_t ml;
-  const size_t need = ra::cache_attn_partial_bytes(p->D, p->Hkv, x->G, max_q, &ml);
+  size_t ml, few_o = 0, few_ml = 0;
+  const size_t need = sinks ? ra::cache_sinks_bytes(p->D, p->Hkv, x->G, max_q, &ml, &few_o, &few_ml)
+                            : ra::cache_attn_partial_bytes(p->D, p->Hkv, x->G, max_q, &ml);
   if ((rc = check_workspace(workspace, workspace_bytes, need))) return rc;
-  x->part_o = static_cast<float*>(workspace);
-  x->part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ml);
+  char* ws = static_cast<char*>(workspace);
+  x->part_o = reinterpret_cast<float*>(ws);
+  x->part_ml = reinterpret_cast<float2*>(ws + ml);
+  x->few_o = reinterpret_cast<float*>(ws + few_o);
+  x->few_ml = reinterpret_cast<float2*>(ws + few_ml);
   x->max_q = max_q;
   return RA_OK;
 }
@@ -298,8 +302,8 @@ int rotate_attn_cache_workspace_size(const ra_cache_params* p, int32_t R, int32_
   if ((rc = check_pieces(p, R, T))) return rc;
   if (max_q < 0) return set_error(RA_ERR_INVALID, "max_q must be >= 0");
   if (!bytes) return set_error(RA_ERR_INVALID, "bytes is NULL");
-  size_t ml;
-  *bytes = ra::cache_attn_partial_bytes(p->D, p->Hkv, p->Hq / p->Hkv, max_q, &ml);
+  size_t ml, few_o, few_ml;
+  *bytes = ra::cache_sinks_bytes(p->D, p->Hkv, p->Hq / p->Hkv, max_q, &ml, &few_o, &few_ml);
   return RA_OK;
 }
 
@@ -398,7 +402,7 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
                            size_t workspace_bytes, void* stream) {
   ra::CacheAttnArgs a;
   const int rc = attn_args(p, R, T, max_q, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope,
-                           rope_rows, o, lse, workspace, workspace_bytes, &a);
+                           rope_rows, o, lse, workspace, workspace_bytes, false, &a);
   if (rc || a.T == 0) return rc;
   return hip_status(ra::launch_cache_attn(a, p->D, static_cast<hipStream_t>(stream)), "cache_attn");
 }
@@ -413,7 +417,7 @@ int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_
   if (sinks > (1 << 30)) return set_error(RA_ERR_UNSUPPORTED, "sinks must not exceed 2^30");
   ra::CacheAttnArgs a;
   const int rc = attn_args(p, R, T, max_q, q, q_token_stride, q_head_stride, cache, block_table, q_start, seq_lens, rope,
-                           rope_rows, o, lse, workspace, workspace_bytes, &a);
+                           rope_rows, o, lse, workspace, workspace_bytes, true, &a);
   if (rc || a.T == 0) return rc;
   a.sinks = sinks;
   return hip_status(ra::launch_cache_attn_sinks(a, p->D, static_cast<hipStream_t>(stream)), "cache_attn_sinks");

@@ -98,7 +98,9 @@ __device__ __forceinline__ Request shared_request(const CacheAttnArgs& a, const 
 constexpr int kPlan = 512;
 constexpr int kKnown = 4096;      // prefixes and requests whose tiles and blocks are kept in LDS
 constexpr int kRounds = 2;
-constexpr int kLeast[2] = {4, 16};    // blocks of a part at least: few, many rows
+// blocks of a part at least, of few and many rows (the latter with 16: 8 requests on 1000 tokens 45 us, with 4 25, with 2
+// 25 too, but calls of many parts slower, whose joins then take longer)
+constexpr int kLeast[2] = {4, 4};
 constexpr int kFixed[2] = {10, 6};
 constexpr float kFewCost = 0.3f;      // of a block of keys for few rows, in blocks for many
 // workgroups of four waves that run at once: two on a compute unit, by registers and LDS

@@ -24,7 +24,7 @@ def _packed_too_near(body):
 
 
 @needs_hipcc
-@pytest.mark.parametrize("name,kinds", [("ra_cache_sinks.hip", {"k_few": 4, "k_fine_few": 4, "k_rows": 8, "k_fine_rows": 4}),
+@pytest.mark.parametrize("name,kinds", [("ra_cache_sinks.hip", {"k_few": 4, "k_fine_few": 4, "k_rows": 8, "k_fine_rows": 4, "k_both": 12}),
                                         ("ra_cache_shared.hip", {"k_few": 2, "k_fine_few": 2, "k_both": 12})])
 def test_no_product_is_used_too_early(tmp_path, name, kinds):
     kernels = _kernels(os.path.join(CSRC, name), tmp_path / "k.s")

@@ -163,6 +163,24 @@ def test_queries_far_from_one(ra, power):
         c.check(_many(c))
 
 
+@pytest.mark.parametrize("Hq,Hkv,out", [(8, 2, "bf16"), (6, 6, "fp32"), (20, 1, "fp16"), (40, 1, "bf16")])
+def test_few_and_many_rows_split_in_one_call(ra, Hq, Hkv, out):
+    """Parts of both kinds of requests lie beside each other in a workspace of just the size."""
+    qs = [1, 70, 2, 1, 150]
+    c = Case(ra, Hq, Hkv, 128, 32, [9000, 4000, 5000, 20, 160], qs, out=out, window=3500, sinks=70, seed=Hq, rope=True)
+    c.run()
+    c.check(True)
+    x, lse = c.o.clone(), c.lse.clone()
+    size = ra.cache_workspace_size(c.p, len(qs), c.T, max(qs))
+    ws = torch.full((size + 4096,), 0xFF, dtype=torch.uint8, device="cuda")
+    c.fresh()
+    ra.cache_attn_sinks(c.p, 70, c.q, torch.from_numpy(c.cache).cuda(), i32(c.table), i32(c.start), i32(c.lens), max(qs), c.o,
+                        ws[2048:2048 + size], lse=c.lse, rope=c.rope())
+    torch.cuda.synchronize()
+    assert torch.equal(x, c.o) and torch.equal(lse, c.lse)
+    assert (ws[:2048] == 0xFF).all() and (ws[2048 + size:] == 0xFF).all()
+
+
 def test_repeats_and_streams(ra):
     c = Case(ra, 8, 2, 128, 32, [5000, 300, 4000], [1, 40, 2], rope=True, had=True, window=1000, sinks=40, seed=30)
     x, lse = (t.clone() for t in c.run())
