@@ -1867,9 +1867,9 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
 
 // How many bf16 values hold P times V's scale for many rows: as many as the output shows.  For bf16 outputs one leaves
 // as much error as their own rounding does, sqrt(2) of it in all.  The errors of a scale group are one error, so over
-// few rows with few keys the mean can be a good deal more than that; there the new operators take two, which costs a
-// tenth (8 queries of 32 heads over 600 keys 33.2 us with one and 36.8 with two; 8 requests over a prefix of 30 000
-// 49.2 and 54.9 us).  At 512 rows 2048 group errors are averaged, and one value's error is sqrt(2) within 2 percent.
+// few rows with few keys the mean can be a good deal more than that; there cache_attn_sinks and cache_attn_shared take two, which
+// costs a twentieth (8 queries of 32 heads over 600 keys 21.2 us with one and 22.1 with two; 8 requests over a prefix of
+// 30 000 40.8 and 43.5 us).  At 512 rows 2048 group errors are averaged, and one value's error is sqrt(2) within 2 percent.
 constexpr int64_t kTwoTerms = 512;   // rows of all heads up to which
 template <Keys K>
 int terms_of(const CacheAttnArgs& a) {
