@@ -437,7 +437,8 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
  * (without a window, or with sinks = 0, what cache_attn sees; causal only).  Pages
  * between the two are not read, and their table entries may be -1
  * (cache_trim).  Arguments, workspace and limits are those of cache_attn; so is the
- * precision of o (one bf16 value only from T * Hq > 512 on), and lse is as exact as
+ * precision of o (one bf16 value only for requests of more than 512 rows, queries times Hq,
+ * whatever else is in the call), and lse is as exact as
  * binary32 arithmetic whatever the type of o; elements of a query are held to within
  * 2^-24 of its largest. */
 int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_t R, int32_t T, int32_t max_q,
@@ -459,9 +460,9 @@ int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_
  * fit touch nothing outside the tensors and the workspace.
  * Limits: 2 * (R + groups) * Hkv + T * Hq / 64 must stay below 2^24 - 4096, T must not exceed
  * 2^22, nor T * Hq 2^26.
- * Precision: o as cache_attn's (with bf16 outputs and T * Hq > 512 weights times V's
- * scales are one bf16 value, 2^-8, where a prefix, or a request's own keys, have more
- * than 16 rows: queries times Hq / Hkv, a prefix having those of its whole group); lse is
+ * Precision: o as cache_attn's (with bf16 outputs weights times V's scales are one bf16
+ * value, 2^-8, for requests of more than 512 rows, queries times Hq; over a prefix only where
+ * all requests of its group that have queries are such ones, two values otherwise); lse is
  * as exact as binary32 arithmetic whatever the type of o; elements of a query are held to
  * within 2^-24 of its largest.
  * Workspace: cache_shared_workspace_size bytes (partial outputs of every row, twice, and

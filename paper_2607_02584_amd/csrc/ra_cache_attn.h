@@ -128,7 +128,16 @@ __device__ __forceinline__ unsigned part_blocks(float W, int target) {
 struct Piece {
   Request q;
   int r, tile, part, parts, slot;   // slot: place in the workspace of part 0 of this tile (kShared: of the request, in rows)
+  bool two;                         // kSinks, kShared: of no more than kTwoTerms rows
 };
+
+// How many bf16 values hold P times V's scale in a piece of many rows: as many as the output shows, so three for binary32
+// and two for binary16 outputs.  For bf16 ones one leaves as much error as their own rounding does (2.3e-3 of both, 1.65e-3
+// of the latter) and saves a quarter of the time where the matrix cores bind, as they do in requests of many rows (prompts
+// under a window 448 us with one value, 565 with two).  cache_attn_sinks and cache_attn_shared take it there only: a
+// request's own rows (queries * Hq) decide, whatever else the call holds or has room for, and for a prefix the least of its
+// requests'.  (A decode step of 64 requests over a prefix of 32 700 tokens 88 us with one value, 98 with two.)
+constexpr int kTwoTerms = 512;   // rows of all heads up to which there are two
 
 struct SchedShared {
   float w[4];
@@ -182,6 +191,7 @@ __device__ __forceinline__ bool find_piece(const CacheAttnArgs& a, SchedShared& 
     out->slot = slot + out->tile * n;
     out->q.lo = 0;
     out->q.table = r;
+    out->two = K == kSinks && q.ql * a.Hq <= kTwoTerms;
   };
   if (a.R <= 64) {
     Request q = {};
@@ -360,7 +370,7 @@ __device__ __forceinline__ int row_position(const CacheAttnArgs& a, const Piece&
   if (p.r >= a.groups) return p.q.first + row / a.G;
   return row < p.q.ql * a.G ? a.positions[p.q.q0 + row / a.G] : 0x3fffffff;
 }
-// Piece x of the list for few (0) or many (1) rows: {request, tile, part, parts}; of a request {q0, ql, n, first}, {lo, table, slot}.
+// Piece x of the list for few (0) or many (1) rows: {request, tile, part, parts}; of a request {q0, ql, n, first}, {lo, table, slot, two}.
 template <int MANY>
 __device__ __forceinline__ bool listed_piece(const CacheAttnArgs& a, int x, Piece* out) {
   if (x >= __builtin_amdgcn_readfirstlane(a.counts[MANY])) return false;
@@ -378,6 +388,7 @@ __device__ __forceinline__ bool listed_piece(const CacheAttnArgs& a, int x, Piec
   out->q.lo = all(v.x);
   out->q.table = all(v.y);
   out->slot = all(v.z);
+  out->two = all(v.w);
   out->q.tiles = out->q.blocks = 0;
   return true;
 }
@@ -1176,9 +1187,9 @@ struct RowsLds {
   SchedShared sched;
 };
 
-// Piece x0 of KV head h.
+// Piece p of KV head h.
 template <int D, bool F16, int TERMS, Keys K>
-__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>& buf, int x0, int h) {
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>& buf, Piece p, int h) {
   constexpr bool SIX = K != kAll;          // Q as digits, K as it lies in the page
   constexpr bool QF = TERMS == 3 || SIX;   // scores are multiplied by `back`
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
@@ -1186,8 +1197,6 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>&
   typedef typename RowsLds<D, K>::Scales Scales;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
-  Piece p;
-  if (!take_piece<M, K>(a, buf.sched, x0, a.target_rows, &p)) return;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
   if (K != kShared && a.causal) p.tile = p.q.tiles - 1 - p.tile;   // the longest first
 
@@ -1687,6 +1696,16 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>&
   if (a.lse && hh == 0) a.lse[out] = l == 0.0f ? kNegInf : (m + log2f(l)) * kLn2;
 }
 
+// Piece x0 of KV head h.  TERMS 1: two for requests of few enough rows.
+template <int D, bool F16, int TERMS, Keys K>
+__device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, RowsLds<D, K>& buf, int x0, int h) {
+  Piece p;
+  if (!take_piece<128, K>(a, buf.sched, x0, a.target_rows, &p)) return;
+  if constexpr (K != kAll && TERMS == 1)
+    if (p.two) return many_rows<D, F16, 2, K>(a, buf, p, h);
+  many_rows<D, F16, TERMS, K>(a, buf, p, h);
+}
+
 // Joins the parts of split tiles, a workgroup for per_group rows: up to eight
 // parts a wave per row, else one row after the other, the parts' weights first,
 // then the sum of their outputs, eight at a time (D / 4 threads each).
@@ -1826,13 +1845,13 @@ template <int D, bool F16, bool LO, Keys K>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
   __shared__ RowsLds<D, K> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
-  many_rows<D, F16, LO ? 2 : 1, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
+  rows_piece<D, F16, LO ? 2 : 1, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, bool F16, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
   __shared__ RowsLds<D, K> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
-  many_rows<D, F16, 3, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
+  rows_piece<D, F16, 3, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 
 template <int D, int M, Keys K>
@@ -1865,23 +1884,14 @@ hipError_t few(const CacheAttnArgs& a, hipStream_t s) {
   return e != hipSuccess ? e : merge<D, M, K>(a, g, a.target, static_cast<int64_t>(a.max_q) * a.G, s);
 }
 
-// How many bf16 values hold P times V's scale for many rows: as many as the output shows.  For bf16 outputs one leaves
-// as much error as their own rounding does, sqrt(2) of it in all.  The errors of a scale group are one error, so over
-// few rows with few keys the mean can be a good deal more than that; there cache_attn_sinks and cache_attn_shared take two, which
-// costs a twentieth (8 queries of 32 heads over 600 keys 21.2 us with one and 22.1 with two; 8 requests over a prefix of
-// 30 000 40.8 and 43.5 us).  At 512 rows 2048 group errors are averaged, and one value's error is sqrt(2) within 2 percent.
-constexpr int64_t kTwoTerms = 512;   // rows of all heads up to which
-template <Keys K>
-int terms_of(const CacheAttnArgs& a) {
-  if (a.out_dtype == RA_FP32) return 3;
-  return a.out_dtype == RA_FP16 || (K != kAll && static_cast<int64_t>(a.T) * a.Hq <= kTwoTerms) ? 2 : 1;
-}
+// Of a launch; with 1 its pieces of few enough rows take two (kTwoTerms).
+int terms_of(const CacheAttnArgs& a) { return a.out_dtype == RA_FP32 ? 3 : a.out_dtype == RA_FP16 ? 2 : 1; }
 
 template <int D, bool F16, Keys K>
 hipError_t rows(const CacheAttnArgs& a, hipStream_t s) {
   const Grid g = grid_of(a, kRowTile, a.target_rows);
   const dim3 grid(static_cast<unsigned>((g.tiles + a.target_rows) * a.g.Hkv));
-  const int terms = terms_of<K>(a);
+  const int terms = terms_of(a);
   if (terms == 3) k_fine_rows<D, F16, K><<<grid, dim3(256), 0, s>>>(a);
   else if (terms == 2) k_rows<D, F16, true, K><<<grid, dim3(256), 0, s>>>(a);
   else k_rows<D, F16, false, K><<<grid, dim3(256), 0, s>>>(a);

@@ -57,10 +57,10 @@ __device__ __forceinline__ int prefix_of(const CacheAttnArgs& a, const Lengths& 
   return n < 0 ? 0 : n > most ? most : n;
 }
 
-// Prefix or request v.  Whatever the device holds, nothing outside the tensors is touched.
-__device__ __forceinline__ Request shared_request(const CacheAttnArgs& a, const Lengths& l, int v) {
+// Prefix or request v, and its group (-1: none).  Whatever the device holds, nothing outside the tensors is touched.
+__device__ __forceinline__ Request shared_request(const CacheAttnArgs& a, const Lengths& l, int v, int& g) {
   Request x;
-  const int g = v < a.groups ? v : group_of(a, l, v - a.groups);
+  g = v < a.groups ? v : group_of(a, l, v - a.groups);
   const int prefix = g < 0 ? 0 : prefix_of(a, l, g);
   int r0 = v - a.groups, r1 = r0 + 1;
   if (v < a.groups) {
@@ -110,6 +110,7 @@ __host__ __device__ constexpr int places_of(int Hkv) { return kPlaces > Hkv ? kP
 struct PlanShared {
   int blocks[kKnown];
   int tiles[kKnown];             // of few rows as they are, of many negative
+  uint8_t two[kKnown];           // groups with a request of few rows (kTwoTerms; those behind are taken for such)
   int lengths[4 * kPlan + 2];    // where they are no more than kPlan each
   int from[2][kPlan];            // first piece of each, of few and of many rows
   int parts[kPlan];
@@ -125,6 +126,8 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   constexpr int NW = kPlan / 64;
   // the lengths with one load each, as finding a request's group and prefix takes one after the other
   Lengths l = {a.group_start, a.prefix_lens, a.q_start, a.seq_lens};
+  const int marked = a.groups < kKnown ? a.groups : kKnown;
+  for (int i = tid; i < marked; i += kPlan) sh.two[i] = 0;
   if (a.R <= kPlan && a.groups <= kPlan) {
     int* x = sh.lengths;
     if (tid <= a.groups && a.groups) x[tid] = a.group_start[tid];
@@ -135,9 +138,9 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       if (a.groups == kPlan) x[kPlan] = a.group_start[kPlan];
       if (a.R == kPlan) x[3 * kPlan + 1] = a.q_start[kPlan];
     }
-    __syncthreads();
     l = {x, x + kPlan + 1, x + 2 * kPlan + 1, x + 3 * kPlan + 2};
   }
+  __syncthreads();
   // what there is: blocks of all tiles, the longest, tiles
   float W[2] = {0.0f, 0.0f};
   int count[2] = {0, 0}, longest[2] = {0, 0}, finest[2] = {0, 0};   // finest: pieces of kLeast blocks
@@ -145,8 +148,10 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   Request mine = {};
 #pragma unroll 1
   for (int v = tid; v < N; v += kPlan) {
-    const Request q = shared_request(a, l, v);
+    int g;
+    const Request q = shared_request(a, l, v, g);
     if (v == tid) mine = q;
+    if (v >= a.groups && static_cast<unsigned>(g) < static_cast<unsigned>(marked) && q.ql > 0 && q.ql * a.Hq <= kTwoTerms) sh.two[g] = 1;
     const int many = q.ql * a.G > kFewShared;
     queries = queries + q.ql < 1 << 24 ? queries + q.ql : 1 << 24;
     if (v < kKnown) {
@@ -303,7 +308,8 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   for (int v0 = 0; v0 < N; v0 += kPlan) {
     const int v = v0 + tid;
     Request q = {};
-    if (v < N) q = v0 == 0 ? mine : shared_request(a, l, v);
+    int g;
+    if (v < N) q = v0 == 0 ? mine : shared_request(a, l, v, g);
     const int many = q.ql * a.G > kFewShared;
     const unsigned c = many ? C[1] : C[0];
     const int parts = q.tiles && fits ? (q.blocks ? static_cast<int>((q.blocks + c - 1) / c) : 1) : 0;
@@ -351,7 +357,8 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     if (v >= N) continue;
     const int base = many ? from[3] : from[2];
     a.requests[2 * v] = make_int4(q.q0, q.ql, q.n, q.first);
-    a.requests[2 * v + 1] = make_int4(q.lo, q.table, base, 0);
+    const int two = v >= a.groups ? q.ql * a.Hq <= kTwoTerms : v < marked ? sh.two[v] : 1;
+    a.requests[2 * v + 1] = make_int4(q.lo, q.table, base, two);
     a.info[v] = make_int2(base, many ? -parts : parts);
   }
   if (tid < 2) {
@@ -480,7 +487,7 @@ __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a) {
     RowsLds<D, kShared> rows;
   } lds;
   const int x = blockIdx.x / a.g.Hkv, h = blockIdx.x - x * a.g.Hkv, many = __builtin_amdgcn_readfirstlane(a.counts[1]);
-  if (x < many) many_rows<D, F16, TERMS, kShared>(a, lds.rows, x, h);
+  if (x < many) rows_piece<D, F16, TERMS, kShared>(a, lds.rows, x, h);
   else few_rows<D, 1, 2, FINE, kShared>(a, lds.few, x - many, h);
 }
 
@@ -563,7 +570,7 @@ hipError_t shared_d(const CacheAttnArgs& a, hipStream_t s) {
     if (a.out_dtype == RA_FP32) k_fine_few<D, 1, 2, kShared><<<grid, dim3(256), 0, s>>>(a);
     else k_few<D, 1, 2, kShared><<<grid, dim3(256), 0, s>>>(a);
   } else {
-    const int terms = terms_of<kShared>(a);
+    const int terms = terms_of(a);
     auto go = [&](auto f16) {
       constexpr bool F16 = decltype(f16)::value;
       if (terms == 3) k_both<D, F16, 3><<<grid, dim3(256), 0, s>>>(a);

@@ -32,7 +32,7 @@ __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a, int rows) {
   } lds;
   const bool many = static_cast<int>(blockIdx.x) < rows;
   const int x = many ? blockIdx.x : blockIdx.x - rows, x0 = x / a.g.Hkv, h = x - x0 * a.g.Hkv;
-  if (many) return many_rows<D, F16, TERMS, kSinks>(a, lds.rows, x0, h);
+  if (many) return rows_piece<D, F16, TERMS, kSinks>(a, lds.rows, x0, h);
   few_parts(a);
   few_rows<D, 2, 2, FINE, kSinks>(a, lds.few, x0, h);
 }
@@ -55,7 +55,7 @@ hipError_t both(const CacheAttnArgs& a, hipStream_t s) {
   const Grid g[2] = {grid_of(a, kRowTile, a.target_rows), few_grid_of(a)};
   const int64_t rows = (g[0].tiles + a.target_rows) * a.g.Hkv, all = rows + (g[1].tiles + a.target) * a.g.Hkv;
   const dim3 grid(static_cast<unsigned>(all));
-  const int terms = terms_of<kSinks>(a);
+  const int terms = terms_of(a);
   if (terms == 3) k_both<D, F16, 3><<<grid, dim3(256), 0, s>>>(a, static_cast<int>(rows));
   else if (terms == 2) k_both<D, F16, 2><<<grid, dim3(256), 0, s>>>(a, static_cast<int>(rows));
   else k_both<D, F16, 1><<<grid, dim3(256), 0, s>>>(a, static_cast<int>(rows));
