@@ -513,7 +513,10 @@ int rotate_attn_cache_pages_workspace_size(const ra_cache_params* p, int32_t R, 
  * which holds no tokens, gets the first L tokens of request parents[i], L = lens[i]
  * (lens may be NULL: all of them).  Full pages are shared: the child's table names them and
  * they have one holder more.  Where L does not end with a page, the page it ends in
- * is copied into one from the top of the stack, in order of the pairs.  A child is named
+ * is copied into one from the top of the stack, in order of the pairs.  Entries of the parent
+ * that are no page are none in the child either: full ones are the parent's, and where L ends in
+ * one no page is taken and the child has -1 there (what it appends up to the next page then
+ * finds no slot: a child that is to go on begins where its parent has a page).  A child is named
  * once; parents may be named often, and are as they were before the call (a parent that is a child
  * of the same call has no tokens).  Entries of a child behind its pages keep what they
  * held.  status[1]: pages taken, [2]: entries that share a page, [3]: the longest request. */

@@ -117,9 +117,11 @@ __host__ __device__ __forceinline__ int pieces_of(const PageTables& t) {
 // Pair i makes request `child` begin with the first L tokens of `parent`: its
 // first L / P entries are the parent's, whose pages have one holder more, and
 // where L % P tokens are left a page from the stack gets the bytes of the page
-// that holds them, so that the page a request appends to is never shared.
+// that holds them, so that the page a request appends to is never shared.  Where
+// that entry is no page (a window lost it) there is nothing to copy, and a page of
+// leftover bytes would be seen: none is taken, and the child's entry is -1.
 //
-// Workspace: L [n], {page copied or -1, its copy} [n].
+// Workspace: L [n], {page copied or -1, its copy or -1} [n].
 
 __global__ __launch_bounds__(kPlan) void k_fork_plan(ForkArgs a) {
   const PageTables& t = a.t;
@@ -142,7 +144,12 @@ __global__ __launch_bounds__(kPlan) void k_fork_plan(ForkArgs a) {
     const bool twice = atomicOr(&seen[c >> 5], 1u << (c & 31)) >> (c & 31) & 1;
     if (twice || t.seq_in[c] != 0 || has < 0 || has > most || L < 0 || L > has) flags = 1;
     len[i] = L;
-    need += L & (t.page - 1) ? 1 : 0;
+    int from = -1;
+    if (L & (t.page - 1) && L > 0 && L <= has && has <= most)
+      from = t.table_in[static_cast<int64_t>(p) * t.max_blocks + (L >> t.page_log)];
+    from = is_page(from, t) ? from : -1;
+    copy[i].x = from;
+    need += from >= 0;
   }
   for (int r = tid; r < t.R; r += kPlan) {
     const int n = t.seq_in[r];
@@ -161,18 +168,10 @@ __global__ __launch_bounds__(kPlan) void k_fork_plan(ForkArgs a) {
     int carry = 0;
     for (int i0 = 0; i0 < a.n; i0 += kPlan) {
       const int i = i0 + tid;
-      const int L = i < a.n ? len[i] : 0;
-      const int part = L & (t.page - 1) ? 1 : 0;
+      const int from = i < a.n ? copy[i].x : -1;   // (this thread's own)
       int all;
-      const int at = carry + block_scan<kPlan>(part, wave, &all);
-      if (i < a.n) {
-        int2 x = make_int2(-1, -1);
-        if (part) {
-          x.x = t.table_in[static_cast<int64_t>(a.parents[i]) * t.max_blocks + (L >> t.page_log)];
-          x.y = t.free_in[count - 1 - at];
-        }
-        copy[i] = x;
-      }
+      const int at = carry + block_scan<kPlan>(from >= 0, wave, &all);
+      if (i < a.n) copy[i].y = from >= 0 ? t.free_in[count - 1 - at] : -1;
       carry += all;
     }
     __syncthreads();   // lengths of parents were read before, those of children are written now
