@@ -24,6 +24,7 @@
 // Bound by HBM while a group's rows are few, by the matrix cores and the softmax
 // beside them from some 64 rows on.
 #include "ra_cache_attn.h"
+#include "ra_cache_cut.h"
 
 namespace ra {
 namespace {
@@ -114,8 +115,8 @@ struct PlanShared {
   int lengths[4 * kPlan + 2];    // where they are no more than kPlan each
   int from[2][kPlan];            // first piece of each, of few and of many rows
   int parts[kPlan];
-  float w[kPlan / 64][2];
-  int n[kPlan / 64][7];
+  float w[kPlan / 64][4];
+  int n[kPlan / 64][5];
   unsigned lo[2][kRounds], hi[2][kRounds];
   int fits[2][4 * (kPlan / 64)], wide[3][2 * kRounds];
 };
@@ -142,8 +143,8 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
   }
   __syncthreads();
   // what there is: blocks of all tiles, the longest, tiles
-  float W[2] = {0.0f, 0.0f};
-  int count[2] = {0, 0}, longest[2] = {0, 0}, finest[2] = {0, 0};   // finest: pieces of kLeast blocks
+  float W[2] = {0.0f, 0.0f}, finest[2] = {0.0f, 0.0f};   // finest: pieces of kLeast blocks
+  int count[2] = {0, 0}, longest[2] = {0, 0};
   int queries = 0;   // of prefixes and requests, no more than 2 T where offsets and groups ascend
   Request mine = {};
 #pragma unroll 1
@@ -164,7 +165,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       W[k] += on ? static_cast<float>(q.tiles) * static_cast<float>(q.blocks) : 0.0f;
       count[k] += on ? q.tiles : 0;
       longest[k] = on && q.blocks > longest[k] ? q.blocks : longest[k];
-      finest[k] += on ? q.tiles * ((q.blocks + kLeast[k] - 1) / kLeast[k]) : 0;
+      finest[k] += on ? cut_finest(q.tiles, q.blocks, kLeast[k]) : 0.0f;
     }
   }
 #pragma unroll
@@ -172,7 +173,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     W[k] = wave_total(W[k]);
     count[k] = __builtin_amdgcn_readlane(wave_sums(count[k]), 63);
     longest[k] = wave_most(longest[k]);
-    finest[k] = __builtin_amdgcn_readlane(wave_sums(finest[k]), 63);
+    finest[k] = wave_total(finest[k]);
   }
   if (lane == 0)
 #pragma unroll
@@ -180,18 +181,18 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       sh.w[w][k] = W[k];
       sh.n[w][k] = count[k];
       sh.n[w][2 + k] = longest[k];
-      sh.n[w][4 + k] = finest[k];
+      sh.w[w][2 + k] = finest[k];
     }
   queries = __builtin_amdgcn_readlane(wave_sums(queries), 63);
-  if (lane == 0) sh.n[w][6] = queries < 1 << 24 ? queries : 1 << 24;
+  if (lane == 0) sh.n[w][4] = queries < 1 << 24 ? queries : 1 << 24;
   __syncthreads();
   queries = 0;
 #pragma unroll
-  for (int i = 0; i < NW; ++i) queries += sh.n[i][6];
+  for (int i = 0; i < NW; ++i) queries += sh.n[i][4];
   // (what does not fit the call has no pieces: their numbers would pass 32 bits)
   const bool fits = queries <= 2 * a.T;
-  W[0] = W[1] = 0.0f;
-  count[0] = count[1] = longest[0] = longest[1] = finest[0] = finest[1] = 0;
+  W[0] = W[1] = finest[0] = finest[1] = 0.0f;
+  count[0] = count[1] = longest[0] = longest[1] = 0;
 #pragma unroll
   for (int i = 0; i < NW; ++i)
 #pragma unroll
@@ -199,7 +200,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
       W[k] += sh.w[i][k];
       count[k] += sh.n[i][k];
       longest[k] = sh.n[i][2 + k] > longest[k] ? sh.n[i][2 + k] : longest[k];
-      finest[k] += sh.n[i][4 + k];
+      finest[k] += sh.w[i][2 + k];
     }
   // either kind's share of the places
   int places_for[2];
@@ -213,26 +214,17 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     places_for[0] = count[1] && all > n ? all - n : all;
   }
   // Blocks of a part.
-  auto most = [](float x) { return x < 0x1p26f ? static_cast<unsigned>(x) : 1u << 26; };   // a request has 2^24 at most
   unsigned C[2];
-  if (finest[0] <= places_for[0] && finest[1] <= places_for[1]) {
+  if (finest[0] <= static_cast<float>(places_for[0]) && finest[1] <= static_cast<float>(places_for[1])) {
     C[0] = kLeast[0];
     C[1] = kLeast[1];
   } else if (N <= kKnown) {
-    // (at `hi` every tile is a small piece, or the tiles' last parts fill what is left of the places)
     if (tid < 2 * kRounds) {
       const int k = tid / kRounds, r = tid % kRounds;
-      const float places = static_cast<float>((r + 1) * (k ? places_for[1] : places_for[0]));
-      const unsigned lo = most((k ? W[1] : W[0]) / places), one = 2 * (k ? longest[1] : longest[0]) + 2;
-      const unsigned all = most(((k ? W[1] : W[0]) + static_cast<float>(kFixed[k]) * static_cast<float>(k ? count[1] : count[0])) / places) + 2;
-      sh.lo[k][r] = lo < static_cast<unsigned>(kLeast[k]) ? kLeast[k] : lo;
-      unsigned hi = one > all ? one : all;
-      const float left = places - static_cast<float>(k ? count[1] : count[0]);
-      if (left >= 1.0f) {
-        const unsigned even = most((k ? W[1] : W[0]) / left) + 1;
-        hi = even < hi ? even : hi;
-      }
-      sh.hi[k][r] = hi > static_cast<unsigned>(kLeast[k]) ? hi : kLeast[k];
+      const CutRange x = cut_range(k ? W[1] : W[0], k ? count[1] : count[0], k ? longest[1] : longest[0],
+                                   static_cast<float>((r + 1) * (k ? places_for[1] : places_for[0])), static_cast<float>(kFixed[k]), kLeast[k]);
+      sh.lo[k][r] = x.lo;
+      sh.hi[k][r] = x.hi;
     }
     __syncthreads();
     // kernel, rounds, and which four of eight values
@@ -256,7 +248,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
         if (t <= 0) continue;
         // (binary32: at the edge a part more or less is of no matter)
 #pragma unroll
-        for (int z = 0; z < NZ; ++z) sum[z] += static_cast<float>(t) * (b > 0.5f * fc[z] ? ceilf(b * inv[z]) : (b + fixed) * per[z]);
+        for (int z = 0; z < NZ; ++z) sum[z] += static_cast<float>(t) * cut_weight(b, fc[z], inv[z], fixed, per[z]);
       }
 #pragma unroll
       for (int z = 0; z < NZ; ++z) {
@@ -298,10 +290,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     }
   } else {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const unsigned c = most(W[i] / static_cast<float>(kRounds * places_for[i])) + 1;
-      C[i] = c < static_cast<unsigned>(kLeast[i]) ? kLeast[i] : c;
-    }
+    for (int i = 0; i < 2; ++i) C[i] = cut_closed(W[i], static_cast<float>(kRounds * places_for[i]), kLeast[i]);
   }
   // pieces and places in the workspace, in order
   int carry[4] = {0, 0, 0, 0};   // pieces and rows of parts, of few and many rows
@@ -312,7 +301,7 @@ __device__ void plan_pieces(const CacheAttnArgs& a) {
     if (v < N) q = v0 == 0 ? mine : shared_request(a, l, v, g);
     const int many = q.ql * a.G > kFewShared;
     const unsigned c = many ? C[1] : C[0];
-    const int parts = q.tiles && fits ? (q.blocks ? static_cast<int>((q.blocks + c - 1) / c) : 1) : 0;
+    const int parts = q.tiles && fits ? cut_parts(q.blocks, c) : 0;
     const int val[4] = {many ? 0 : q.tiles * parts, many ? q.tiles * parts : 0, many ? 0 : q.ql * a.G * parts,
                         many ? q.ql * a.G * parts : 0};
     int from[4];
