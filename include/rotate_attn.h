@@ -438,9 +438,11 @@ int rotate_attn_cache_attn(const ra_cache_params* p, int32_t R, int32_t T, int32
  * between the two are not read, and their table entries may be -1
  * (cache_trim).  Arguments, workspace and limits are those of cache_attn; so is the
  * precision of o (one bf16 value only for requests of more than 512 rows, queries times Hq,
- * whatever else is in the call), and lse is as exact as
- * binary32 arithmetic whatever the type of o; elements of a query are held to within
- * 2^-24 of its largest. */
+ * whatever else is in the call).  lse is that of binary32 arithmetic whatever the type of o, on
+ * elements of the query (after RoPE, rotation and scale) that are held to within 2^-23 of
+ * themselves, or 2^-39 of the row's largest; with a rotation, which gives every element a part of
+ * every channel, requests of more than 32 rows (queries times Hq / Hkv) hold them to within
+ * 2^-24 of the row's largest.  (Of rows whose largest is below 2^-106, read 2^-106 for it.) */
 int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_t R, int32_t T, int32_t max_q,
                                  const void* q, int64_t q_token_stride, int64_t q_head_stride, const void* cache,
                                  const int32_t* block_table, const int32_t* q_start, const int32_t* seq_lens,
@@ -462,9 +464,10 @@ int rotate_attn_cache_attn_sinks(const ra_cache_params* p, int32_t sinks, int32_
  * 2^22, nor T * Hq 2^26.
  * Precision: o as cache_attn's (with bf16 outputs weights times V's scales are one bf16
  * value, 2^-8, for requests of more than 512 rows, queries times Hq; over a prefix only where
- * all requests of its group that have queries are such ones, two values otherwise); lse is
- * as exact as binary32 arithmetic whatever the type of o; elements of a query are held to
- * within 2^-24 of its largest.
+ * all requests of its group that have queries are such ones, two values otherwise); lse, and
+ * the elements of a query, as cache_attn_sinks' (with a rotation to within 2^-24 of the row's
+ * largest where a prefix, or a request's own keys, have more than 16 rows: queries times Hq / Hkv,
+ * a prefix having those of its whole group).
  * Workspace: cache_shared_workspace_size bytes (partial outputs of every row, twice, and
  * Q: about T Hq (15.75 D + 16), and 147 456 rows of (4 D + 8) for cuts), 256-byte
  * aligned; its contents do not matter before or after. */

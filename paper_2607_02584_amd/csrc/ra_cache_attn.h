@@ -397,13 +397,19 @@ __device__ __forceinline__ bool take_piece(const CacheAttnArgs& a, SchedShared& 
   if constexpr (K == kShared) return listed_piece<(M > kFewRows)>(a, x, out);
   else return find_piece<M, K>(a, sh, x, false, target, out);
 }
-// Q of cache_attn_sinks and cache_attn_shared for many rows: a row, scaled by a power of two so that its largest element is in
-// [1, 2), as the sum of kTerms digits to the base 32, multiples of 1/8 up to 2 times 32^-z.  An E2M3 code holds such a
+// Q of cache_attn_sinks and cache_attn_shared for many rows where it is rotated: a row, scaled by a power of two so that its largest
+// element is in [1, 2), as the sum of kTerms digits to the base 32, multiples of 1/8 up to 2 times 32^-z.  An E2M3 code holds such a
 // digit (its value times 8 and its sign are the code), and the matrix cores take 6-bit codes of Q and the 4-bit ones of K, as
 // they lie in the page, at four times the rate of 16 bits.  Five digits hold every element to within 2^-24 of the row's largest,
-// in 20 products of 32 cycles for a wave's 32 rows and 64 keys; two binary16 values needed 32, codes turned into
+// in 20 products of 32 cycles for a wave's 32 rows and 64 keys; two binary16 values need 32, codes turned into
 // binary16 and four times the LDS for K.  (sinks_prompt 545 -> 457 us, shared_documents 780 -> 674, shared_decode 98 -> 89;
 // four digits would leave 2e-6 of an lse over few keys.)
+//
+// Every element of a rotated row is a sum of all channels, rounded where binary32 forms it by 2^-24 of the partial sums, so
+// that digits as fine as the largest add no more.  Without the rotation one channel can be far larger than the rest while keys are
+// 0 there: what binary32 then holds to 2^-24 of the rest, digits would hold to 2^-24 of that channel (a channel 1000 times the
+// others: 2e-4 of a score, 2e-6 in binary32).  There many rows take two binary16 values, as few rows do, 2^-23 of each element
+// (sinks_prompt without rotation 441 us with digits, 523 so; shared_documents 675 and 766).
 constexpr int kTerms = 5;
 // 1.5 * 2^k with k such that adding it leaves multiples of 32^-z / 8
 __host__ __device__ constexpr float digit_of(int z) { return 1.5f * (1 << 20 >> (5 * z)); }
@@ -661,7 +667,7 @@ struct Rows {
 // second 16 rows were skipped inside the step).  N is therefore a constant.
 // Q is two binary16 values for binary32 outputs, and for all of cache_attn_sinks and cache_attn_shared: their lse is as
 // exact as binary32 arithmetic whatever the outputs' type.  (Two bf16 values left 2e-6 of an lse over few keys.)
-// For many rows these hold Q as digits.
+// For many rows these hold a rotated Q as digits.
 template <bool FINE, Keys K>
 constexpr bool fine_q() { return FINE || K != kAll; }
 
@@ -1175,26 +1181,25 @@ __device__ __forceinline__ float load_q6(const CacheAttnArgs& a, const Piece& p,
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
 // TERMS: bf16 values that hold P * (V's scale); three come with binary16 pairs of Q.
-template <int D, Keys K>
+template <int D>
 struct RowsLds {
   struct Scales {
     float ks[64], vs[64];
     unsigned long long there, plain;   // keys that are on a page; those of them with a finite V
   };
-  __align__(16) uint4 k[2][K == kAll ? D / 8 : D / 32][64];   // chunks of 8 channels in 16 bits, of 32 in 4
+  __align__(16) uint4 k[2][D / 8][64];   // chunks of 8 channels in 16 bits (digits: of 32 in 4, and fewer of them)
   __align__(16) uint4 v[2][8][D];
   Scales sc[2];
   SchedShared sched;
 };
 
-// Piece p of KV head h.
-template <int D, bool F16, int TERMS, Keys K>
-__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>& buf, Piece p, int h) {
-  constexpr bool SIX = K != kAll;          // Q as digits, K as it lies in the page
-  constexpr bool QF = TERMS == 3 || SIX;   // scores are multiplied by `back`
+// Piece p of KV head h.  SIX: Q as digits, K as it lies in the page.
+template <int D, bool F16, int TERMS, Keys K, bool SIX>
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& buf, Piece p, int h) {
+  constexpr bool QF = fine_q<TERMS == 3, K>();   // scores are multiplied by `back`
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
-  typedef typename RowsLds<D, K>::Scales Scales;
+  typedef typename RowsLds<D>::Scales Scales;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
@@ -1354,8 +1359,17 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>&
   uint32_t q6[D / 64][kTerms][6];   // digits
   float back = 1.0f;
   if constexpr (K == kShared) {
-    turned6<D>(a, p, h, row, hh, q6);
-    back = turned_back(a, p, h, row) * 0x1p14f;
+    back = turned_back(a, p, h, row);
+    if constexpr (SIX) {
+      turned6<D>(a, p, h, row, hh, q6);
+      back *= 0x1p14f;
+    } else {
+#pragma unroll
+      for (int kc = 0; kc < KC; ++kc) {
+        q[kc] = turned<D>(a, p, h, row, 0, hh * (D / 2) + kc * 8);
+        q_lo[kc] = turned<D>(a, p, h, row, 1, hh * (D / 2) + kc * 8);
+      }
+    }
   } else if constexpr (SIX) {
     back = load_q6<D, F16>(a, p, h, row, lane, q6);
   } else {
@@ -1698,12 +1712,21 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D, K>&
 
 // Piece x0 of KV head h.  TERMS 1: two for requests of few enough rows.
 template <int D, bool F16, int TERMS, Keys K>
-__device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, RowsLds<D, K>& buf, int x0, int h) {
+__device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, RowsLds<D>& buf, int x0, int h) {
   Piece p;
   if (!take_piece<128, K>(a, buf.sched, x0, a.target_rows, &p)) return;
-  if constexpr (K != kAll && TERMS == 1)
-    if (p.two) return many_rows<D, F16, 2, K>(a, buf, p, h);
-  many_rows<D, F16, TERMS, K>(a, buf, p, h);
+  if constexpr (K == kAll) {
+    many_rows<D, F16, TERMS, K, false>(a, buf, p, h);
+  } else {
+    auto go = [&](auto six) {
+      constexpr bool SIX = decltype(six)::value;
+      if constexpr (TERMS == 1)
+        if (p.two) return many_rows<D, F16, 2, K, SIX>(a, buf, p, h);
+      many_rows<D, F16, TERMS, K, SIX>(a, buf, p, h);
+    };
+    if (a.had) go(std::integral_constant<bool, true>{});
+    else go(std::integral_constant<bool, false>{});
+  }
 }
 
 // Joins the parts of split tiles, a workgroup for per_group rows: up to eight
@@ -1843,13 +1866,13 @@ __global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
 
 template <int D, bool F16, bool LO, Keys K>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
-  __shared__ RowsLds<D, K> lds;
+  __shared__ RowsLds<D> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   rows_piece<D, F16, LO ? 2 : 1, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, bool F16, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
-  __shared__ RowsLds<D, K> lds;
+  __shared__ RowsLds<D> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   rows_piece<D, F16, 3, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }

@@ -415,7 +415,8 @@ __device__ __forceinline__ void turn_q(const CacheAttnArgs& a, int64_t row) {
     *reinterpret_cast<uint4*>(dst) = hi;
     *reinterpret_cast<uint4*>(dst + D) = lo;
   }
-  // the digits' codes: |n| in eighths, and the sign
+  if (!a.had) return;
+  // digits (of a rotated row): codes |n| in eighths, and the sign
   uint16_t* six = reinterpret_cast<uint16_t*>(a.turned6 + row * row_bytes6<D>() + b * 6);
 #pragma unroll
   for (int e = 0; e < 8; ++e) y[e] *= 0x1p-14f;
@@ -473,7 +474,7 @@ __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a) {
   constexpr bool FINE = TERMS == 3;
   __shared__ union {
     FewLds<D, 1, true> few;
-    RowsLds<D, kShared> rows;
+    RowsLds<D> rows;
   } lds;
   const int x = blockIdx.x / a.g.Hkv, h = blockIdx.x - x * a.g.Hkv, many = __builtin_amdgcn_readfirstlane(a.counts[1]);
   if (x < many) rows_piece<D, F16, TERMS, kShared>(a, lds.rows, x, h);
