@@ -494,6 +494,12 @@ int rotate_attn_cache_attn_shared(const ra_cache_params* p, int32_t R, int32_t T
  * params alone, so that a captured graph follows the tables.  Calls on the same tables,
  * cache or workspace must be ordered by the caller (one stream, or events).
  *
+ * Layers.  A model's layers have one set of tables and a cache each, and every call moves
+ * the bytes of one.  For a model, each operator is called once per layer, on the same old
+ * tables and with the same arrays of their own for the new state (it comes out the same every
+ * time); these are the tables of the step after it.  In place only the first layer's call would
+ * find what there is to move.
+ *
  * status[0] is 0, or tells why the call was refused as a whole -- bit 0: a
  * length or number of a request that is impossible, bit 2: too few free pages, bit 3:
  * free_count impossible, bit 4 (compact): a page number on the stack that is none, or is there
