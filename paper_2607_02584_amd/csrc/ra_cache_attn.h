@@ -134,9 +134,9 @@ struct Piece {
 // How many bf16 values hold P times V's scale in a piece of many rows: as many as the output shows, so three for binary32
 // and two for binary16 outputs.  For bf16 ones one leaves as much error as their own rounding does (2.3e-3 of both, 1.65e-3
 // of the latter) and saves a quarter of the time where the matrix cores bind, as they do in requests of many rows (prompts
-// under a window 448 us with one value, 565 with two).  cache_attn_sinks and cache_attn_shared take it there only: a
+// under a window 451 us with one value, 560 with two).  cache_attn_sinks and cache_attn_shared take it there only: a
 // request's own rows (queries * Hq) decide, whatever else the call holds or has room for, and for a prefix the least of its
-// requests'.  (A decode step of 64 requests over a prefix of 32 700 tokens 88 us with one value, 98 with two.)
+// requests'.  (A decode step of 64 requests over a prefix of 32 700 tokens 90 us with one value, 100 with two.)
 constexpr int kTwoTerms = 512;   // rows of all heads up to which there are two
 
 struct SchedShared {
@@ -1181,25 +1181,32 @@ __device__ __forceinline__ float load_q6(const CacheAttnArgs& a, const Piece& p,
 // kAhead products ahead.  So K is staged two tiles ahead and V (with both
 // scales) one, and two LDS buffers of each suffice.
 // TERMS: bf16 values that hold P * (V's scale); three come with binary16 pairs of Q.
-template <int D>
-struct RowsLds {
+template <int D, bool SIX>
+struct TilesLds {
   struct Scales {
     float ks[64], vs[64];
     unsigned long long there, plain;   // keys that are on a page; those of them with a finite V
   };
-  __align__(16) uint4 k[2][D / 8][64];   // chunks of 8 channels in 16 bits (digits: of 32 in 4, and fewer of them)
+  __align__(16) uint4 k[2][SIX ? D / 32 : D / 8][64];   // chunks of 8 channels in 16 bits, of 32 in 4
   __align__(16) uint4 v[2][8][D];
   Scales sc[2];
-  SchedShared sched;
+};
+template <int D, Keys K>
+struct RowsLds {
+  union {
+    TilesLds<D, false> pairs;
+    TilesLds<D, K != kAll> six;
+  };
+  SchedShared sched;   // (read while the first waves fill tiles)
 };
 
 // Piece p of KV head h.  SIX: Q as digits, K as it lies in the page.
 template <int D, bool F16, int TERMS, Keys K, bool SIX>
-__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& buf, Piece p, int h) {
+__device__ __forceinline__ void many_rows(const CacheAttnArgs& a, TilesLds<D, SIX>& buf, Piece p, int h) {
   constexpr bool QF = fine_q<TERMS == 3, K>();   // scores are multiplied by `back`
   typedef typename std::conditional<D == 128, uint4, uint2>::type Codes;   // a lane's share of 16 tokens
   constexpr int NW = 4, M = 32 * NW, E = D / 16, KC = D / 16, MT = D / 32;
-  typedef typename RowsLds<D>::Scales Scales;
+  typedef typename TilesLds<D, SIX>::Scales Scales;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int hh = lane >> 5, j = lane & 31;
   const bool prefix = K == kShared && p.r < a.groups;   // causal only: its rows may be at any position
@@ -1710,22 +1717,34 @@ __device__ __forceinline__ void many_rows(const CacheAttnArgs& a, RowsLds<D>& bu
   if (a.lse && hh == 0) a.lse[out] = l == 0.0f ? kNegInf : (m + log2f(l)) * kLn2;
 }
 
+// The kernel's first argument, read again: of several bodies in one kernel each has its own copy, or what they share is loaded
+// ahead of them and kept in scalar registers that their loops lack (24 moves out of spilled ones for each tile of keys,
+// sinks_prompt 452 us instead of 444).
+__device__ __forceinline__ const CacheAttnArgs& own_args() {
+  typedef const __attribute__((address_space(4))) CacheAttnArgs* Args;
+  Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+#if defined(__HIP_DEVICE_COMPILE__)
+  asm volatile("" : "+s"(a));
+#endif
+  return *(const CacheAttnArgs*)a;
+}
+
 // Piece x0 of KV head h.  TERMS 1: two for requests of few enough rows.
 template <int D, bool F16, int TERMS, Keys K>
-__device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, RowsLds<D>& buf, int x0, int h) {
+__device__ __forceinline__ void rows_piece(const CacheAttnArgs& a, RowsLds<D, K>& buf, int x0, int h) {
   Piece p;
   if (!take_piece<128, K>(a, buf.sched, x0, a.target_rows, &p)) return;
   if constexpr (K == kAll) {
-    many_rows<D, F16, TERMS, K, false>(a, buf, p, h);
+    many_rows<D, F16, TERMS, K, false>(a, buf.pairs, p, h);
   } else {
-    auto go = [&](auto six) {
+    auto go = [&](auto six, auto& tiles) {
       constexpr bool SIX = decltype(six)::value;
       if constexpr (TERMS == 1)
-        if (p.two) return many_rows<D, F16, 2, K, SIX>(a, buf, p, h);
-      many_rows<D, F16, TERMS, K, SIX>(a, buf, p, h);
+        if (p.two) return many_rows<D, F16, 2, K, SIX>(own_args(), tiles, p, h);
+      many_rows<D, F16, TERMS, K, SIX>(own_args(), tiles, p, h);
     };
-    if (a.had) go(std::integral_constant<bool, true>{});
-    else go(std::integral_constant<bool, false>{});
+    if (a.had) go(std::integral_constant<bool, true>{}, buf.six);
+    else go(std::integral_constant<bool, false>{}, buf.pairs);
   }
 }
 
@@ -1866,13 +1885,13 @@ __global__ __launch_bounds__(256, 2) void k_fine_few(CacheAttnArgs a) {
 
 template <int D, bool F16, bool LO, Keys K>
 __global__ __launch_bounds__(256, 2) void k_rows(CacheAttnArgs a) {
-  __shared__ RowsLds<D> lds;
+  __shared__ RowsLds<D, K> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   rows_piece<D, F16, LO ? 2 : 1, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }
 template <int D, bool F16, Keys K>
 __global__ __launch_bounds__(256, 2) void k_fine_rows(CacheAttnArgs a) {
-  __shared__ RowsLds<D> lds;
+  __shared__ RowsLds<D, K> lds;
   const int x0 = blockIdx.x / a.g.Hkv;
   rows_piece<D, F16, 3, K>(a, lds, x0, blockIdx.x - x0 * a.g.Hkv);
 }

@@ -474,7 +474,7 @@ __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a) {
   constexpr bool FINE = TERMS == 3;
   __shared__ union {
     FewLds<D, 1, true> few;
-    RowsLds<D> rows;
+    RowsLds<D, kShared> rows;
   } lds;
   const int x = blockIdx.x / a.g.Hkv, h = blockIdx.x - x * a.g.Hkv, many = __builtin_amdgcn_readfirstlane(a.counts[1]);
   if (x < many) rows_piece<D, F16, TERMS, kShared>(a, lds.rows, x, h);

@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256, 2) void k_both(CacheAttnArgs a, int rows) {
   constexpr bool FINE = TERMS == 3;
   __shared__ union {
     FewLds<D, 2, true> few;
-    RowsLds<D> rows;
+    RowsLds<D, kSinks> rows;
   } lds;
   const bool many = static_cast<int>(blockIdx.x) < rows;
   const int x = many ? blockIdx.x : blockIdx.x - rows, x0 = x / a.g.Hkv, h = x - x0 * a.g.Hkv;
