@@ -405,8 +405,8 @@ __device__ __forceinline__ bool take_piece(const CacheAttnArgs& a, SchedShared& 
 // binary16 and four times the LDS for K.  (sinks_prompt 545 -> 457 us, shared_documents 780 -> 674, shared_decode 98 -> 89;
 // four digits would leave 2e-6 of an lse over few keys.)
 //
-// Every element of a rotated row is a sum of all channels, rounded where binary32 forms it by 2^-24 of the partial sums, so
-// that digits as fine as the largest add no more.  Without the rotation one channel can be far larger than the rest while keys are
+// Every element of a rotated row is a sum of all channels, which binary32 rounds by 2^-24 of its partial sums: no finer, as a
+// rule, than digits hold it.  Without the rotation one channel can be far larger than the rest while keys are
 // 0 there: what binary32 then holds to 2^-24 of the rest, digits would hold to 2^-24 of that channel (a channel 1000 times the
 // others: 2e-4 of a score, 2e-6 in binary32).  There many rows take two binary16 values, as few rows do, 2^-23 of each element
 // (sinks_prompt without rotation 441 us with digits, 523 so; shared_documents 675 and 766).

@@ -18,8 +18,8 @@
 // rows come first in the grid and are cut for their share of the places that the
 // card has, so that those of few run beside them from the start: 64 requests on a
 // prefix of 32 700 tokens took 117 us with one launch after the other, 101 with the
-// two kinds alternating (whoever waits for a place ends as much later), 96 so (now
-// 88, with Q in digits).
+// two kinds alternating (whoever waits for a place ends as much later), 96 so (88 with
+// Q in digits, now 98, with two values of the weights).
 //
 // Bound by HBM while a group's rows are few, by the matrix cores and the softmax
 // beside them from some 64 rows on.
