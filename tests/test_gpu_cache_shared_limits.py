@@ -46,3 +46,16 @@ def test_impossible_prefixes(ra, long, low, queries, out):
     for t in (o, lse):
         assert (t[:32] == 7.0).all() and (t[32 + live:] == 7.0).all()
     assert (ws[:2048] == 0x33).all() and (ws[2048 + size:] == 0x33).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,had", [(8, 2, True), (6, 6, False)])
+def test_prompts_behind_a_prefix(ra, Hq, Hkv, had):
+    """Hundreds to thousands of new tokens a request behind a cached prefix, beside requests that decode: what cache_attn
+    gives, both within 2^-18 of 64-bit results with binary32 outputs."""
+    qs = [2000, 1, 700, 3300, 1, 0, 513]
+    lens = [3000 + 1 + 7 * i + q for i, q in enumerate(qs)]
+    c = Case(ra, Hq, Hkv, 128, 64, lens, qs, out="fp32", rope=True, had=had, groups=[(0, 5, 3000), (5, 7, 3000)], seed=9, pad=30)
+    x, lse = (t.clone() for t in c.run())
+    c.groups = []
+    y, lse2 = c.run()
+    assert (x - y).abs().max() <= 2.0 ** -17 * y.abs().max() and (lse - lse2).abs().max() <= 2.0 ** -17
